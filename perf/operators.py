@@ -137,7 +137,8 @@ def _draw(rng):
                      len_hi=hi, spare=rng.choice([0, 1, 37]))
     cp, batch = rng.choice([1, 1, 2, 8]), rng.choice([1, 1, 2, 5])
     lo = rng.choice([16, 64, 256, 576])
-    seq, keys = _log(rng, 1, 131072), _log(rng, 1, 40139)
+    # with one state to see, the gradients of q and k are zero and a plain form's rounding noise: 16 and more there
+    seq, keys = _log(rng, 1, 131072), _log(rng, 16 if op == "attend_train" else 1, 40139)
     seq = max(1, round(seq / (2 * cp))) * 2 * cp if cp > 1 else seq
     most = (MOST_SCORES if op == "attend" else MOST_SCORES_TRAIN) / (8 if f32 else 1)
     scores = batch * (seq // cp) * batch * keys
