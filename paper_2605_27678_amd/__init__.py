@@ -4,6 +4,8 @@ kernels (libhp.so) plus this thin binding."""
 from .binding import (HpError, Plan, hp_backward, hp_backward_accumulate, hp_forward, hp_forward_static, hp_zero_image_rows, hp_text_grads, hp_get_option, hp_plan_create,
                       hp_plan_create_batched, hp_plan_create_host, hp_plan_create_joined, hp_plan_tune, hp_probe_stream, hp_probe_stream_ex,
                       hp_forget_tuned_shapes, hp_release_cached_memory, hp_profile_enable, hp_profile_read, hp_set_option, hp_version)
+from .operators import (RotaryScaling, hp_cross_attend, hp_cross_attend_backward, hp_cross_attend_step, hp_cross_attend_workspace,
+                        hp_gated_norm, hp_gated_norm_backward, hp_gated_norm_workspace, hp_image_ranges, hp_rotary, hp_rotary_table)
 from .workloads import Grid, TokenMap
 
 
@@ -16,4 +18,6 @@ def boundary_transform(plan, src_bufs, text_bufs):
 
 
 __all__ = ["Grid", "TokenMap", "boundary_transform", "Plan", "HpError", "hp_plan_create", "hp_plan_create_host", "hp_plan_create_batched", "hp_plan_create_joined", "hp_plan_tune", "hp_probe_stream", "hp_probe_stream_ex", "hp_release_cached_memory", "hp_forget_tuned_shapes",
-           "hp_forward", "hp_forward_static", "hp_zero_image_rows", "hp_text_grads", "hp_backward", "hp_backward_accumulate", "hp_set_option", "hp_get_option", "hp_profile_enable", "hp_profile_read", "hp_version"]
+           "hp_forward", "hp_forward_static", "hp_zero_image_rows", "hp_text_grads", "hp_backward", "hp_backward_accumulate", "hp_set_option", "hp_get_option", "hp_profile_enable", "hp_profile_read", "hp_version",
+           "RotaryScaling", "hp_rotary_table", "hp_rotary", "hp_gated_norm", "hp_gated_norm_backward", "hp_gated_norm_workspace",
+           "hp_cross_attend", "hp_cross_attend_step", "hp_cross_attend_backward", "hp_cross_attend_workspace", "hp_image_ranges"]

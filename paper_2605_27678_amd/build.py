@@ -13,7 +13,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_PKG)
 CSRC = os.path.join(_PKG, "csrc")
 LIB_PATH = os.path.join(_PKG, "libhp.so")
-SOURCES = ["hp_api.hip", "hp_plan.cpp"]
+SOURCES = ["hp_api.hip", "hp_plan.cpp", "hp_attend.hip", "hp_norm.hip", "hp_rotary.hip", "hp_ranges.cpp"]
 MARSHAL_PATH = os.path.join(_PKG, "hp_marshal.so")
 
 HIPCC_FLAGS = [
@@ -70,17 +70,29 @@ def build_marshal(verbose: bool = False) -> Optional[str]:
 def build_library(verbose: bool = False, extra_flags=()) -> str:
     """Compile every source for gfx950 into paper_2605_27678_amd/libhp.so, and
     the marshalling extension beside it where that can be built."""
+    import tempfile
+    from concurrent.futures import ThreadPoolExecutor
     build_marshal(verbose)
-    cmd = [hipcc_path(), *HIPCC_FLAGS, *extra_flags,
-           "-I", os.path.join(_ROOT, "include"), "-I", CSRC,
-           "-o", LIB_PATH, *[os.path.join(CSRC, s) for s in SOURCES]]
-    if verbose:
-        print(" ".join(cmd), flush=True)
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        raise RuntimeError("hipcc failed:\n" + res.stdout + res.stderr)
-    if verbose and res.stderr.strip():
-        print(res.stderr)
+    inc = ["-I", os.path.join(_ROOT, "include"), "-I", CSRC]
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd), flush=True)
+        return subprocess.run(cmd, capture_output=True, text=True)
+
+    with tempfile.TemporaryDirectory() as tmp:         # the sources one by one, at a time as many as there are
+        objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
+        compile_flags = [f for f in HIPCC_FLAGS if f != "-shared"]
+        with ThreadPoolExecutor(len(SOURCES)) as pool:
+            done = list(pool.map(run, [[hipcc_path(), *compile_flags, *extra_flags, *inc, "-c", "-o", o, os.path.join(CSRC, s)]
+                                       for s, o in zip(SOURCES, objects)]))
+        if all(r.returncode == 0 for r in done):
+            done.append(run([hipcc_path(), "-shared", "-fPIC", "--offload-arch=gfx950", "-o", LIB_PATH, *objects]))
+    for res in done:
+        if res.returncode != 0:
+            raise RuntimeError("hipcc failed:\n" + res.stdout + res.stderr)
+        if verbose and res.stderr.strip():
+            print(res.stderr)
     return LIB_PATH
 
 

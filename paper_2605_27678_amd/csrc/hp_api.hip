@@ -23,6 +23,7 @@
 #include <vector>
 
 #include "hp.h"
+#include "hp_error.hpp"
 #include "hp_plan.hpp"
 #include "hp_tile.hpp"
 
@@ -34,6 +35,12 @@ using hp::KParams;
 using hp::TileView;
 
 thread_local int g_last_hip_error = 0;
+}  // namespace
+
+// for the calls whose kernels are in other files (hp_error.hpp)
+void hp::note_hip_error(int e) { g_last_hip_error = e; }
+
+namespace {
 
 inline bool hip_failed(hipError_t e) {
     if (e == hipSuccess) return false;

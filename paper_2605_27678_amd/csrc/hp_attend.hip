@@ -1,0 +1,979 @@
+// Attention of packed query rows to packed states: row r sees the states lo(r) .. hi(r) - 1.
+//     s = scale q k^T,  p = exp(s - m) / sum,  out = p v
+// in one pass over the states with a running maximum m and sum, and backward, with P = exp(s - lse) and
+// delta = sum over channels of dout out,
+//     dv = P^T dout,  dS = P (dout v^T - delta),  dq = scale dS k,  dk = scale dS^T q.
+//
+// The query heads that share a state head are rows of one matrix: its row M = row * group + head of the group, so a
+// tile of states serves all of them, and their gradients add up in the accumulators.
+//
+// Every product is v_mfma_f32_32x32x16_bf16, or eight v_mfma_f32_32x32x2_f32 over the same 16 values for binary32, and
+// is laid out so that no intermediate leaves the registers.  For such a product lane l holds, of the left operand, row
+// l % 32, of the right one column l % 32, and of the result column l % 32 and rows 8b + 4(l / 32) + t (b, t < 4).  With the
+// states on the left, S^T = K Q^T, each lane has scores of one query row, so maxima and sums are taken within the lane and
+// its partner l ^ 32; and the rows that a lane holds of P^T are, taken eight at a time, the 8 of 16 inner values that it
+// has to hold of the right operand of the next product, out^T = V^T P^T, if V^T is read with its keys in that order.  That
+// left operand comes from V as it lies in memory, by the transposing LDS load (four keys of one channel in a lane).
+//
+// A row must not feel what it does not see, and 0 * inf is NaN: scores are masked by selection, and where a tile of
+// states that not all rows of a wave see holds an infinity or NaN, its product is made value by value instead
+// (careful_product).
+#include <cfloat>
+#include <climits>
+#include <cmath>
+
+#include "hp_device.hpp"
+#include "hp_operators.h"
+
+#pragma clang fp contract(fast)
+
+namespace {
+
+using namespace hp;
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr int kBlock = 256, kWaves = kBlock / kWave;
+constexpr int kTileM = 32 * kWaves;                 // query rows (times group) of a workgroup
+constexpr int kStepKeys = 32 * kWaves;              // states that a workgroup of the single-token kernel takes at a time
+
+typedef float Acc __attribute__((ext_vector_type(16)));
+template <class T> using Frag = Vec<T, 8>;
+
+struct Attend {
+    int64_t rows, keys;
+    int32_t heads_q, heads_k, group, dim, splits, m_total;
+    float scale, scale2;                            // scale2: for exponents of two
+    hp_heads_t q, k, v, out, dout, dq, dk, dv;
+    const int32_t *ranges;
+    float *lse;
+    float *part, *part_lse;                         // [splits][rows * heads_q][dim], [splits][rows * heads_q]
+    float *delta;                                   // [rows * heads_q]
+    int4 *bounds;                                   // of each 32 rows M
+    float *part_k, *part_v;                         // [splits][keys * heads_k][dim]
+};
+
+__device__ __forceinline__ Acc mma(const Frag<__bf16> &a, const Frag<__bf16> &b, const Acc &c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ Acc mma(const Frag<float> &a, const Frag<float> &b, Acc c) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+    return c;
+}
+
+// Elements between rows of a tile in LDS: 32 bytes more than the row, so that eight rows at one place, and four rows
+// of 32 bytes, lie in different banks.
+template <class T, int DP> constexpr int kLd = DP + 32 / (int)sizeof(T);
+
+// Row `row` of a tile, channels 16s + 8(l / 32) and on: an operand whose inner index is the channel.
+template <class T> __device__ __forceinline__ Frag<T> row_frag(const T *tile, int ld, int row, int s, int half) {
+    typedef Frag<T> aligned __attribute__((aligned(16)));
+    return *(const aligned *)(tile + row * ld + 16 * s + 8 * half);
+}
+
+// Rows 16 ks + 4(l / 32) + {0..3} and 8 more of a tile, at channel 32 db + l % 32: a left operand whose inner index is
+// the tile's row, in the order in which a lane holds the rows of a result.
+template <class T> __device__ __forceinline__ Frag<T> column_frag(const T *tile, int ld, int ks, int db, int lane) {
+    if constexpr (sizeof(T) == 2) {
+        typedef short Quad __attribute__((ext_vector_type(4)));
+        typedef __attribute__((address_space(3))) Quad *Lds;
+        const int i = lane % 16, row = 16 * ks + 4 * (lane / 32) + i / 4, col = 32 * db + 16 * ((lane / 16) % 2) + 4 * (i % 4);
+        const T *p = tile + row * ld + col;
+        union {
+            Quad q[2];
+            Frag<T> f;
+        } u;
+        u.q[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)p);
+        u.q[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p + 8 * ld));
+        return u.f;
+    } else {
+        Frag<T> f;
+        const T *p = tile + (16 * ks + 4 * (lane / 32)) * ld + 32 * db + lane % 32;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = p[(8 * (j / 4) + j % 4) * ld];
+        return f;
+    }
+}
+
+// Eight of a result's rows as the right operand of the next product.
+template <class T> __device__ __forceinline__ Frag<T> result_frag(const Acc &r, int eighths) {
+    Frag<T> f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = (T)r[8 * eighths + j];          // rounded to nearest even for bf16
+    return f;
+}
+
+__device__ __forceinline__ int result_row(int i, int half) { return 8 * (i / 4) + 4 * half + i % 4; }
+
+// The values of lanes l % 32 and l % 32 + 32.
+__device__ __forceinline__ float2 both_halves(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return make_float2(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+template <class T> __device__ __forceinline__ bool not_finite(const Frag<T> &f) {
+    bool bad = false;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        if constexpr (sizeof(T) == 2) bad |= (__builtin_bit_cast(uint16_t, f[j]) & 0x7f80) == 0x7f80;
+        else bad |= (__builtin_bit_cast(uint32_t, f[j]) & 0x7f800000) == 0x7f800000;
+    }
+    return bad;
+}
+
+// acc^T += tile^T p^T over the 32 rows of a tile that p holds, leaving out what is not seen: for values there that are
+// not finite, which a product would carry into every row.
+template <class T, int DB, class Seen>
+__device__ __forceinline__ void careful_product(Acc (&acc)[DB], const Acc &p, const T *tile, int ld, int half, const Seen &seen) {
+    for (int j = 0; j < 32; ++j) {
+        float own = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) own = i == 4 * (j / 8) + j % 4 ? p[i] : own;
+        const float2 two = both_halves(own);
+        const float w = (j / 4) % 2 ? two.y : two.x;
+        if (!seen(j)) continue;
+        const T *row = tile + j * ld;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[db][i] += w * (float)row[32 * db + result_row(i, half)];
+    }
+}
+
+// A tile of ROWS rows on its way from memory through registers to LDS; channels from dim on are zeros.
+template <class T, int DP, int ROWS, int THREADS> struct Stage {
+    static constexpr int kChunks = DP / 8, kEach = (ROWS * kChunks + THREADS - 1) / THREADS;
+    Frag<T> r[kEach];
+    // at(row): the row's address, or NULL for zeros
+    template <class At> __device__ __forceinline__ void fetch(int tid, int dim, const At &at) {
+#pragma unroll
+        for (int n = 0; n < kEach; ++n) {
+            const int e = n * THREADS + tid, row = e / kChunks, c = e % kChunks;
+            const T *p = row < ROWS ? at(row) : nullptr;
+            r[n] = load<8>(p + 8 * c, p ? dim - 8 * c : 0);
+        }
+    }
+    __device__ __forceinline__ bool commit(T *tile, int tid, bool look) {
+        typedef Frag<T> aligned __attribute__((aligned(16)));
+        bool bad = false;
+#pragma unroll
+        for (int n = 0; n < kEach; ++n) {
+            const int e = n * THREADS + tid, row = e / kChunks, c = e % kChunks;
+            if (row < ROWS) *(aligned *)(tile + row * kLd<T, DP> + 8 * c) = r[n];
+            if (look) bad |= not_finite<T>(r[n]);
+        }
+        return bad;
+    }
+};
+
+// What one query row sees.
+struct Range {
+    int lo, hi;
+    __device__ __forceinline__ bool empty() const { return lo >= hi; }
+    __device__ __forceinline__ bool has(int key) const { return key >= lo && key < hi; }
+};
+__device__ __forceinline__ Range range_of(const Attend &p, int64_t row) {
+    Range r{0, (int)p.keys};
+    if (p.ranges) {
+        r.lo = max(p.ranges[2 * row], 0);
+        r.hi = min(p.ranges[2 * row + 1], (int)p.keys);
+    }
+    if (r.lo >= r.hi) r.lo = r.hi = 0;
+    return r;
+}
+
+// first .. end: what any of some rows sees; all .. all_end: what all of them see (rows that see nothing count for neither).
+struct Bounds {
+    int first, end, all, all_end;
+    __device__ __forceinline__ void add(const Bounds &o) {
+        first = min(first, o.first), end = max(end, o.end), all = max(all, o.all), all_end = min(all_end, o.all_end);
+    }
+    __device__ __forceinline__ bool meets(int a, int b) const { return a < end && b > first; }
+    __device__ __forceinline__ bool covers(int a, int b) const { return a >= all && b <= all_end; }
+};
+__device__ __forceinline__ Bounds bounds_of(const Range &r, bool counts) {
+    return counts && !r.empty() ? Bounds{r.lo, r.hi, r.lo, r.hi} : Bounds{INT_MAX, INT_MIN, INT_MIN, INT_MAX};
+}
+__device__ __forceinline__ Bounds over_columns(Bounds b) {              // of the 32 rows of a wave
+#pragma unroll
+    for (int d = 16; d; d /= 2) b.add(Bounds{__shfl_xor(b.first, d), __shfl_xor(b.end, d), __shfl_xor(b.all, d), __shfl_xor(b.all_end, d)});
+    return Bounds{__builtin_amdgcn_readfirstlane(b.first), __builtin_amdgcn_readfirstlane(b.end),
+                  __builtin_amdgcn_readfirstlane(b.all), __builtin_amdgcn_readfirstlane(b.all_end)};
+}
+__device__ __forceinline__ Bounds over_waves(const Bounds &mine, Bounds *slots, int wave, int lane) {
+    if (lane == 0) slots[wave] = mine;
+    __syncthreads();
+    Bounds b = slots[0];
+    for (int w = 1; w < kWaves; ++w) b.add(slots[w]);
+    return Bounds{__builtin_amdgcn_readfirstlane(b.first), __builtin_amdgcn_readfirstlane(b.end),
+                  __builtin_amdgcn_readfirstlane(b.all), __builtin_amdgcn_readfirstlane(b.all_end)};
+}
+
+// A lane's place: its column of the wave's 32 rows M.
+struct Place {
+    int m, row, head;
+    bool valid;
+};
+__device__ __forceinline__ Place place_of(const Attend &p, int m, int state_head) {
+    Place at;
+    at.valid = m < p.m_total;
+    at.m = at.valid ? m : p.m_total - 1;
+    at.row = at.m / p.group;
+    at.head = state_head * p.group + (at.m - at.row * p.group);
+    return at;
+}
+template <class T> __device__ __forceinline__ T *address(const hp_heads_t &t, int64_t row, int head) {
+    return (T *)t.data + row * t.row_stride + (int64_t)head * t.head_stride;
+}
+
+// The running maximum, sum and product of one query row in a lane and its partner.  `top` is a maximum of s * scale2
+// that lags: it is raised when a score passes it by 2^8, so that most tiles leave the product as it is.
+struct Running {
+    float top = -INFINITY, sum = 0.0f;
+};
+constexpr float kLag = 8.0f;
+
+// Scores (unscaled) of NB blocks of 32 states -> exponentials, with the statistics and the product so far brought up.
+template <int NB, int DB> __device__ __forceinline__ void soften(Running &run, Acc (&s)[NB], Acc (&acc)[DB], float scale2) {
+    float top = s[0][0];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, s[b][i]);
+    const float2 two = both_halves(top);
+    top = fmaxf(two.x, two.y) * scale2;
+    const bool grows = top > run.top + kLag;
+    if (__any(grows)) {
+        const float next = grows ? top : run.top;
+        const float keep = grows ? __builtin_amdgcn_exp2f(run.top - next) : 1.0f;
+        run.top = next;
+        run.sum *= keep;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[db][i] *= keep;
+    }
+    const float base = run.top == -INFINITY ? 0.0f : run.top;
+    float sum = 0.0f;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            s[b][i] = __builtin_amdgcn_exp2f(s[b][i] * scale2 - base);
+            sum += s[b][i];
+        }
+    run.sum += sum;
+}
+
+// Writes a lane's part of a result^T: column l % 32 is one row of `to`.
+template <class T, int DB> __device__ __forceinline__ void store_result(T *to, const Acc (&acc)[DB], float scale, int dim, int half) {
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            Vec<T, 4> v;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) v[t] = (T)(acc[db][4 * b + t] * scale);
+            const int d = 32 * db + 8 * b + 4 * half;
+            store<4>(to + d, v, dim - d);
+        }
+}
+
+// Whether a tile is loaded into registers while the one before it is worked on: where 1 KiB rows leave no room for it,
+// tiles go to LDS as they come.
+template <class T, int DP> constexpr bool kAhead = DP < 256;
+
+template <class T> constexpr int kTileKeys = sizeof(T) == 2 ? 64 : 32;
+
+// One workgroup: 128 rows M against a part of what they see.
+template <class T, int DP> __global__ __launch_bounds__(kBlock) void attend_forward_kernel(Attend p) {
+    constexpr int NK = kTileKeys<T>, NB = NK / 32, DB = DP / 32, DS = DP / 16, LD = kLd<T, DP>;
+    __shared__ __attribute__((aligned(16))) T k_tile[NK * LD], v_tile[NK * LD];
+    __shared__ Bounds slots[kWaves];
+    __shared__ int bad[2];                           // by turns: the one of the next tile is cleared where all are done with the last
+    const int tid = (int)threadIdx.x, lane = tid % kWave, wave = tid / kWave, half = lane / 32, col = lane % 32;
+    const int state_head = (int)blockIdx.y, split = (int)blockIdx.z;
+    // later rows tend to see more: they begin first
+    const Place at = place_of(p, ((int)gridDim.x - 1 - (int)blockIdx.x) * kTileM + 32 * wave + col, state_head);
+    const Range see = range_of(p, at.row);
+    const Bounds own = over_columns(bounds_of(see, at.valid));
+    if (tid < 2) bad[tid] = 0;
+    const Bounds any = over_waves(own, slots, wave, lane);
+    Frag<T> q[DS];
+#pragma unroll
+    for (int s = 0; s < DS; ++s) {
+        const int d = 16 * s + 8 * half;
+        q[s] = load<8>(address<const T>(p.q, at.row, at.head) + d, p.dim - d);
+    }
+    Running run;
+    Acc acc[DB] = {};
+    const int tiles = any.end > any.first ? (any.end - any.first + NK - 1) / NK : 0;
+    const int begin = (int)((int64_t)tiles * split / p.splits), end = (int)((int64_t)tiles * (split + 1) / p.splits);
+    Stage<T, DP, NK, kBlock> ks, vs;
+    auto fetch_k = [&](int tile) {
+        const int key0 = any.first + tile * NK;
+        ks.fetch(tid, p.dim, [&](int r) { return key0 + r < any.end ? address<const T>(p.k, key0 + r, state_head) : nullptr; });
+    };
+    auto fetch_v = [&](int tile) {
+        const int key0 = any.first + tile * NK;
+        vs.fetch(tid, p.dim, [&](int r) { return key0 + r < any.end ? address<const T>(p.v, key0 + r, state_head) : nullptr; });
+    };
+    if (kAhead<T, DP> && begin < end) fetch_k(begin), fetch_v(begin);
+    for (int tile = begin; tile < end; ++tile) {
+        const int key0 = any.first + tile * NK;
+        const bool look = !any.covers(key0, key0 + NK);
+        const int turn = (tile - begin) % 2;
+        __syncthreads();                             // the last tile's readers are done
+        if (tid == 0) bad[turn ^ 1] = 0;
+        if constexpr (!kAhead<T, DP>) fetch_k(tile);
+        ks.commit(k_tile, tid, false);
+        if constexpr (!kAhead<T, DP>) fetch_v(tile);
+        if (vs.commit(v_tile, tid, look)) bad[turn] = 1;
+        __syncthreads();
+        if (kAhead<T, DP> && tile + 1 < end) fetch_k(tile + 1), fetch_v(tile + 1);
+        if (!own.meets(key0, key0 + NK)) continue;
+        Acc s[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            s[b] = Acc{};
+#pragma unroll
+            for (int d = 0; d < DS; ++d) s[b] = mma(row_frag(k_tile, LD, 32 * b + col, d, half), q[d], s[b]);
+        }
+        const bool whole = own.covers(key0, key0 + NK);
+        if (!whole)
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    s[b][i] = see.has(key0 + 32 * b + result_row(i, half)) ? s[b][i] : -INFINITY;
+        soften(run, s, acc, p.scale2);
+        if (!whole && bad[turn]) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+                careful_product<T, DB>(acc, s[b], v_tile + 32 * b * LD, LD, half, [&](int j) { return see.has(key0 + 32 * b + j); });
+            continue;
+        }
+#pragma unroll
+        for (int k = 0; k < 2 * NB; ++k) {
+            const Frag<T> w = result_frag<T>(s[k / 2], k % 2);
+#pragma unroll
+            for (int db = 0; db < DB; ++db) acc[db] = mma(column_frag(v_tile, LD, k, db, lane), w, acc[db]);
+        }
+    }
+    const float2 two = both_halves(run.sum);
+    const float sum = two.x + two.y;
+    const bool none = see.empty() || sum == 0.0f;
+    if (none)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) acc[db] = Acc{};
+    const float inv = none ? 0.0f : 1.0f / sum, lse2 = none ? -INFINITY : run.top + __builtin_amdgcn_logf(sum);
+    if (!at.valid) return;
+    const int64_t out_row = (int64_t)at.row * p.heads_q + at.head;
+    if (p.splits > 1) {
+        const int64_t n = p.rows * p.heads_q;
+        store_result(p.part + (split * n + out_row) * p.dim, acc, inv, p.dim, half);
+        if (half == 0) p.part_lse[split * n + out_row] = lse2;
+        return;
+    }
+    store_result(address<T>(p.out, at.row, at.head), acc, inv, p.dim, half);
+    if (p.lse && half == 0) p.lse[out_row] = lse2 * kLn2;
+}
+
+// One workgroup: up to 32 heads of one row against a part of what the row sees.  The waves take 32 states each on their
+// own, without waiting for one another, and join at the end.
+// Waves of a workgroup: as LDS has room for their tiles.
+template <class T, int DP> constexpr int kStepWaves = DP * sizeof(T) <= 512 ? 4 : 2;
+
+template <class T, int DP> __global__ __launch_bounds__((kStepWaves<T, DP> * kWave)) void attend_step_kernel(Attend p) {
+    constexpr int kWaves = kStepWaves<T, DP>, DB = DP / 32, DS = DP / 16, LD = kLd<T, DP>;
+    __shared__ __attribute__((aligned(16))) T tiles[kWaves][2][32 * LD];
+    __shared__ float tops[kWaves][32], sums[kWaves][32];
+    const int tid = (int)threadIdx.x, lane = tid % kWave, wave = tid / kWave, half = lane / 32, col = lane % 32;
+    const int64_t row = blockIdx.x;
+    const int parts = (p.group + 31) / 32, state_head = (int)blockIdx.y / parts, first_head = ((int)blockIdx.y % parts) * 32;
+    const int split = (int)blockIdx.z;
+    const int heads = min(p.group - first_head, 32), head0 = state_head * p.group + first_head;
+    const Range see = range_of(p, row);
+    T *k_tile = tiles[wave][0], *v_tile = tiles[wave][1];
+    Frag<T> q[DS];
+#pragma unroll
+    for (int s = 0; s < DS; ++s) {
+        const int d = 16 * s + 8 * half;
+        q[s] = load<8>(address<const T>(p.q, row, head0 + min(col, heads - 1)) + d, p.dim - d);
+    }
+    Running run;
+    Acc acc[DB] = {};
+    const int n_tiles = (see.hi - see.lo + 31) / 32;
+    const int begin = (int)((int64_t)n_tiles * split / p.splits), end = (int)((int64_t)n_tiles * (split + 1) / p.splits);
+    Stage<T, DP, 32, kWave> ks, vs;
+    auto fetch_k = [&](int tile) {
+        const int key0 = see.lo + tile * 32;
+        ks.fetch(lane, p.dim, [&](int r) { return key0 + r < see.hi ? address<const T>(p.k, key0 + r, state_head) : nullptr; });
+    };
+    auto fetch_v = [&](int tile) {
+        const int key0 = see.lo + tile * 32;
+        vs.fetch(lane, p.dim, [&](int r) { return key0 + r < see.hi ? address<const T>(p.v, key0 + r, state_head) : nullptr; });
+    };
+    if (kAhead<T, DP> && begin + wave < end) fetch_k(begin + wave), fetch_v(begin + wave);
+    for (int tile = begin + wave; tile < end; tile += kWaves) {
+        const int key0 = see.lo + tile * 32;
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");     // the wave's own LDS: its loads of the last tile come first
+        if constexpr (!kAhead<T, DP>) fetch_k(tile);
+        ks.commit(k_tile, lane, false);
+        if constexpr (!kAhead<T, DP>) fetch_v(tile);
+        vs.commit(v_tile, lane, false);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        if (kAhead<T, DP> && tile + kWaves < end) fetch_k(tile + kWaves), fetch_v(tile + kWaves);
+        Acc s[1] = {};
+#pragma unroll
+        for (int d = 0; d < DS; ++d) s[0] = mma(row_frag(k_tile, LD, col, d, half), q[d], s[0]);
+        if (key0 + 32 > see.hi)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[0][i] = key0 + result_row(i, half) < see.hi ? s[0][i] : -INFINITY;
+        soften(run, s, acc, p.scale2);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const Frag<T> w = result_frag<T>(s[0], k);
+#pragma unroll
+            for (int db = 0; db < DB; ++db) acc[db] = mma(column_frag(v_tile, LD, k, db, lane), w, acc[db]);
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+    // join the waves: statistics through LDS, then the products, 32 channels at a time, in the tiles' place
+    const float2 two = both_halves(run.sum);
+    if (half == 0) {
+        tops[wave][col] = run.top;
+        sums[wave][col] = two.x + two.y;
+    }
+    __syncthreads();
+    float top = -INFINITY;
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, tops[w][col]);
+    float sum = 0.0f;
+    // a wave without a maximum has seen nothing, or NaN alone
+    const auto weight = [&](float t) { return t == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(t - top); };
+    for (int w = 0; w < kWaves; ++w) sum += sums[w][col] * weight(tops[w][col]);
+    const float share = sum == 0.0f ? 0.0f : weight(run.top) / sum;
+    const float lse2 = sum == 0.0f ? -INFINITY : top + __builtin_amdgcn_logf(sum);
+    float *join = (float *)&tiles[0][0][0];                        // [wave][32 heads][36]
+    static_assert(sizeof(tiles) >= sizeof(float) * kWaves * 32 * 36, "room for the join");
+    const int64_t n = p.rows * p.heads_q, out_row = row * p.heads_q + head0;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) {
+        __syncthreads();
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            Vec<float, 4> v;
+#pragma unroll
+            for (int t = 0; t < 4; ++t) v[t] = acc[db][4 * b + t] * share;
+            *(Vec<float, 4> *)(join + (wave * 32 + col) * 36 + 8 * b + 4 * half) = v;
+        }
+        __syncthreads();
+        const int d0 = (tid % 8) * 4, d = 32 * db + d0;
+        for (int m = tid / 8; m < heads; m += kWaves * kWave / 8) {
+            Vec<float, 4> v = {};
+            for (int w = 0; w < kWaves; ++w) v += *(const Vec<float, 4> *)(join + (w * 32 + m) * 36 + d0);
+            if (p.splits > 1) {
+                store<4>(p.part + (split * n + out_row + m) * p.dim + d, v, p.dim - d);
+            } else {
+                Vec<T, 4> o;
+#pragma unroll
+                for (int t = 0; t < 4; ++t) o[t] = (T)v[t];
+                store<4>(address<T>(p.out, row, head0 + m) + d, o, p.dim - d);
+            }
+        }
+    }
+    if (wave == 0 && half == 0 && col < heads) {
+        if (p.splits > 1) p.part_lse[split * n + out_row + col] = lse2;
+        else if (p.lse) p.lse[out_row + col] = lse2 * kLn2;
+    }
+}
+
+// Joins the parts of each row and head: a wave each.
+template <class T> __global__ __launch_bounds__(kBlock) void attend_join_kernel(Attend p) {
+    const int64_t n = p.rows * p.heads_q, at = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave;
+    const int lane = (int)threadIdx.x % kWave;
+    if (at >= n) return;
+    const int64_t row = at / p.heads_q;
+    const int head = (int)(at - row * p.heads_q);
+    float top = -INFINITY, sum = 0.0f;
+    for (int s = 0; s < p.splits; ++s) top = fmaxf(top, p.part_lse[s * n + at]);
+    Vec<float, 4> acc = {};
+    const int d = 4 * lane;
+    for (int s = 0; s < p.splits; ++s) {
+        const float lse2 = p.part_lse[s * n + at];
+        if (lse2 == -INFINITY) continue;                            // nothing seen in this part (a NaN is not skipped)
+        const float w = __builtin_amdgcn_exp2f(lse2 - top);
+        sum += w;
+        acc += w * load<4>(p.part + (s * n + at) * p.dim + d, p.dim - d);
+    }
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    Vec<T, 4> o;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) o[t] = (T)(acc[t] * inv);
+    store<4>(address<T>(p.out, row, head) + d, o, p.dim - d);
+    if (p.lse && lane == 0) p.lse[at] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+}
+
+// Whether a lane keeps its own rows' operands in registers, or takes them from memory (the L2 cache) for every tile:
+// 16 KiB of two operands a wave are what the accumulators leave room for.
+template <class T, int DP> constexpr bool kHoldQuery = DP * sizeof(T) <= 512;
+template <class T, int DP> constexpr bool kHoldState = DP * sizeof(T) <= 256;
+
+// dq of 128 rows M over a part of what they see; delta and the rows' bounds for the other kernel on the way.
+template <class T, int DP> __global__ __launch_bounds__(kBlock) void attend_dq_kernel(Attend p) {
+    constexpr int NK = kTileKeys<T>, NB = NK / 32, DB = DP / 32, DS = DP / 16, LD = kLd<T, DP>;
+    constexpr bool kHold = kHoldQuery<T, DP>;
+    __shared__ __attribute__((aligned(16))) T k_tile[NK * LD], v_tile[NK * LD];
+    __shared__ Bounds slots[kWaves];
+    __shared__ int bad[2];                           // by turns: the one of the next tile is cleared where all are done with the last
+    const int tid = (int)threadIdx.x, lane = tid % kWave, wave = tid / kWave, half = lane / 32, col = lane % 32;
+    const int state_head = (int)blockIdx.y, split = (int)blockIdx.z;
+    const int tile_m = (int)gridDim.x - 1 - (int)blockIdx.x;
+    const Place at = place_of(p, tile_m * kTileM + 32 * wave + col, state_head);
+    const Range see = range_of(p, at.row);
+    const Bounds own = over_columns(bounds_of(see, at.valid));
+    if (tid < 2) bad[tid] = 0;
+    const Bounds any = over_waves(own, slots, wave, lane);
+    const T *q_at = address<const T>(p.q, at.row, at.head), *do_at = address<const T>(p.dout, at.row, at.head);
+    auto frag = [&](const T *from, int s) {
+        const int d = 16 * s + 8 * half;
+        return load<8>(from + d, p.dim - d);
+    };
+    Frag<T> q[kHold ? DS : 1], dout[kHold ? DS : 1];
+    float delta = 0.0f;
+#pragma unroll
+    for (int s = 0; s < DS; ++s) {
+        const Frag<T> g = frag(do_at, s), o = frag(address<const T>(p.out, at.row, at.head), s);
+        if constexpr (kHold) {
+            q[s] = frag(q_at, s);
+            dout[s] = g;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) delta += (float)g[j] * (float)o[j];
+    }
+    const float2 two = both_halves(delta);
+    delta = two.x + two.y;
+    const int64_t out_row = (int64_t)at.row * p.heads_q + at.head;
+    if (split == 0) {
+        if (at.valid && half == 0) p.delta[out_row] = delta;
+        // rows that see nothing, or are not there, keep the states' kernel from taking 32 rows for unmasked
+        const bool all = __all(at.valid && !see.empty());
+        if (state_head == 0 && lane == 0)
+            p.bounds[tile_m * kWaves + wave] = make_int4(own.first, own.end, all ? own.all : INT_MAX, all ? own.all_end : INT_MIN);
+    }
+    const float lse2 = p.lse[out_row] * kLog2e;
+    Acc acc[DB] = {};
+    const int tiles = any.end > any.first ? (any.end - any.first + NK - 1) / NK : 0;
+    const int begin = (int)((int64_t)tiles * split / p.splits), end = (int)((int64_t)tiles * (split + 1) / p.splits);
+    Stage<T, DP, NK, kBlock> ks, vs;
+    auto fetch_k = [&](int tile) {
+        const int key0 = any.first + tile * NK;
+        ks.fetch(tid, p.dim, [&](int r) { return key0 + r < any.end ? address<const T>(p.k, key0 + r, state_head) : nullptr; });
+    };
+    auto fetch_v = [&](int tile) {
+        const int key0 = any.first + tile * NK;
+        vs.fetch(tid, p.dim, [&](int r) { return key0 + r < any.end ? address<const T>(p.v, key0 + r, state_head) : nullptr; });
+    };
+    if (kAhead<T, DP> && begin < end) fetch_k(begin), fetch_v(begin);
+    for (int tile = begin; tile < end; ++tile) {
+        const int key0 = any.first + tile * NK;
+        const bool look = !any.covers(key0, key0 + NK);
+        const int turn = (tile - begin) % 2;
+        __syncthreads();
+        if (tid == 0) bad[turn ^ 1] = 0;
+        if constexpr (!kAhead<T, DP>) fetch_k(tile);
+        if (ks.commit(k_tile, tid, look)) bad[turn] = 1;
+        if constexpr (!kAhead<T, DP>) fetch_v(tile);
+        vs.commit(v_tile, tid, false);
+        __syncthreads();
+        if (kAhead<T, DP> && tile + 1 < end) fetch_k(tile + 1), fetch_v(tile + 1);
+        if (!own.meets(key0, key0 + NK)) continue;
+        const bool whole = own.covers(key0, key0 + NK);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            Acc s = {}, dp = {};
+#pragma unroll
+            for (int d = 0; d < DS; ++d) {
+                s = mma(row_frag(k_tile, LD, 32 * b + col, d, half), kHold ? q[kHold ? d : 0] : frag(q_at, d), s);
+                dp = mma(row_frag(v_tile, LD, 32 * b + col, d, half), kHold ? dout[kHold ? d : 0] : frag(do_at, d), dp);
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float w = __builtin_amdgcn_exp2f(s[i] * p.scale2 - lse2) * (dp[i] - delta);
+                s[i] = whole || see.has(key0 + 32 * b + result_row(i, half)) ? w : 0.0f;
+            }
+            if (!whole && bad[turn]) {
+                careful_product<T, DB>(acc, s, k_tile + 32 * b * LD, LD, half, [&](int j) { return see.has(key0 + 32 * b + j); });
+                continue;
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const Frag<T> w = result_frag<T>(s, k);
+#pragma unroll
+                for (int db = 0; db < DB; ++db) acc[db] = mma(column_frag(k_tile, LD, 2 * b + k, db, lane), w, acc[db]);
+            }
+        }
+    }
+    if (!at.valid) return;
+    if (see.empty())
+#pragma unroll
+        for (int db = 0; db < DB; ++db) acc[db] = Acc{};
+    if (p.splits > 1) store_result(p.part + (split * p.rows * p.heads_q + out_row) * p.dim, acc, p.scale, p.dim, half);
+    else store_result(address<T>(p.dq, at.row, at.head), acc, p.scale, p.dim, half);
+}
+
+// dk and dv of 128 states over a part of the rows that see them: the same products with the roles exchanged, 32 rows M
+// in LDS at a time, lanes that hold the states.
+template <class T, int DP> __global__ __launch_bounds__(kBlock) void attend_dkv_kernel(Attend p) {
+    constexpr int DB = DP / 32, DS = DP / 16, LD = kLd<T, DP>, NM = 32;
+    constexpr bool kHold = kHoldState<T, DP>;
+    __shared__ __attribute__((aligned(16))) T q_tile[NM * LD], do_tile[NM * LD];
+    __shared__ __attribute__((aligned(16))) float lse_of[NM], delta_of[NM];
+    __shared__ Range range_at[NM];
+    __shared__ int bad[2], first_tile, last_tile;
+    const int tid = (int)threadIdx.x, lane = tid % kWave, wave = tid / kWave, half = lane / 32, col = lane % 32;
+    const int state_head = (int)blockIdx.y, split = (int)blockIdx.z;
+    const int block0 = (int)blockIdx.x * 32 * kWaves, block_end = min(block0 + 32 * kWaves, (int)p.keys);
+    const int key0 = block0 + 32 * wave, key = key0 + col;
+    const bool valid = key < p.keys;
+    const T *k_at = address<const T>(p.k, valid ? key : p.keys - 1, state_head), *v_at = address<const T>(p.v, valid ? key : p.keys - 1, state_head);
+    auto frag = [&](const T *from, int s) {
+        const int d = 16 * s + 8 * half;
+        return load<8>(from + d, valid ? p.dim - d : 0);
+    };
+    Frag<T> k[kHold ? DS : 1], v[kHold ? DS : 1];
+    if constexpr (kHold)
+#pragma unroll
+        for (int s = 0; s < DS; ++s) {
+            k[s] = frag(k_at, s);
+            v[s] = frag(v_at, s);
+        }
+    Acc dk[DB] = {}, dv[DB] = {};
+    // the first and last 32 rows that see any of the block's states
+    const int m_tiles = (p.m_total + NM - 1) / NM;
+    if (tid == 0) {
+        first_tile = INT_MAX;
+        last_tile = -1;
+        bad[0] = bad[1] = 0;
+    }
+    __syncthreads();
+    int first = INT_MAX, last = -1;
+    for (int t = tid; t < m_tiles; t += kBlock) {
+        const int4 b = p.bounds[t];
+        if (block0 < b.y && block_end > b.x) {
+            first = min(first, t);
+            last = max(last, t);
+        }
+    }
+    if (last >= 0) {
+        atomicMin(&first_tile, first);
+        atomicMax(&last_tile, last);
+    }
+    __syncthreads();
+    first = first_tile;
+    const int count = last_tile >= 0 ? last_tile + 1 - first : 0;
+    const int begin = first + (int)((int64_t)count * split / p.splits), end = first + (int)((int64_t)count * (split + 1) / p.splits);
+    Stage<T, DP, NM, kBlock> qs, dos;
+    float next_lse = 0.0f, next_delta = 0.0f;
+    Range next_range{0, 0};
+    auto next_of = [&](int t) {                          // the next 32 rows with something to add
+        for (; t < end; ++t) {
+            const int4 b = p.bounds[t];
+            if (block0 < b.y && block_end > b.x) break;
+        }
+        return t;
+    };
+    auto fetch = [&](int t) {
+        const auto row_at = [&](const hp_heads_t &x, int r) {
+            const Place at = place_of(p, t * NM + r, state_head);
+            return at.valid ? address<const T>(x, at.row, at.head) : nullptr;
+        };
+        qs.fetch(tid, p.dim, [&](int r) { return row_at(p.q, r); });
+        dos.fetch(tid, p.dim, [&](int r) { return row_at(p.dout, r); });
+        if (tid < NM) {
+            const Place at = place_of(p, t * NM + tid, state_head);
+            const int64_t out_row = (int64_t)at.row * p.heads_q + at.head;
+            next_lse = p.lse[out_row] * kLog2e;
+            next_delta = p.delta[out_row];
+            next_range = at.valid ? range_of(p, at.row) : Range{0, 0};
+        }
+    };
+    int tile = count ? next_of(begin) : end, turn = 0;
+    if (kAhead<T, DP> && count && tile < end) fetch(tile);
+    while (count && tile < end) {
+        const int4 b = p.bounds[tile];
+        const bool whole = key0 >= b.z && key0 + 32 <= b.w, meets = key0 < b.y && key0 + 32 > b.x;
+        const bool look = !(block0 >= b.z && block0 + 32 * kWaves <= b.w);
+        __syncthreads();
+        if (tid == 0) bad[turn ^ 1] = 0;
+        if constexpr (!kAhead<T, DP>) fetch(tile);
+        const bool one = qs.commit(q_tile, tid, look), other = dos.commit(do_tile, tid, look);
+        if (one || other) bad[turn] = 1;
+        if (tid < NM) {
+            lse_of[tid] = next_lse;
+            delta_of[tid] = next_delta;
+            range_at[tid] = next_range;
+        }
+        __syncthreads();
+        const int next = next_of(tile + 1);
+        if (kAhead<T, DP> && next < end) fetch(next);
+        tile = next;
+        const int now = turn;
+        turn ^= 1;
+        if (!meets) continue;
+        Acc s = {}, dp = {};
+#pragma unroll
+        for (int d = 0; d < DS; ++d) {
+            s = mma(row_frag(q_tile, LD, col, d, half), kHold ? k[kHold ? d : 0] : frag(k_at, d), s);
+            dp = mma(row_frag(do_tile, LD, col, d, half), kHold ? v[kHold ? d : 0] : frag(v_at, d), dp);
+        }
+#pragma unroll
+        for (int b4 = 0; b4 < 4; ++b4) {
+            const Vec<float, 4> lse2 = *(const Vec<float, 4> *)&lse_of[8 * b4 + 4 * half], delta = *(const Vec<float, 4> *)&delta_of[8 * b4 + 4 * half];
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const int i = 4 * b4 + t;
+                const bool sees = whole || range_at[result_row(i, half)].has(key);
+                const float w = __builtin_amdgcn_exp2f(s[i] * p.scale2 - lse2[t]);
+                s[i] = sees ? w : 0.0f;
+                dp[i] = sees ? w * (dp[i] - delta[t]) : 0.0f;
+            }
+        }
+        if (!whole && bad[now]) {
+            const auto seen = [&](int j) { return range_at[j].has(key); };
+            careful_product<T, DB>(dv, s, do_tile, LD, half, seen);
+            careful_product<T, DB>(dk, dp, q_tile, LD, half, seen);
+            continue;
+        }
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            const Frag<T> w = result_frag<T>(s, m), g = result_frag<T>(dp, m);
+#pragma unroll
+            for (int db = 0; db < DB; ++db) {
+                dv[db] = mma(column_frag(do_tile, LD, m, db, lane), w, dv[db]);
+                dk[db] = mma(column_frag(q_tile, LD, m, db, lane), g, dk[db]);
+            }
+        }
+    }
+    if (!valid) return;
+    if (p.splits > 1) {
+        const int64_t at = ((split * p.keys + key) * p.heads_k + state_head) * p.dim;
+        store_result(p.part_k + at, dk, p.scale, p.dim, half);
+        store_result(p.part_v + at, dv, 1.0f, p.dim, half);
+    } else {
+        store_result(address<T>(p.dk, key, state_head), dk, p.scale, p.dim, half);
+        store_result(address<T>(p.dv, key, state_head), dv, 1.0f, p.dim, half);
+    }
+}
+
+// Adds parts [splits][rows * heads][dim] up, in order: a wave a row and head.
+template <class T> __global__ __launch_bounds__(kBlock) void attend_sum_kernel(const float *part, int splits, int64_t rows, int heads, int dim, hp_heads_t out) {
+    const int64_t n = rows * heads, at = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave;
+    const int d = 4 * ((int)threadIdx.x % kWave);
+    if (at >= n || d >= dim) return;
+    const int64_t row = at / heads;
+    Vec<float, 4> acc = {};
+    for (int s = 0; s < splits; ++s) acc += load<4>(part + (s * n + at) * dim + d, dim - d);
+    Vec<T, 4> o;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) o[t] = (T)acc[t];
+    store<4>(address<T>(out, row, (int)(at - row * heads)) + d, o, dim - d);
+}
+
+// ---- host ------------------------------------------------------------------------------------------------------
+
+// Parts of the long axis: until the launch has about `want` workgroups, none with less than `least` of `length`.
+int32_t parts_of(int64_t blocks, int64_t want, int64_t length, int64_t least, int64_t most) {
+    int64_t n = (want + blocks - 1) / blocks;
+    const int64_t by_length = length / least;
+    n = n < by_length ? n : by_length;
+    n = n < most ? n : most;
+    return (int32_t)(n < 1 ? 1 : n);
+}
+
+struct Plan {
+    int64_t blocks_m, blocks_k;                     // of 128 rows M, of 128 states
+    int32_t splits, splits_dq, splits_dkv, splits_step;
+};
+
+Plan plan_of(const hp_attend_args_t &a) {
+    Plan n;
+    const int64_t group = a.heads_q / a.heads_k, m = a.rows * group;
+    n.blocks_m = (m + kTileM - 1) / kTileM;
+    n.blocks_k = (a.keys + 32 * kWaves - 1) / (32 * kWaves);
+    const int64_t one = n.blocks_m * a.heads_k > 0 ? n.blocks_m * a.heads_k : 1, two = n.blocks_k * a.heads_k > 0 ? n.blocks_k * a.heads_k : 1;
+    n.splits = parts_of(one, 2 * kComputeUnits, a.keys, 256, 32);
+    n.splits_dq = parts_of(one, kComputeUnits, a.keys, 256, 32);
+    n.splits_dkv = parts_of(two, 2 * kComputeUnits, m, 256, 32);
+    const int64_t each = a.rows * a.heads_k * ((group + 31) / 32);
+    n.splits_step = parts_of(each > 0 ? each : 1, 8 * kComputeUnits, a.keys, kStepKeys, 64);
+    return n;
+}
+
+int64_t align16(int64_t n) { return (n + 15) / 16 * 16; }
+
+int64_t workspace_of(const hp_attend_args_t &a, int call) {
+    const Plan n = plan_of(a);
+    const int64_t outs = a.rows * a.heads_q, states = a.keys * a.heads_k;
+    if (call == HP_ATTEND_BACKWARD) {
+        const int64_t parts = 4 * a.dim * (n.splits_dq > 1 ? n.splits_dq * outs : 0), parts_kv = 4 * a.dim * (n.splits_dkv > 1 ? 2 * n.splits_dkv * states : 0);
+        return align16(4 * outs) + align16(16 * n.blocks_m * kWaves) + (parts > parts_kv ? parts : parts_kv);
+    }
+    const int32_t splits = call == HP_ATTEND_STEP ? n.splits_step : n.splits;
+    return splits > 1 ? align16(4 * splits * outs) + 4 * splits * outs * a.dim : 0;
+}
+
+bool misaligned(const void *p, int to) { return (uintptr_t)p % to != 0; }
+
+int check_sizes(const hp_attend_args_t *a) {
+    if (!a) return HP_EINVAL;
+    if (a->dtype != HP_BF16 && a->dtype != HP_F32) return HP_EINVAL;
+    if (a->dim < 1 || a->dim > HP_ATTEND_MAX_DIM || a->heads_k < 1 || a->heads_q < 1) return HP_EINVAL;
+    if (a->heads_q % a->heads_k || a->heads_q > 16384) return HP_ELAYOUT;
+    if (a->rows < 0 || a->keys < 0) return HP_EINVAL;
+    // rows M, states and lanes of a launch are counted in 32 bits, with tiles to spare
+    if (a->rows > (1 << 30) / (a->heads_q / a->heads_k) || a->keys > INT_MAX - 1024) return HP_ELAYOUT;
+    return HP_OK;
+}
+
+int check(const hp_attend_args_t *a, int call) {
+    if (const int rc = check_sizes(a)) return rc;
+    if (!(a->scale > 0) || !std::isfinite(a->scale) || !std::isfinite(a->scale * kLog2e)) return HP_EINVAL;
+    const int size = a->dtype == HP_BF16 ? 2 : 4;
+    const bool back = call == HP_ATTEND_BACKWARD;
+    for (const hp_heads_t *t : {&a->q, &a->out, &a->dout, &a->dq}) {
+        if (!back && (t == &a->dout || t == &a->dq)) continue;
+        if (a->rows > 0 && !t->data) return HP_EINVAL;
+        if (misaligned(t->data, size)) return HP_EALIGN;
+    }
+    for (const hp_heads_t *t : {&a->k, &a->v, &a->dk, &a->dv}) {
+        if (!back && (t == &a->dk || t == &a->dv)) continue;
+        if (a->keys > 0 && !t->data) return HP_EINVAL;
+        if (misaligned(t->data, size)) return HP_EALIGN;
+    }
+    if (back && a->rows > 0 && !a->lse) return HP_EINVAL;
+    if (misaligned(a->ranges, 4) || misaligned(a->lse, 4) || misaligned(a->workspace, 16)) return HP_EALIGN;
+    const int64_t need = a->rows > 0 || back ? workspace_of(*a, call) : 0;
+    if (need > 0 && (!a->workspace || a->workspace_bytes < need)) return HP_EINVAL;
+    return HP_OK;
+}
+
+Attend params_of(const hp_attend_args_t &a) {
+    Attend p{};
+    p.rows = a.rows, p.keys = a.keys;
+    p.heads_q = a.heads_q, p.heads_k = a.heads_k, p.group = a.heads_q / a.heads_k, p.dim = a.dim;
+    p.splits = 1, p.m_total = (int32_t)(a.rows * p.group);
+    p.scale = a.scale, p.scale2 = a.scale * kLog2e;
+    p.q = a.q, p.k = a.k, p.v = a.v, p.out = a.out, p.dout = a.dout, p.dq = a.dq, p.dk = a.dk, p.dv = a.dv;
+    p.ranges = a.ranges, p.lse = a.lse;
+    return p;
+}
+
+bool failed() { return hip_failed(hipGetLastError()); }
+
+enum Kernel { kForward, kStep, kDq, kDkv };
+
+template <class T, int DP> void launch(Kernel what, const Attend &p, const dim3 &grid, hipStream_t s) {
+    if (what == kForward) attend_forward_kernel<T, DP><<<grid, kBlock, 0, s>>>(p);
+    else if (what == kStep) attend_step_kernel<T, DP><<<grid, kStepWaves<T, DP> * kWave, 0, s>>>(p);
+    else if (what == kDq) attend_dq_kernel<T, DP><<<grid, kBlock, 0, s>>>(p);
+    else attend_dkv_kernel<T, DP><<<grid, kBlock, 0, s>>>(p);
+}
+
+template <class T> void launch(Kernel what, const Attend &p, const dim3 &grid, hipStream_t s) {
+    if (p.dim <= 64) launch<T, 64>(what, p, grid, s);
+    else if (p.dim <= 96) launch<T, 96>(what, p, grid, s);
+    else if (p.dim <= 128) launch<T, 128>(what, p, grid, s);
+    else launch<T, 256>(what, p, grid, s);
+}
+
+void launch(Kernel what, int dtype, const Attend &p, const dim3 &grid, hipStream_t s) {
+    if (dtype == HP_BF16) launch<__bf16>(what, p, grid, s);
+    else launch<float>(what, p, grid, s);
+}
+
+// Forward in either shape: the launch, and the join of the parts.
+int forward(const hp_attend_args_t &a, Kernel what, const dim3 &grid, hipStream_t s) {
+    Attend p = params_of(a);
+    p.splits = (int32_t)grid.z;
+    if (p.splits > 1) {
+        p.part_lse = (float *)a.workspace;
+        p.part = (float *)((char *)a.workspace + align16(4 * p.splits * p.rows * p.heads_q));
+    }
+    launch(what, a.dtype, p, grid, s);
+    if (failed()) return HP_EHIP;
+    if (p.splits > 1) {
+        const uint32_t blocks = (uint32_t)((p.rows * p.heads_q + kWaves - 1) / kWaves);
+        if (a.dtype == HP_BF16) attend_join_kernel<__bf16><<<blocks, kBlock, 0, s>>>(p);
+        else attend_join_kernel<float><<<blocks, kBlock, 0, s>>>(p);
+        if (failed()) return HP_EHIP;
+    }
+    return HP_OK;
+}
+
+int add_up(const float *part, int splits, int dtype, int64_t rows, int heads, int dim, const hp_heads_t &out, hipStream_t s) {
+    const uint32_t blocks = (uint32_t)((rows * heads + kWaves - 1) / kWaves);
+    if (dtype == HP_BF16) attend_sum_kernel<__bf16><<<blocks, kBlock, 0, s>>>(part, splits, rows, heads, dim, out);
+    else attend_sum_kernel<float><<<blocks, kBlock, 0, s>>>(part, splits, rows, heads, dim, out);
+    return failed() ? HP_EHIP : HP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t hp_cross_attend_workspace(const hp_attend_args_t *a, int32_t call) {
+    if (const int rc = check_sizes(a)) return rc;
+    if (call < HP_ATTEND_FORWARD || call > HP_ATTEND_BACKWARD) return HP_EINVAL;
+    return workspace_of(*a, call);
+}
+
+int hp_cross_attend(const hp_attend_args_t *a, void *stream) {
+    if (const int rc = check(a, HP_ATTEND_FORWARD)) return rc;
+    if (a->rows == 0) return HP_OK;
+    const Plan n = plan_of(*a);
+    return forward(*a, kForward, dim3((uint32_t)n.blocks_m, (uint32_t)a->heads_k, (uint32_t)n.splits), (hipStream_t)stream);
+}
+
+int hp_cross_attend_step(const hp_attend_args_t *a, void *stream) {
+    if (const int rc = check(a, HP_ATTEND_STEP)) return rc;
+    if (a->rows > 1 << 23) return HP_ELAYOUT;
+    if (a->rows == 0) return HP_OK;
+    const Plan n = plan_of(*a);
+    const int32_t parts = (a->heads_q / a->heads_k + 31) / 32;
+    return forward(*a, kStep, dim3((uint32_t)a->rows, (uint32_t)(a->heads_k * parts), (uint32_t)n.splits_step), (hipStream_t)stream);
+}
+
+int hp_cross_attend_backward(const hp_attend_args_t *a, void *stream) {
+    if (const int rc = check(a, HP_ATTEND_BACKWARD)) return rc;
+    const Plan n = plan_of(*a);
+    const hipStream_t s = (hipStream_t)stream;
+    Attend p = params_of(*a);
+    char *ws = (char *)a->workspace;
+    p.delta = (float *)ws;
+    p.bounds = (int4 *)(ws + align16(4 * a->rows * a->heads_q));
+    float *parts = (float *)(ws + align16(4 * a->rows * a->heads_q) + align16(16 * n.blocks_m * kWaves));
+    if (a->rows > 0) {
+        p.splits = n.splits_dq;
+        p.part = parts;
+        launch(kDq, a->dtype, p, dim3((uint32_t)n.blocks_m, (uint32_t)a->heads_k, (uint32_t)p.splits), s);
+        if (failed()) return HP_EHIP;
+        if (p.splits > 1)
+            if (const int rc = add_up(parts, p.splits, a->dtype, a->rows, a->heads_q, a->dim, a->dq, s)) return rc;
+    }
+    if (a->keys > 0) {
+        p.splits = n.splits_dkv;
+        p.part_k = parts;                            // what dq's parts were is read by now: the stream is in order
+        p.part_v = parts + (int64_t)p.splits * a->keys * a->heads_k * a->dim;
+        launch(kDkv, a->dtype, p, dim3((uint32_t)n.blocks_k, (uint32_t)a->heads_k, (uint32_t)p.splits), s);
+        if (failed()) return HP_EHIP;
+        if (p.splits > 1) {
+            if (const int rc = add_up(p.part_k, p.splits, a->dtype, a->keys, a->heads_k, a->dim, a->dk, s)) return rc;
+            if (const int rc = add_up(p.part_v, p.splits, a->dtype, a->keys, a->heads_k, a->dim, a->dv, s)) return rc;
+        }
+    }
+    return HP_OK;
+}
+
+}  // extern "C"

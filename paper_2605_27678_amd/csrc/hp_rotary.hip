@@ -1,0 +1,261 @@
+// Rotary positions.  A pair (a, b) of a head's channels is turned by the angle
+// that belongs to its row's position:
+//     out_a = x_a c - x_b s,   out_b = x_b c + x_a s,
+// with (c, s) from a table of binary32 pairs.  The gradient is the same turn
+// with -s.  Bound by memory: every value is read and written once, 3 operations
+// each; the table's row (8 bytes a pair) is read once a lane and used for
+// several heads.
+#include <cmath>
+
+#include "hp_device.hpp"
+#include "hp_operators.h"
+
+#pragma clang fp contract(fast)
+
+namespace {
+
+using namespace hp;
+
+constexpr int kThreads = 256;
+
+// Heads that a lane turns with the pairs that it has read from the table.
+constexpr int kHeads = 4;
+
+struct RotaryParams {
+    int64_t rows, table_rows, axis_stride;
+    const float *table;
+    const int32_t *positions;
+    int32_t n_tensors, n_heads;               // of all tensors together
+    int32_t dim, half, n_axes, inverse;
+    int32_t units, copies, per_row, rows_per_block;   // lanes: pairs / VEC, channels behind them / VEC, of a row, and rows of a block
+    int32_t axis_end[HP_ROTARY_MAX_AXES];
+    int32_t heads[HP_ROTARY_MAX_TENSORS];
+    hp_heads_t x[HP_ROTARY_MAX_TENSORS], out[HP_ROTARY_MAX_TENSORS];
+};
+
+// One lane: VEC pairs of one row, in kHeads heads (or VEC copied channels there).
+// Consecutive lanes take consecutive pairs, then the next heads: a wave reads
+// runs of half a head.
+template <class T, int VEC, bool INTERLEAVED> __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryParams p) {
+    const int item = (int)blockIdx.y * kThreads + (int)threadIdx.x;
+    const int in_block = p.rows_per_block > 1 ? item / p.per_row : 0;
+    const int at_row = item - in_block * p.per_row;
+    if (in_block >= p.rows_per_block || at_row >= p.per_row) return;
+    const int group = at_row / p.units, u = at_row - group * p.units;
+    const int turned = p.units - p.copies;
+    for (int64_t block = blockIdx.x; block * p.rows_per_block < p.rows; block += gridDim.x) {
+        const int64_t row = block * p.rows_per_block + in_block;
+        if (row >= p.rows) break;
+        float c[VEC], s[VEC];
+        if (u < turned) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) c[j] = s[j] = __builtin_nanf("");
+            if (p.n_axes == 1) {
+                const int64_t pos = p.positions[row];
+                if (pos >= 0 && pos < p.table_rows) {
+                    const Vec<float, 2 * VEC> t = load<2 * VEC>(p.table + (pos * p.half + u * VEC) * 2, 2 * VEC);
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) c[j] = t[2 * j], s[j] = t[2 * j + 1];
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    const int i = u * VEC + j;
+                    int axis = 0;
+                    while (axis < p.n_axes - 1 && i >= p.axis_end[axis]) ++axis;
+                    const int64_t pos = p.positions[axis * p.axis_stride + row];
+                    if (pos >= 0 && pos < p.table_rows) {
+                        const Vec<float, 2> t = load<2>(p.table + (pos * p.half + i) * 2, 2);
+                        c[j] = t[0], s[j] = t[1];
+                    }
+                }
+            }
+            if (p.inverse)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) s[j] = -s[j];
+        }
+        Vec<T, VEC> a[kHeads], b[kHeads];
+        T *to[kHeads];
+#pragma unroll
+        for (int k = 0; k < kHeads; ++k) {
+            int h = group * kHeads + k;
+            to[k] = nullptr;
+            if (h >= p.n_heads) continue;
+            int t = 0;
+            while (t < p.n_tensors - 1 && h >= p.heads[t]) h -= p.heads[t++];
+            const T *from = (const T *)p.x[t].data + row * p.x[t].row_stride + h * p.x[t].head_stride;
+            to[k] = (T *)p.out[t].data + row * p.out[t].row_stride + h * p.out[t].head_stride;
+            if (u >= turned) {
+                a[k] = load<VEC>(from + 2 * p.half + (u - turned) * VEC, VEC);
+            } else if constexpr (INTERLEAVED) {
+                a[k] = load<VEC>(from + 2 * u * VEC, VEC);
+                b[k] = load<VEC>(from + 2 * u * VEC + VEC, VEC);
+            } else {
+                a[k] = load<VEC>(from + u * VEC, VEC);
+                b[k] = load<VEC>(from + p.half + u * VEC, VEC);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kHeads; ++k) {
+            if (!to[k]) continue;
+            if (u >= turned) {
+                store<VEC>(to[k] + 2 * p.half + (u - turned) * VEC, a[k], VEC);
+                continue;
+            }
+            Vec<T, VEC> ra, rb;
+            if constexpr (INTERLEAVED) {           // 2 * VEC channels in a row: pair j is channels 2j, 2j + 1 of them
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    const int e = 2 * j, o = e + 1;
+                    const float xa = e < VEC ? at<VEC, T>(a[k], e) : at<VEC, T>(b[k], e - VEC);
+                    const float xb = o < VEC ? at<VEC, T>(a[k], o) : at<VEC, T>(b[k], o - VEC);
+                    const float ya = xa * c[j] - xb * s[j], yb = xb * c[j] + xa * s[j];
+                    if (e < VEC) put<VEC, T>(ra, e, ya); else put<VEC, T>(rb, e - VEC, ya);
+                    if (o < VEC) put<VEC, T>(ra, o, yb); else put<VEC, T>(rb, o - VEC, yb);
+                }
+                store<VEC>(to[k] + 2 * u * VEC, ra, VEC);
+                store<VEC>(to[k] + 2 * u * VEC + VEC, rb, VEC);
+            } else {
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    const float xa = at<VEC, T>(a[k], j), xb = at<VEC, T>(b[k], j);
+                    put<VEC, T>(ra, j, xa * c[j] - xb * s[j]);
+                    put<VEC, T>(rb, j, xb * c[j] + xa * s[j]);
+                }
+                store<VEC>(to[k] + u * VEC, ra, VEC);
+                store<VEC>(to[k] + p.half + u * VEC, rb, VEC);
+            }
+        }
+    }
+}
+
+template <class T, int VEC> void launch(RotaryParams &p, bool interleaved, bool copies, hipStream_t stream) {
+    p.copies = copies ? (p.dim - 2 * p.half) / VEC : 0;
+    p.units = p.half / VEC + p.copies;
+    p.per_row = p.units * ((p.n_heads + kHeads - 1) / kHeads);
+    p.rows_per_block = p.per_row >= kThreads ? 1 : kThreads / p.per_row;
+    const int64_t blocks = (p.rows + p.rows_per_block - 1) / p.rows_per_block;
+    const dim3 grid((uint32_t)(blocks < (1 << 22) ? blocks : (1 << 22)), p.per_row > kThreads ? (p.per_row + kThreads - 1) / kThreads : 1);
+    if (interleaved) rotary_kernel<T, VEC, true><<<grid, kThreads, 0, stream>>>(p);
+    else rotary_kernel<T, VEC, false><<<grid, kThreads, 0, stream>>>(p);
+}
+
+struct TableParams {
+    float *table;
+    int64_t n, first;
+    int32_t half, kind;
+    double log_base, factor, original, low, high, amplitude;
+};
+
+__global__ __launch_bounds__(kThreads) void table_kernel(TableParams t) {
+    const int64_t total = t.n * t.half;
+    for (int64_t e = (int64_t)blockIdx.x * kThreads + threadIdx.x; e < total; e += (int64_t)gridDim.x * kThreads) {
+        const int64_t p = e / t.half;
+        const int i = (int)(e - p * t.half);
+        double f = exp(-t.log_base * i / t.half);
+        if (t.kind == HP_ROTARY_LINEAR) {
+            f /= t.factor;
+        } else if (t.kind == HP_ROTARY_BY_TURNS) {
+            const double turns = t.original * f / 6.283185307179586476925;
+            double keep = (turns - t.low) / (t.high - t.low);
+            keep = keep < 0 ? 0 : keep > 1 ? 1 : keep;
+            f = f * keep + f / t.factor * (1 - keep);
+        }
+        double s, c;
+        sincos((double)(t.first + p) * f, &s, &c);
+        t.table[2 * e] = (float)(t.amplitude * c);
+        t.table[2 * e + 1] = (float)(t.amplitude * s);
+    }
+}
+
+bool misaligned(const void *p, int to) { return (uintptr_t)p % to != 0; }
+
+}  // namespace
+
+extern "C" {
+
+int hp_rotary_table(float *table, int64_t n, int64_t first, int32_t rot, const hp_rotary_scaling_t *scaling,
+                    void *stream) {
+    if (!scaling || n < 0 || first < 0 || rot < 2 || rot % 2 || (n > 0 && !table)) return HP_EINVAL;
+    if (n > ((int64_t)1 << 40) / rot || first > ((int64_t)1 << 40)) return HP_EINVAL;
+    const hp_rotary_scaling_t &s = *scaling;
+    if (s.kind < HP_ROTARY_PLAIN || s.kind > HP_ROTARY_BY_TURNS) return HP_EINVAL;
+    if (!(s.base > 0) || !std::isfinite(s.base) || !std::isfinite(s.amplitude)) return HP_EINVAL;
+    if (s.kind != HP_ROTARY_PLAIN && (!(s.factor > 0) || !std::isfinite(s.factor))) return HP_EINVAL;
+    if (s.kind == HP_ROTARY_BASE && rot < 4) return HP_EINVAL;
+    if (s.kind == HP_ROTARY_BY_TURNS && (!(s.original_length > 0) || !std::isfinite(s.original_length) || !(s.low_turns < s.high_turns) ||
+                                         !std::isfinite(s.high_turns - s.low_turns)))
+        return HP_EINVAL;
+    if (misaligned(table, 4)) return HP_EALIGN;
+    if (n == 0) return HP_OK;
+    TableParams t{table, n, first, rot / 2, s.kind, std::log(s.base), s.factor, s.original_length, s.low_turns, s.high_turns, s.amplitude};
+    if (s.kind == HP_ROTARY_BASE) t.log_base += std::log(s.factor) * rot / (rot - 2);
+    const int64_t blocks = (n * t.half + kThreads - 1) / kThreads;
+    table_kernel<<<(uint32_t)(blocks < 65536 ? blocks : 65536), kThreads, 0, (hipStream_t)stream>>>(t);
+    return hip_failed(hipGetLastError()) ? HP_EHIP : HP_OK;
+}
+
+int hp_rotary(const hp_rotary_args_t *a, void *stream) {
+    if (!a) return HP_EINVAL;
+    if (a->dtype != HP_BF16 && a->dtype != HP_F32) return HP_EINVAL;
+    if (a->n_tensors < 1 || a->n_tensors > HP_ROTARY_MAX_TENSORS || a->rows < 0 || a->table_rows < 1) return HP_EINVAL;
+    if (a->dim < 2 || a->dim > 1024 || a->rot < 2 || a->rot % 2 || a->rot > a->dim) return HP_EINVAL;
+    if (a->n_axes < 1 || a->n_axes > HP_ROTARY_MAX_AXES) return HP_EINVAL;
+    RotaryParams p{};
+    p.half = a->rot / 2;
+    if (a->n_axes > 1) {
+        int64_t sum = 0;
+        for (int i = 0; i < a->n_axes; ++i) {
+            if (a->sections[i] < 0) return HP_EINVAL;
+            sum += a->sections[i];
+            if (sum > p.half) return HP_EINVAL;
+            p.axis_end[i] = (int32_t)sum;
+        }
+        if (sum != p.half) return HP_EINVAL;
+    }
+    const int size = a->dtype == HP_BF16 ? 2 : 4;
+    bool in_place = true;
+    int64_t n_heads = 0;
+    for (int t = 0; t < a->n_tensors; ++t) {
+        if (a->heads[t] < 0 || a->heads[t] > 4096) return HP_EINVAL;
+        if (a->rows > 0 && a->heads[t] > 0 && (!a->x[t].data || !a->out[t].data)) return HP_EINVAL;
+        if (misaligned(a->x[t].data, size) || misaligned(a->out[t].data, size)) return HP_EALIGN;
+        const bool same = a->x[t].data == a->out[t].data;
+        if (same && (a->x[t].row_stride != a->out[t].row_stride || a->x[t].head_stride != a->out[t].head_stride)) return HP_EINVAL;
+        in_place = in_place && same;
+        n_heads += a->heads[t];
+        p.heads[t] = a->heads[t];
+        p.x[t] = a->x[t];
+        p.out[t] = a->out[t];
+    }
+    if (a->rows > 0 && n_heads > 0 && (!a->table || !a->positions)) return HP_EINVAL;
+    if (misaligned(a->table, 4) || misaligned(a->positions, 4)) return HP_EALIGN;
+    if (a->rows == 0 || n_heads == 0) return HP_OK;
+    p.rows = a->rows;
+    p.table_rows = a->table_rows;
+    p.axis_stride = a->axis_stride;
+    p.table = a->table;
+    p.positions = a->positions;
+    p.n_tensors = a->n_tensors;
+    p.n_heads = (int32_t)n_heads;
+    p.dim = a->dim;
+    p.n_axes = a->n_axes;
+    p.inverse = a->inverse != 0;
+    // The widest lanes that divide the pairs and the channels behind them, 16 bytes at most.
+    const bool copies = !in_place && a->dim > a->rot, inter = a->interleaved != 0;
+    const int all = p.half | (copies ? a->dim - a->rot : 0);
+    const hipStream_t s = (hipStream_t)stream;
+    if (a->dtype == HP_BF16) {
+        if (all % 8 == 0) launch<__bf16, 8>(p, inter, copies, s);
+        else if (all % 4 == 0) launch<__bf16, 4>(p, inter, copies, s);
+        else if (all % 2 == 0) launch<__bf16, 2>(p, inter, copies, s);
+        else launch<__bf16, 1>(p, inter, copies, s);
+    } else {
+        if (all % 4 == 0) launch<float, 4>(p, inter, copies, s);
+        else if (all % 2 == 0) launch<float, 2>(p, inter, copies, s);
+        else launch<float, 1>(p, inter, copies, s);
+    }
+    return hip_failed(hipGetLastError()) ? HP_EHIP : HP_OK;
+}
+
+}  // extern "C"
