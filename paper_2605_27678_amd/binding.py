@@ -78,6 +78,7 @@ EXPORTS = ["hp_plan_create", "hp_plan_create_host", "hp_plan_create_batched", "h
 
 _handle = None
 _marshal = None                 # hp_marshal's call(), once loaded
+_marshal_module = None          # hp_marshal itself, if it is used
 _ADDR = {}                      # addresses of the calls that go through it
 SRC, DST, ACCUM = 0, 1, 2       # what a list of buffers is: source, destination, binary32 accumulators
 
@@ -91,7 +92,7 @@ class _Desc(C.Structure):
 def _load_marshal():
     """Loads hp_marshal.so once.  Only called when torch is there (it needs its libraries).  Without it, or with one that
     was built for another torch, every call takes the way through Python."""
-    global _marshal
+    global _marshal, _marshal_module
     from importlib.machinery import ExtensionFileLoader
     from importlib.util import module_from_spec, spec_from_file_location
     path = os.path.join(_PKG, "hp_marshal.so")
@@ -110,6 +111,7 @@ def _load_marshal():
     for name in ("hp_forward", "hp_forward_static", "hp_backward", "hp_backward_accumulate", "hp_text_grads"):
         _ADDR[name] = C.cast(getattr(_lib(), name), C.c_void_p).value
     _marshal = module.call
+    _marshal_module = module
 
 
 def _leave(*args):

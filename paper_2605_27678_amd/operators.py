@@ -19,7 +19,7 @@ from typing import Optional, Sequence
 import numpy as np
 
 from . import binding
-from .binding import _check, _stream_handle, _token_map, hp_token_map_t
+from .binding import HpError, _check, _stream_handle, _token_map, hp_token_map_t
 from .workloads import TokenMap
 
 MAX_TENSORS = MAX_AXES = 4
@@ -74,6 +74,31 @@ EXPORTS = ["hp_rotary_table", "hp_rotary", "hp_gated_norm", "hp_gated_norm_backw
            "hp_image_ranges"]
 
 _ready = None
+_fast = None            # hp_marshal, or False where it is not used
+_at = {}                # addresses of the calls that go through it
+
+
+def _call(function: str, name: str, *args) -> bool:
+    """The call through hp_marshal.  False if the arguments need a closer look than it takes."""
+    global _fast
+    if _fast is None:
+        if "torch" not in sys.modules:
+            return False
+        if binding._marshal is None:
+            binding._load_marshal()
+        _fast = binding._marshal_module or False
+        L = _lib()
+        for f in ("hp_rotary", "hp_gated_norm", "hp_gated_norm_backward", "hp_cross_attend", "hp_cross_attend_step",
+                  "hp_cross_attend_backward"):
+            _at[f] = C.cast(getattr(L, f), C.c_void_p).value
+    if _fast is False:
+        return False
+    rc = getattr(_fast, function)(_at[name], *args)
+    if rc is None:
+        return False
+    if rc < 0:
+        raise HpError(rc, name)
+    return True
 
 
 def _lib():
@@ -181,6 +206,8 @@ def hp_rotary(xs: Sequence, outs: Sequence, table, positions, *, interleaved: bo
     """outs[t] = xs[t] [rows, heads, dim] turned by `positions`, int32 [rows], or [axes, rows] with `sections`, the
     numbers of pairs that go by each axis.  The table's width says how many channels turn.  xs and outs: lists of up
     to four tensors (queries and keys); an output may be its input."""
+    if _call("rotary", "hp_rotary", xs, outs, table, positions, interleaved, inverse, sections, stream):
+        return
     torch = sys.modules.get("torch")
     if not 1 <= len(xs) <= MAX_TENSORS or len(xs) != len(outs):
         raise ValueError(f"need 1 to {MAX_TENSORS} tensors and as many outputs")
@@ -236,6 +263,9 @@ def hp_gated_norm(x, y, h, z, w_post=None, gate=None, w_pre=None, *, gate_tanh: 
     """h = residual_scale * x + t * norm(y) * w_post and z = norm(h) * w_pre for rows [rows, hidden]; t = gate or
     tanh(gate), one value or one a channel.  w_post None: y is taken as it is; gate None: t = 1; y None: no block.
     h or z None: not written.  rstd: float32 [2, rows] for the backward call."""
+    if _call("norm", "hp_gated_norm", x, y, w_post, gate, w_pre, gate_tanh, residual_scale, unit_offset, eps, rstd, h, z,
+             stream):
+        return
     a = _norm_args(x, y, w_post, gate, w_pre, gate_tanh, residual_scale, unit_offset, eps, rstd)
     for name, t in (("h", h), ("z", z)):
         if t is not None:
@@ -253,6 +283,9 @@ def hp_gated_norm_backward(dh, dz, x, y, rstd, w_post, gate, w_pre, dx, dy, dw_p
                            gate_tanh: bool = False, residual_scale: float = 1.0, unit_offset: bool = False,
                            eps: float = 1e-6, workspace=None, stream=None) -> None:
     """Gradients of hp_gated_norm from those of h and z (one may be None).  Outputs that are None are not computed."""
+    if _call("norm_backward", "hp_gated_norm_backward", x, y, w_post, gate, w_pre, gate_tanh, residual_scale, unit_offset,
+             eps, rstd, dh, dz, dx, dy, dw_post, dgate, dw_pre, workspace, stream):
+        return
     a = _norm_args(x, y, w_post, gate, w_pre, gate_tanh, residual_scale, unit_offset, eps, rstd)
     g = hp_norm_grads_t()
     for name, t in (("dh", dh), ("dz", dz), ("dx", dx), ("dy", dy)):
@@ -297,6 +330,8 @@ def hp_cross_attend(q, k, v, ranges, out, *, lse=None, scale: Optional[float] = 
     """out = attention of query rows q [rows, heads_q, dim] to states k, v [keys, heads_k, dim]; row r sees states
     ranges[r, 0] to ranges[r, 1] - 1 (int32; None: all).  scale None: 1 / sqrt(dim).  lse: float32 [rows, heads_q]
     for the backward call."""
+    if _call("attend", "hp_cross_attend", q, k, v, ranges, out, lse, scale, workspace, None, stream):
+        return
     a = _attend_args(q, k, v, ranges, out, lse, scale, workspace)
     _check(_lib().hp_cross_attend(C.byref(a), _stream_handle(stream)), "hp_cross_attend")
 
@@ -304,6 +339,8 @@ def hp_cross_attend(q, k, v, ranges, out, *, lse=None, scale: Optional[float] = 
 def hp_cross_attend_step(q, k, v, ranges, out, *, lse=None, scale: Optional[float] = None, workspace=None,
                          stream=None) -> None:
     """hp_cross_attend for rows that share nothing, as single tokens of many requests."""
+    if _call("attend", "hp_cross_attend_step", q, k, v, ranges, out, lse, scale, workspace, None, stream):
+        return
     a = _attend_args(q, k, v, ranges, out, lse, scale, workspace)
     _check(_lib().hp_cross_attend_step(C.byref(a), _stream_handle(stream)), "hp_cross_attend_step")
 
@@ -311,6 +348,8 @@ def hp_cross_attend_step(q, k, v, ranges, out, *, lse=None, scale: Optional[floa
 def hp_cross_attend_backward(q, k, v, ranges, out, lse, dout, dq, dk, dv, *, scale: Optional[float] = None,
                              workspace=None, stream=None) -> None:
     """Gradients of q, k and v from the forward's arguments, its out and lse, and the gradient of out."""
+    if _call("attend", "hp_cross_attend_backward", q, k, v, ranges, out, lse, scale, workspace, (dout, dq, dk, dv), stream):
+        return
     a = _attend_args(q, k, v, ranges, out, lse, scale, workspace)
     for name, t, like in (("dout", dout, q), ("dq", dq, q), ("dk", dk, k), ("dv", dv, k)):
         setattr(a, name, _heads(_tensor(t, name, like.shape, like=q)))
