@@ -39,9 +39,16 @@ constexpr int kStepKeys = 32 * kWaves;              // states that a workgroup o
 typedef float Acc __attribute__((ext_vector_type(16)));
 template <class T> using Frag = Vec<T, 8>;
 
+// Division of numbers below 2^31 by one that a launch keeps.
+struct Divisor {
+    uint32_t by, factor, shift;
+    __device__ __forceinline__ int operator()(int n) const { return (int)(by == 1 ? (uint32_t)n : __umulhi((uint32_t)n, factor) >> shift); }
+};
+
 struct Attend {
     int64_t rows, keys;
     int32_t heads_q, heads_k, group, dim, splits, m_total;
+    Divisor by_group;
     float scale, scale2;                            // scale2: for exponents of two
     hp_heads_t q, k, v, out, dout, dq, dk, dv;
     const int32_t *ranges;
@@ -61,36 +68,70 @@ __device__ __forceinline__ Acc mma(const Frag<float> &a, const Frag<float> &b, A
     return c;
 }
 
-// Elements between rows of a tile in LDS: 32 bytes more than the row, so that eight rows at one place, and four rows
-// of 32 bytes, lie in different banks.
-template <class T, int DP> constexpr int kLd = DP + 32 / (int)sizeof(T);
+// A tile of states or query rows in LDS: rows of DP elements, one behind the other as the loads that write LDS directly
+// leave them, the 16-byte pieces of each row turned among themselves.  Operands take one piece of 8 neighbouring rows, or
+// two pieces of 4, at a time: turned, these lie in different banks.
+template <class T, int DP> struct Tile {
+    static constexpr int kPiece = 16 / (int)sizeof(T), kPieces = DP / kPiece;
+    static __device__ __forceinline__ int turn(int row) {              // the same for rows 16 apart
+        if constexpr (kPieces == 8) return (row & 6) | ((row >> 3) & 1);
+        else if constexpr (kPieces == 12) return (row >> 2) & 3;
+        else if constexpr (kPieces == 24) return (row >> 1) & 7;
+        else return ((row << 1) & 14) | ((row >> 3) & 1);
+    }
+    static constexpr bool kRolls = kPieces == 12 || kPieces == 24;     // no power of two: turned round, not exchanged
+    static __device__ __forceinline__ int slot_of(int row, int piece) {
+        if constexpr (kRolls) {
+            const int at = piece + turn(row);
+            return at >= kPieces ? at - kPieces : at;
+        } else return piece ^ turn(row);
+    }
+    static __device__ __forceinline__ int piece_of(int row, int slot) {
+        if constexpr (kRolls) {
+            const int at = slot - turn(row);
+            return at < 0 ? at + kPieces : at;
+        } else return slot ^ turn(row);
+    }
+    static __device__ __forceinline__ int offset(int row, int piece) { return row * DP + slot_of(row, piece) * kPiece; }
+    static __device__ __forceinline__ float value(const T *tile, int row, int channel) {
+        return (float)tile[offset(row, channel / kPiece) + channel % kPiece];
+    }
+};
 
 // Row `row` of a tile, channels 16s + 8(l / 32) and on: an operand whose inner index is the channel.
-template <class T> __device__ __forceinline__ Frag<T> row_frag(const T *tile, int ld, int row, int s, int half) {
-    typedef Frag<T> aligned __attribute__((aligned(16)));
-    return *(const aligned *)(tile + row * ld + 16 * s + 8 * half);
+template <class T, int DP> __device__ __forceinline__ Frag<T> row_frag(const T *tile, int row, int s, int half) {
+    typedef Vec<T, 16 / (int)sizeof(T)> Piece;
+    if constexpr (sizeof(T) == 2) {
+        return *(const Piece *)(tile + Tile<T, DP>::offset(row, 2 * s + half));
+    } else {
+        const Piece a = *(const Piece *)(tile + Tile<T, DP>::offset(row, 4 * s + 2 * half)), b = *(const Piece *)(tile + Tile<T, DP>::offset(row, 4 * s + 2 * half + 1));
+        return Frag<T>{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    }
 }
 
 // Rows 16 ks + 4(l / 32) + {0..3} and 8 more of a tile, at channel 32 db + l % 32: a left operand whose inner index is
 // the tile's row, in the order in which a lane holds the rows of a result.
-template <class T> __device__ __forceinline__ Frag<T> column_frag(const T *tile, int ld, int ks, int db, int lane) {
+template <class T, int DP> __device__ __forceinline__ Frag<T> column_frag(const T *tile, int ks, int db, int lane) {
     if constexpr (sizeof(T) == 2) {
         typedef short Quad __attribute__((ext_vector_type(4)));
         typedef __attribute__((address_space(3))) Quad *Lds;
-        const int i = lane % 16, row = 16 * ks + 4 * (lane / 32) + i / 4, col = 32 * db + 16 * ((lane / 16) % 2) + 4 * (i % 4);
-        const T *p = tile + row * ld + col;
+        // 16 lanes together take 16 channels of four rows, four of them each, and get four rows of one
+        const int i = lane % 16, row = 4 * (lane / 32) + i / 4, piece = 4 * db + 2 * ((lane / 16) % 2) + (i % 4) / 2;
         union {
             Quad q[2];
             Frag<T> f;
         } u;
-        u.q[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)p);
-        u.q[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(p + 8 * ld));
+        u.q[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(tile + Tile<T, DP>::offset(row, piece) + 16 * ks * DP + 4 * (i % 2)));
+        u.q[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(tile + Tile<T, DP>::offset(row + 8, piece) + 16 * ks * DP + 4 * (i % 2)));
         return u.f;
     } else {
         Frag<T> f;
-        const T *p = tile + (16 * ks + 4 * (lane / 32)) * ld + 32 * db + lane % 32;
+        const int channel = 32 * db + lane % 32;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = p[(8 * (j / 4) + j % 4) * ld];
+        for (int j = 0; j < 8; ++j) {
+            const int row = 4 * (lane / 32) + 8 * (j / 4) + j % 4;
+            f[j] = tile[Tile<T, DP>::offset(row, channel / 4) + 16 * ks * DP + channel % 4];
+        }
         return f;
     }
 }
@@ -111,20 +152,25 @@ __device__ __forceinline__ float2 both_halves(float x) {
     return make_float2(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-template <class T> __device__ __forceinline__ bool not_finite(const Frag<T> &f) {
+// Whether any of the tile's values is an infinity or NaN, as far as this lane looks.
+template <class T, int DP, int ROWS> __device__ __forceinline__ bool not_finite(const T *tile, int tid) {
+    typedef uint32_t Piece __attribute__((ext_vector_type(4)));
     bool bad = false;
+    for (int e = tid; e < ROWS * Tile<T, DP>::kPieces; e += kBlock) {
+        const Piece v = *(const Piece *)(tile + e * Tile<T, DP>::kPiece);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        if constexpr (sizeof(T) == 2) bad |= (__builtin_bit_cast(uint16_t, f[j]) & 0x7f80) == 0x7f80;
-        else bad |= (__builtin_bit_cast(uint32_t, f[j]) & 0x7f800000) == 0x7f800000;
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (sizeof(T) == 2) bad |= (v[j] & 0x7f80u) == 0x7f80u || (v[j] & 0x7f800000u) == 0x7f800000u;
+            else bad |= (v[j] & 0x7f800000u) == 0x7f800000u;
+        }
     }
     return bad;
 }
 
-// acc^T += tile^T p^T over the 32 rows of a tile that p holds, leaving out what is not seen: for values there that are
-// not finite, which a product would carry into every row.
-template <class T, int DB, class Seen>
-__device__ __forceinline__ void careful_product(Acc (&acc)[DB], const Acc &p, const T *tile, int ld, int half, const Seen &seen) {
+// acc^T += tile^T p^T over 32 rows of a tile that p holds (from `row0`), leaving out what is not seen: for values there
+// that are not finite, which a product would carry into every row.
+template <class T, int DP, int DB, class Seen>
+__device__ __forceinline__ void careful_product(Acc (&acc)[DB], const Acc &p, const T *tile, int row0, int half, const Seen &seen) {
     for (int j = 0; j < 32; ++j) {
         float own = 0.0f;
 #pragma unroll
@@ -132,37 +178,77 @@ __device__ __forceinline__ void careful_product(Acc (&acc)[DB], const Acc &p, co
         const float2 two = both_halves(own);
         const float w = (j / 4) % 2 ? two.y : two.x;
         if (!seen(j)) continue;
-        const T *row = tile + j * ld;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) acc[db][i] += w * (float)row[32 * db + result_row(i, half)];
+            for (int i = 0; i < 16; ++i) acc[db][i] += w * Tile<T, DP>::value(tile, row0 + j, 32 * db + result_row(i, half));
     }
 }
 
-// A tile of ROWS rows on its way from memory through registers to LDS; channels from dim on are zeros.
-template <class T, int DP, int ROWS, int THREADS> struct Stage {
-    static constexpr int kChunks = DP / 8, kEach = (ROWS * kChunks + THREADS - 1) / THREADS;
-    Frag<T> r[kEach];
-    // at(row): the row's address, or NULL for zeros
-    template <class At> __device__ __forceinline__ void fetch(int tid, int dim, const At &at) {
+// Brings tiles of ROWS rows from memory to LDS.  Where rows are whole aligned pieces (EXACT) the loads write LDS
+// themselves, from a buffer that begins at the tile's first row, and what lies behind its rows or channels is out of the
+// buffer's bounds and comes as zeros; the caller waits (arrived()) before the barrier behind which the tile is read.
+// Other rows pass through registers at once.
+constexpr uint32_t kOutside = 0x80000000u;
+__device__ __forceinline__ void arrived() { __builtin_amdgcn_s_waitcnt(0x0f70); }            // vmcnt(0)
+
+template <class T, int DP, int ROWS, int THREADS, bool EXACT> struct Loader {
+    typedef Tile<T, DP> L;
+    static constexpr int kEach = ROWS * L::kPieces / THREADS;
+    static_assert(ROWS * L::kPieces % THREADS == 0, "a tile is the same number of pieces for every lane");
+    static __device__ __forceinline__ void piece(T *tile, int n, const T *p, int valid, int tid) {
+        *(Vec<T, L::kPiece> *)(tile + (n * THREADS + tid) * L::kPiece) = load<L::kPiece>(p, valid);
+    }
+    static __device__ __forceinline__ void direct(T *tile, int n, const __amdgpu_buffer_rsrc_t &from, uint32_t offset, int tid) {
+        // a wave writes 64 pieces in a row
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)(tile + (n * THREADS + __builtin_amdgcn_readfirstlane(tid / kWave * kWave)) * L::kPiece),
+                                                 16, (int)offset, 0, 0, 0);
+    }
+    static __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void *base) {
+        return __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, 0x7fffffff, 0x00020000);
+    }
+    uint32_t offsets[EXACT ? kEach : 1];
+
+    // Tiles of consecutive rows of one head.
+    __device__ __forceinline__ void plan(int64_t row_stride, int dim, int tid) {
+        if constexpr (EXACT)
 #pragma unroll
-        for (int n = 0; n < kEach; ++n) {
-            const int e = n * THREADS + tid, row = e / kChunks, c = e % kChunks;
-            const T *p = row < ROWS ? at(row) : nullptr;
-            r[n] = load<8>(p + 8 * c, p ? dim - 8 * c : 0);
+            for (int n = 0; n < kEach; ++n) {
+                const int e = n * THREADS + tid, row = e / L::kPieces, c = L::piece_of(row, e % L::kPieces);
+                offsets[n] = c * L::kPiece < dim ? (uint32_t)(row * row_stride * sizeof(T)) + c * 16 : kOutside;
+            }
+    }
+    // first: the tile's first row; left: rows from there on that are there
+    __device__ __forceinline__ void fetch(T *tile, const T *first, int64_t row_stride, int left, int dim, int tid) const {
+        if constexpr (EXACT) {
+            const auto from = buffer(first);
+#pragma unroll
+            for (int n = 0; n < kEach; ++n) direct(tile, n, from, (n * THREADS + tid) / L::kPieces < left ? offsets[n] : kOutside, tid);
+        } else {
+#pragma unroll
+            for (int n = 0; n < kEach; ++n) {
+                const int e = n * THREADS + tid, row = e / L::kPieces, c = L::piece_of(row, e % L::kPieces);
+                piece(tile, n, first + row * row_stride + c * L::kPiece, row < left ? dim - c * L::kPiece : 0, tid);
+            }
         }
     }
-    __device__ __forceinline__ bool commit(T *tile, int tid, bool look) {
-        typedef Frag<T> aligned __attribute__((aligned(16)));
-        bool bad = false;
+    // Rows M of the matrix that a state head's query heads make.
+    static __device__ __forceinline__ void fetch_m(T *tile, const hp_heads_t &x, int m0, int m_total, const Divisor &group, int head0, int dim, int tid) {
+        const int row0 = __builtin_amdgcn_readfirstlane(group(m0));
+        const T *first = (const T *)x.data + row0 * x.row_stride + (int64_t)head0 * x.head_stride;
+        const auto from = buffer(first);
 #pragma unroll
         for (int n = 0; n < kEach; ++n) {
-            const int e = n * THREADS + tid, row = e / kChunks, c = e % kChunks;
-            if (row < ROWS) *(aligned *)(tile + row * kLd<T, DP> + 8 * c) = r[n];
-            if (look) bad |= not_finite<T>(r[n]);
+            const int e = n * THREADS + tid, r = e / L::kPieces, c = L::piece_of(r, e % L::kPieces), m = m0 + r;
+            const int row = group(m), head = m - row * (int)group.by;
+            if constexpr (EXACT) {
+                const uint32_t at = (uint32_t)(((row - row0) * (int)x.row_stride + head * (int)x.head_stride) * (int)sizeof(T)) + c * 16;
+                direct(tile, n, from, m < m_total && c * L::kPiece < dim ? at : kOutside, tid);
+            } else {
+                const int64_t at = (row - row0) * x.row_stride + head * x.head_stride + c * L::kPiece;
+                piece(tile, n, first + at, m < m_total ? dim - c * L::kPiece : 0, tid);
+            }
         }
-        return bad;
     }
 };
 
@@ -218,7 +304,7 @@ __device__ __forceinline__ Place place_of(const Attend &p, int m, int state_head
     Place at;
     at.valid = m < p.m_total;
     at.m = at.valid ? m : p.m_total - 1;
-    at.row = at.m / p.group;
+    at.row = p.by_group(at.m);
     at.head = state_head * p.group + (at.m - at.row * p.group);
     return at;
 }
@@ -279,18 +365,15 @@ template <class T, int DB> __device__ __forceinline__ void store_result(T *to, c
         }
 }
 
-// Whether a tile is loaded into registers while the one before it is worked on: where 1 KiB rows leave no room for it,
-// tiles go to LDS as they come.
-template <class T, int DP> constexpr bool kAhead = DP < 256;
+template <class T, int DP> constexpr int kTileRows = DP * sizeof(T) <= 256 ? 64 : 32;
 
-template <class T> constexpr int kTileKeys = sizeof(T) == 2 ? 64 : 32;
-
-// One workgroup: 128 rows M against a part of what they see.
-template <class T, int DP> __global__ __launch_bounds__(kBlock) void attend_forward_kernel(Attend p) {
-    constexpr int NK = kTileKeys<T>, NB = NK / 32, DB = DP / 32, DS = DP / 16, LD = kLd<T, DP>;
-    __shared__ __attribute__((aligned(16))) T k_tile[NK * LD], v_tile[NK * LD];
+// One workgroup: 128 rows M against a part of what they see.  Two tiles of states in LDS: while one is worked on the next
+// is on its way.
+template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock, DP * sizeof(T) <= 256 ? 2 : 1) void attend_forward_kernel(Attend p) {
+    constexpr int NK = kTileRows<T, DP>, NB = NK / 32, DB = DP / 32, DS = DP / 16;
+    __shared__ __attribute__((aligned(16))) T k_tiles[2][NK * DP], v_tiles[2][NK * DP];
     __shared__ Bounds slots[kWaves];
-    __shared__ int bad[2];                           // by turns: the one of the next tile is cleared where all are done with the last
+    __shared__ int bad[2];                           // by turns: the next tile's is cleared where all are done with the last
     const int tid = (int)threadIdx.x, lane = tid % kWave, wave = tid / kWave, half = lane / 32, col = lane % 32;
     const int state_head = (int)blockIdx.y, split = (int)blockIdx.z;
     // later rows tend to see more: they begin first
@@ -309,36 +392,34 @@ template <class T, int DP> __global__ __launch_bounds__(kBlock) void attend_forw
     Acc acc[DB] = {};
     const int tiles = any.end > any.first ? (any.end - any.first + NK - 1) / NK : 0;
     const int begin = (int)((int64_t)tiles * split / p.splits), end = (int)((int64_t)tiles * (split + 1) / p.splits);
-    Stage<T, DP, NK, kBlock> ks, vs;
-    auto fetch_k = [&](int tile) {
-        const int key0 = any.first + tile * NK;
-        ks.fetch(tid, p.dim, [&](int r) { return key0 + r < any.end ? address<const T>(p.k, key0 + r, state_head) : nullptr; });
+    Loader<T, DP, NK, kBlock, EXACT> ks, vs;
+    ks.plan(p.k.row_stride, p.dim, tid);
+    vs.plan(p.v.row_stride, p.dim, tid);
+    auto fetch = [&](int tile) {
+        const int key0 = any.first + tile * NK, stage = tile & 1;
+        ks.fetch(k_tiles[stage], address<const T>(p.k, key0, state_head), p.k.row_stride, any.end - key0, p.dim, tid);
+        vs.fetch(v_tiles[stage], address<const T>(p.v, key0, state_head), p.v.row_stride, any.end - key0, p.dim, tid);
     };
-    auto fetch_v = [&](int tile) {
-        const int key0 = any.first + tile * NK;
-        vs.fetch(tid, p.dim, [&](int r) { return key0 + r < any.end ? address<const T>(p.v, key0 + r, state_head) : nullptr; });
-    };
-    if (kAhead<T, DP> && begin < end) fetch_k(begin), fetch_v(begin);
+    if (begin < end) fetch(begin);
     for (int tile = begin; tile < end; ++tile) {
-        const int key0 = any.first + tile * NK;
-        const bool look = !any.covers(key0, key0 + NK);
-        const int turn = (tile - begin) % 2;
-        __syncthreads();                             // the last tile's readers are done
-        if (tid == 0) bad[turn ^ 1] = 0;
-        if constexpr (!kAhead<T, DP>) fetch_k(tile);
-        ks.commit(k_tile, tid, false);
-        if constexpr (!kAhead<T, DP>) fetch_v(tile);
-        if (vs.commit(v_tile, tid, look)) bad[turn] = 1;
-        __syncthreads();
-        if (kAhead<T, DP> && tile + 1 < end) fetch_k(tile + 1), fetch_v(tile + 1);
+        const int key0 = any.first + tile * NK, stage = tile & 1;
+        const T *k_tile = k_tiles[stage], *v_tile = v_tiles[stage];
+        arrived();
+        __syncthreads();                             // this tile is there, and the last one's readers are done
+        if (tile + 1 < end) fetch(tile + 1);
+        if (tid == 0) bad[stage ^ 1] = 0;
+        if (!any.covers(key0, key0 + NK)) {
+            if (not_finite<T, DP, NK>(v_tile, tid)) bad[stage] = 1;
+            __syncthreads();
+        }
         if (!own.meets(key0, key0 + NK)) continue;
         Acc s[NB];
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            s[b] = Acc{};
+        for (int b = 0; b < NB; ++b) s[b] = Acc{};
 #pragma unroll
-            for (int d = 0; d < DS; ++d) s[b] = mma(row_frag(k_tile, LD, 32 * b + col, d, half), q[d], s[b]);
-        }
+        for (int d = 0; d < DS; ++d)
+#pragma unroll
+            for (int b = 0; b < NB; ++b) s[b] = mma(row_frag<T, DP>(k_tile, 32 * b + col, d, half), q[d], s[b]);
         const bool whole = own.covers(key0, key0 + NK);
         if (!whole)
 #pragma unroll
@@ -347,17 +428,17 @@ template <class T, int DP> __global__ __launch_bounds__(kBlock) void attend_forw
                 for (int i = 0; i < 16; ++i)
                     s[b][i] = see.has(key0 + 32 * b + result_row(i, half)) ? s[b][i] : -INFINITY;
         soften(run, s, acc, p.scale2);
-        if (!whole && bad[turn]) {
+        if (!whole && bad[stage]) {
 #pragma unroll
             for (int b = 0; b < NB; ++b)
-                careful_product<T, DB>(acc, s[b], v_tile + 32 * b * LD, LD, half, [&](int j) { return see.has(key0 + 32 * b + j); });
+                careful_product<T, DP, DB>(acc, s[b], v_tile, 32 * b, half, [&](int j) { return see.has(key0 + 32 * b + j); });
             continue;
         }
 #pragma unroll
         for (int k = 0; k < 2 * NB; ++k) {
             const Frag<T> w = result_frag<T>(s[k / 2], k % 2);
 #pragma unroll
-            for (int db = 0; db < DB; ++db) acc[db] = mma(column_frag(v_tile, LD, k, db, lane), w, acc[db]);
+            for (int db = 0; db < DB; ++db) acc[db] = mma(column_frag<T, DP>(v_tile, k, db, lane), w, acc[db]);
         }
     }
     const float2 two = both_halves(run.sum);
@@ -381,20 +462,20 @@ template <class T, int DP> __global__ __launch_bounds__(kBlock) void attend_forw
 
 // One workgroup: up to 32 heads of one row against a part of what the row sees.  The waves take 32 states each on their
 // own, without waiting for one another, and join at the end.
-// Waves of a workgroup: as LDS has room for their tiles.
+// Waves of a workgroup, and tiles that each has on their way or in work: as LDS has room for.
 template <class T, int DP> constexpr int kStepWaves = DP * sizeof(T) <= 512 ? 4 : 2;
+template <class T, int DP> constexpr int kStepStages = DP * sizeof(T) <= 256 ? 2 : 1;
 
-template <class T, int DP> __global__ __launch_bounds__((kStepWaves<T, DP> * kWave)) void attend_step_kernel(Attend p) {
-    constexpr int kWaves = kStepWaves<T, DP>, DB = DP / 32, DS = DP / 16, LD = kLd<T, DP>;
-    __shared__ __attribute__((aligned(16))) T tiles[kWaves][2][32 * LD];
+template <class T, int DP, bool EXACT> __global__ __launch_bounds__((kStepWaves<T, DP> * kWave)) void attend_step_kernel(Attend p) {
+    constexpr int kWaves = kStepWaves<T, DP>, kStages = kStepStages<T, DP>, DB = DP / 32, DS = DP / 16;
+    __shared__ __attribute__((aligned(16))) T tiles[kWaves][kStages][2][32 * DP];
     __shared__ float tops[kWaves][32], sums[kWaves][32];
-    const int tid = (int)threadIdx.x, lane = tid % kWave, wave = tid / kWave, half = lane / 32, col = lane % 32;
+    const int tid = (int)threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), half = lane / 32, col = lane % 32;
     const int64_t row = blockIdx.x;
     const int parts = (p.group + 31) / 32, state_head = (int)blockIdx.y / parts, first_head = ((int)blockIdx.y % parts) * 32;
     const int split = (int)blockIdx.z;
     const int heads = min(p.group - first_head, 32), head0 = state_head * p.group + first_head;
     const Range see = range_of(p, row);
-    T *k_tile = tiles[wave][0], *v_tile = tiles[wave][1];
     Frag<T> q[DS];
 #pragma unroll
     for (int s = 0; s < DS; ++s) {
@@ -405,29 +486,30 @@ template <class T, int DP> __global__ __launch_bounds__((kStepWaves<T, DP> * kWa
     Acc acc[DB] = {};
     const int n_tiles = (see.hi - see.lo + 31) / 32;
     const int begin = (int)((int64_t)n_tiles * split / p.splits), end = (int)((int64_t)n_tiles * (split + 1) / p.splits);
-    Stage<T, DP, 32, kWave> ks, vs;
-    auto fetch_k = [&](int tile) {
+    Loader<T, DP, 32, kWave, EXACT> ks, vs;
+    ks.plan(p.k.row_stride, p.dim, lane);
+    vs.plan(p.v.row_stride, p.dim, lane);
+    auto fetch = [&](int tile, int stage) {
         const int key0 = see.lo + tile * 32;
-        ks.fetch(lane, p.dim, [&](int r) { return key0 + r < see.hi ? address<const T>(p.k, key0 + r, state_head) : nullptr; });
+        ks.fetch(tiles[wave][stage][0], address<const T>(p.k, key0, state_head), p.k.row_stride, see.hi - key0, p.dim, lane);
+        vs.fetch(tiles[wave][stage][1], address<const T>(p.v, key0, state_head), p.v.row_stride, see.hi - key0, p.dim, lane);
     };
-    auto fetch_v = [&](int tile) {
-        const int key0 = see.lo + tile * 32;
-        vs.fetch(lane, p.dim, [&](int r) { return key0 + r < see.hi ? address<const T>(p.v, key0 + r, state_head) : nullptr; });
-    };
-    if (kAhead<T, DP> && begin + wave < end) fetch_k(begin + wave), fetch_v(begin + wave);
-    for (int tile = begin + wave; tile < end; tile += kWaves) {
-        const int key0 = see.lo + tile * 32;
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");     // the wave's own LDS: its loads of the last tile come first
-        if constexpr (!kAhead<T, DP>) fetch_k(tile);
-        ks.commit(k_tile, lane, false);
-        if constexpr (!kAhead<T, DP>) fetch_v(tile);
-        vs.commit(v_tile, lane, false);
+    // a wave's tiles are its own: no barriers, only its own loads to wait for and its own reads to finish
+    auto settle = [] {
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
-        if (kAhead<T, DP> && tile + kWaves < end) fetch_k(tile + kWaves), fetch_v(tile + kWaves);
+    };
+    int stage = 0;
+    if (begin + wave < end) fetch(begin + wave, 0);
+    for (int tile = begin + wave; tile < end; tile += kWaves) {
+        const int key0 = see.lo + tile * 32;
+        const T *k_tile = tiles[wave][stage][0], *v_tile = tiles[wave][stage][1];
+        arrived();
+        settle();
+        if (kStages > 1 && tile + kWaves < end) fetch(tile + kWaves, stage ^ 1);
         Acc s[1] = {};
 #pragma unroll
-        for (int d = 0; d < DS; ++d) s[0] = mma(row_frag(k_tile, LD, col, d, half), q[d], s[0]);
+        for (int d = 0; d < DS; ++d) s[0] = mma(row_frag<T, DP>(k_tile, col, d, half), q[d], s[0]);
         if (key0 + 32 > see.hi)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[0][i] = key0 + result_row(i, half) < see.hi ? s[0][i] : -INFINITY;
@@ -436,9 +518,12 @@ template <class T, int DP> __global__ __launch_bounds__((kStepWaves<T, DP> * kWa
         for (int k = 0; k < 2; ++k) {
             const Frag<T> w = result_frag<T>(s[0], k);
 #pragma unroll
-            for (int db = 0; db < DB; ++db) acc[db] = mma(column_frag(v_tile, LD, k, db, lane), w, acc[db]);
+            for (int db = 0; db < DB; ++db) acc[db] = mma(column_frag<T, DP>(v_tile, k, db, lane), w, acc[db]);
         }
-        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_s_waitcnt(0xc07f);          // lgkmcnt(0): nothing of this tile is still to be read
+        settle();
+        if (kStages == 1 && tile + kWaves < end) fetch(tile + kWaves, 0);
+        stage = (stage + 1) % kStages;
     }
     // join the waves: statistics through LDS, then the products, 32 channels at a time, in the tiles' place
     const float2 two = both_halves(run.sum);
@@ -455,7 +540,7 @@ template <class T, int DP> __global__ __launch_bounds__((kStepWaves<T, DP> * kWa
     for (int w = 0; w < kWaves; ++w) sum += sums[w][col] * weight(tops[w][col]);
     const float share = sum == 0.0f ? 0.0f : weight(run.top) / sum;
     const float lse2 = sum == 0.0f ? -INFINITY : top + __builtin_amdgcn_logf(sum);
-    float *join = (float *)&tiles[0][0][0];                        // [wave][32 heads][36]
+    float *join = (float *)&tiles[0][0][0][0];                     // [wave][32 heads][36]
     static_assert(sizeof(tiles) >= sizeof(float) * kWaves * 32 * 36, "room for the join");
     const int64_t n = p.rows * p.heads_q, out_row = row * p.heads_q + head0;
 #pragma unroll
@@ -516,15 +601,15 @@ template <class T> __global__ __launch_bounds__(kBlock) void attend_join_kernel(
 }
 
 // Whether a lane keeps its own rows' operands in registers, or takes them from memory (the L2 cache) for every tile:
-// 16 KiB of two operands a wave are what the accumulators leave room for.
+// the accumulators leave room for 16 KiB of one operand a wave at most.
 template <class T, int DP> constexpr bool kHoldQuery = DP * sizeof(T) <= 512;
 template <class T, int DP> constexpr bool kHoldState = DP * sizeof(T) <= 256;
 
 // dq of 128 rows M over a part of what they see; delta and the rows' bounds for the other kernel on the way.
-template <class T, int DP> __global__ __launch_bounds__(kBlock) void attend_dq_kernel(Attend p) {
-    constexpr int NK = kTileKeys<T>, NB = NK / 32, DB = DP / 32, DS = DP / 16, LD = kLd<T, DP>;
+template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock, DP * sizeof(T) <= 256 ? 2 : 1) void attend_dq_kernel(Attend p) {
+    constexpr int NK = kTileRows<T, DP>, NB = NK / 32, DB = DP / 32, DS = DP / 16;
     constexpr bool kHold = kHoldQuery<T, DP>;
-    __shared__ __attribute__((aligned(16))) T k_tile[NK * LD], v_tile[NK * LD];
+    __shared__ __attribute__((aligned(16))) T k_tiles[2][NK * DP], v_tiles[2][NK * DP];
     __shared__ Bounds slots[kWaves];
     __shared__ int bad[2];                           // by turns: the one of the next tile is cleared where all are done with the last
     const int tid = (int)threadIdx.x, lane = tid % kWave, wave = tid / kWave, half = lane / 32, col = lane % 32;
@@ -566,28 +651,26 @@ template <class T, int DP> __global__ __launch_bounds__(kBlock) void attend_dq_k
     Acc acc[DB] = {};
     const int tiles = any.end > any.first ? (any.end - any.first + NK - 1) / NK : 0;
     const int begin = (int)((int64_t)tiles * split / p.splits), end = (int)((int64_t)tiles * (split + 1) / p.splits);
-    Stage<T, DP, NK, kBlock> ks, vs;
-    auto fetch_k = [&](int tile) {
-        const int key0 = any.first + tile * NK;
-        ks.fetch(tid, p.dim, [&](int r) { return key0 + r < any.end ? address<const T>(p.k, key0 + r, state_head) : nullptr; });
+    Loader<T, DP, NK, kBlock, EXACT> ks, vs;
+    ks.plan(p.k.row_stride, p.dim, tid);
+    vs.plan(p.v.row_stride, p.dim, tid);
+    auto fetch = [&](int tile) {
+        const int key0 = any.first + tile * NK, stage = tile & 1;
+        ks.fetch(k_tiles[stage], address<const T>(p.k, key0, state_head), p.k.row_stride, any.end - key0, p.dim, tid);
+        vs.fetch(v_tiles[stage], address<const T>(p.v, key0, state_head), p.v.row_stride, any.end - key0, p.dim, tid);
     };
-    auto fetch_v = [&](int tile) {
-        const int key0 = any.first + tile * NK;
-        vs.fetch(tid, p.dim, [&](int r) { return key0 + r < any.end ? address<const T>(p.v, key0 + r, state_head) : nullptr; });
-    };
-    if (kAhead<T, DP> && begin < end) fetch_k(begin), fetch_v(begin);
+    if (begin < end) fetch(begin);
     for (int tile = begin; tile < end; ++tile) {
-        const int key0 = any.first + tile * NK;
-        const bool look = !any.covers(key0, key0 + NK);
-        const int turn = (tile - begin) % 2;
+        const int key0 = any.first + tile * NK, stage = tile & 1;
+        const T *k_tile = k_tiles[stage], *v_tile = v_tiles[stage];
+        arrived();
         __syncthreads();
-        if (tid == 0) bad[turn ^ 1] = 0;
-        if constexpr (!kAhead<T, DP>) fetch_k(tile);
-        if (ks.commit(k_tile, tid, look)) bad[turn] = 1;
-        if constexpr (!kAhead<T, DP>) fetch_v(tile);
-        vs.commit(v_tile, tid, false);
-        __syncthreads();
-        if (kAhead<T, DP> && tile + 1 < end) fetch_k(tile + 1), fetch_v(tile + 1);
+        if (tile + 1 < end) fetch(tile + 1);
+        if (tid == 0) bad[stage ^ 1] = 0;
+        if (!any.covers(key0, key0 + NK)) {
+            if (not_finite<T, DP, NK>(k_tile, tid)) bad[stage] = 1;
+            __syncthreads();
+        }
         if (!own.meets(key0, key0 + NK)) continue;
         const bool whole = own.covers(key0, key0 + NK);
 #pragma unroll
@@ -595,23 +678,23 @@ template <class T, int DP> __global__ __launch_bounds__(kBlock) void attend_dq_k
             Acc s = {}, dp = {};
 #pragma unroll
             for (int d = 0; d < DS; ++d) {
-                s = mma(row_frag(k_tile, LD, 32 * b + col, d, half), kHold ? q[kHold ? d : 0] : frag(q_at, d), s);
-                dp = mma(row_frag(v_tile, LD, 32 * b + col, d, half), kHold ? dout[kHold ? d : 0] : frag(do_at, d), dp);
+                s = mma(row_frag<T, DP>(k_tile, 32 * b + col, d, half), kHold ? q[kHold ? d : 0] : frag(q_at, d), s);
+                dp = mma(row_frag<T, DP>(v_tile, 32 * b + col, d, half), kHold ? dout[kHold ? d : 0] : frag(do_at, d), dp);
             }
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const float w = __builtin_amdgcn_exp2f(s[i] * p.scale2 - lse2) * (dp[i] - delta);
                 s[i] = whole || see.has(key0 + 32 * b + result_row(i, half)) ? w : 0.0f;
             }
-            if (!whole && bad[turn]) {
-                careful_product<T, DB>(acc, s, k_tile + 32 * b * LD, LD, half, [&](int j) { return see.has(key0 + 32 * b + j); });
+            if (!whole && bad[stage]) {
+                careful_product<T, DP, DB>(acc, s, k_tile, 32 * b, half, [&](int j) { return see.has(key0 + 32 * b + j); });
                 continue;
             }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
                 const Frag<T> w = result_frag<T>(s, k);
 #pragma unroll
-                for (int db = 0; db < DB; ++db) acc[db] = mma(column_frag(k_tile, LD, 2 * b + k, db, lane), w, acc[db]);
+                for (int db = 0; db < DB; ++db) acc[db] = mma(column_frag<T, DP>(k_tile, 2 * b + k, db, lane), w, acc[db]);
             }
         }
     }
@@ -625,12 +708,12 @@ template <class T, int DP> __global__ __launch_bounds__(kBlock) void attend_dq_k
 
 // dk and dv of 128 states over a part of the rows that see them: the same products with the roles exchanged, 32 rows M
 // in LDS at a time, lanes that hold the states.
-template <class T, int DP> __global__ __launch_bounds__(kBlock) void attend_dkv_kernel(Attend p) {
-    constexpr int DB = DP / 32, DS = DP / 16, LD = kLd<T, DP>, NM = 32;
+template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock, DP * sizeof(T) <= 256 ? 2 : 1) void attend_dkv_kernel(Attend p) {
+    constexpr int NM = kTileRows<T, DP>, NB = NM / 32, DB = DP / 32, DS = DP / 16;
     constexpr bool kHold = kHoldState<T, DP>;
-    __shared__ __attribute__((aligned(16))) T q_tile[NM * LD], do_tile[NM * LD];
-    __shared__ __attribute__((aligned(16))) float lse_of[NM], delta_of[NM];
-    __shared__ Range range_at[NM];
+    __shared__ __attribute__((aligned(16))) T q_tiles[2][NM * DP], do_tiles[2][NM * DP];
+    __shared__ __attribute__((aligned(16))) float lse_of[2][NM], delta_of[2][NM];
+    __shared__ Range range_at[2][NM];
     __shared__ int bad[2], first_tile, last_tile;
     const int tid = (int)threadIdx.x, lane = tid % kWave, wave = tid / kWave, half = lane / 32, col = lane % 32;
     const int state_head = (int)blockIdx.y, split = (int)blockIdx.z;
@@ -650,8 +733,18 @@ template <class T, int DP> __global__ __launch_bounds__(kBlock) void attend_dkv_
             v[s] = frag(v_at, s);
         }
     Acc dk[DB] = {}, dv[DB] = {};
-    // the first and last 32 rows that see any of the block's states
+    // the first and last tile of rows M that see any of the block's states
     const int m_tiles = (p.m_total + NM - 1) / NM;
+    auto bounds_at = [&](int t) {
+        int4 b = p.bounds[t * NB];
+        if (NB > 1 && (t * NB + 1) * 32 < p.m_total) {
+            const int4 o = p.bounds[t * NB + 1];
+            b = make_int4(min(b.x, o.x), max(b.y, o.y), max(b.z, o.z), min(b.w, o.w));
+        } else if (NB > 1) {
+            b.z = INT_MAX, b.w = INT_MIN;                // rows that are not there see nothing
+        }
+        return b;
+    };
     if (tid == 0) {
         first_tile = INT_MAX;
         last_tile = -1;
@@ -660,7 +753,7 @@ template <class T, int DP> __global__ __launch_bounds__(kBlock) void attend_dkv_
     __syncthreads();
     int first = INT_MAX, last = -1;
     for (int t = tid; t < m_tiles; t += kBlock) {
-        const int4 b = p.bounds[t];
+        const int4 b = bounds_at(t);
         if (block0 < b.y && block_end > b.x) {
             first = min(first, t);
             last = max(last, t);
@@ -671,88 +764,91 @@ template <class T, int DP> __global__ __launch_bounds__(kBlock) void attend_dkv_
         atomicMax(&last_tile, last);
     }
     __syncthreads();
-    first = first_tile;
-    const int count = last_tile >= 0 ? last_tile + 1 - first : 0;
-    const int begin = first + (int)((int64_t)count * split / p.splits), end = first + (int)((int64_t)count * (split + 1) / p.splits);
-    Stage<T, DP, NM, kBlock> qs, dos;
-    float next_lse = 0.0f, next_delta = 0.0f;
-    Range next_range{0, 0};
-    auto next_of = [&](int t) {                          // the next 32 rows with something to add
+    first = __builtin_amdgcn_readfirstlane(first_tile);
+    last = __builtin_amdgcn_readfirstlane(last_tile);
+    const int count = last >= 0 ? last + 1 - first : 0;
+    const int begin = last >= 0 ? first + (int)((int64_t)count * split / p.splits) : 0, end = last >= 0 ? first + (int)((int64_t)count * (split + 1) / p.splits) : 0;
+    auto next_of = [&](int t) {                          // the next tile with something to add
         for (; t < end; ++t) {
-            const int4 b = p.bounds[t];
+            const int4 b = bounds_at(t);
             if (block0 < b.y && block_end > b.x) break;
         }
         return t;
     };
-    auto fetch = [&](int t) {
-        const auto row_at = [&](const hp_heads_t &x, int r) {
-            const Place at = place_of(p, t * NM + r, state_head);
-            return at.valid ? address<const T>(x, at.row, at.head) : nullptr;
-        };
-        qs.fetch(tid, p.dim, [&](int r) { return row_at(p.q, r); });
-        dos.fetch(tid, p.dim, [&](int r) { return row_at(p.dout, r); });
+    typedef Loader<T, DP, NM, kBlock, EXACT> Load;
+    auto fetch = [&](int t, int stage) {
+        Load::fetch_m(q_tiles[stage], p.q, t * NM, p.m_total, p.by_group, state_head * p.group, p.dim, tid);
+        Load::fetch_m(do_tiles[stage], p.dout, t * NM, p.m_total, p.by_group, state_head * p.group, p.dim, tid);
         if (tid < NM) {
             const Place at = place_of(p, t * NM + tid, state_head);
             const int64_t out_row = (int64_t)at.row * p.heads_q + at.head;
-            next_lse = p.lse[out_row] * kLog2e;
-            next_delta = p.delta[out_row];
-            next_range = at.valid ? range_of(p, at.row) : Range{0, 0};
+            lse_of[stage][tid] = p.lse[out_row] * kLog2e;
+            delta_of[stage][tid] = p.delta[out_row];
+            range_at[stage][tid] = at.valid ? range_of(p, at.row) : Range{0, 0};
         }
     };
-    int tile = count ? next_of(begin) : end, turn = 0;
-    if (kAhead<T, DP> && count && tile < end) fetch(tile);
-    while (count && tile < end) {
-        const int4 b = p.bounds[tile];
+    int tile = next_of(begin), stage = 0;
+    if (tile < end) fetch(tile, 0);
+    while (tile < end) {
+        const int4 b = bounds_at(tile);
+        const T *q_tile = q_tiles[stage], *do_tile = do_tiles[stage];
         const bool whole = key0 >= b.z && key0 + 32 <= b.w, meets = key0 < b.y && key0 + 32 > b.x;
-        const bool look = !(block0 >= b.z && block0 + 32 * kWaves <= b.w);
-        __syncthreads();
-        if (tid == 0) bad[turn ^ 1] = 0;
-        if constexpr (!kAhead<T, DP>) fetch(tile);
-        const bool one = qs.commit(q_tile, tid, look), other = dos.commit(do_tile, tid, look);
-        if (one || other) bad[turn] = 1;
-        if (tid < NM) {
-            lse_of[tid] = next_lse;
-            delta_of[tid] = next_delta;
-            range_at[tid] = next_range;
-        }
+        arrived();
         __syncthreads();
         const int next = next_of(tile + 1);
-        if (kAhead<T, DP> && next < end) fetch(next);
+        if (next < end) fetch(next, stage ^ 1);
         tile = next;
-        const int now = turn;
-        turn ^= 1;
+        if (tid == 0) bad[stage ^ 1] = 0;
+        if (!(block0 >= b.z && block0 + 32 * kWaves <= b.w)) {
+            const bool one = not_finite<T, DP, NM>(q_tile, tid), other = not_finite<T, DP, NM>(do_tile, tid);
+            if (one || other) bad[stage] = 1;
+            __syncthreads();
+        }
+        const int now = stage;
+        stage ^= 1;
         if (!meets) continue;
-        Acc s = {}, dp = {};
+        const bool careful = !whole && bad[now];
 #pragma unroll
-        for (int d = 0; d < DS; ++d) {
-            s = mma(row_frag(q_tile, LD, col, d, half), kHold ? k[kHold ? d : 0] : frag(k_at, d), s);
-            dp = mma(row_frag(do_tile, LD, col, d, half), kHold ? v[kHold ? d : 0] : frag(v_at, d), dp);
-        }
+        for (int mb = 0; mb < NB; ++mb) {
+            Acc s = {}, dp = {};
 #pragma unroll
-        for (int b4 = 0; b4 < 4; ++b4) {
-            const Vec<float, 4> lse2 = *(const Vec<float, 4> *)&lse_of[8 * b4 + 4 * half], delta = *(const Vec<float, 4> *)&delta_of[8 * b4 + 4 * half];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const int i = 4 * b4 + t;
-                const bool sees = whole || range_at[result_row(i, half)].has(key);
-                const float w = __builtin_amdgcn_exp2f(s[i] * p.scale2 - lse2[t]);
-                s[i] = sees ? w : 0.0f;
-                dp[i] = sees ? w * (dp[i] - delta[t]) : 0.0f;
+            for (int d = 0; d < DS; ++d) {
+                s = mma(row_frag<T, DP>(q_tile, 32 * mb + col, d, half), kHold ? k[kHold ? d : 0] : frag(k_at, d), s);
+                dp = mma(row_frag<T, DP>(do_tile, 32 * mb + col, d, half), kHold ? v[kHold ? d : 0] : frag(v_at, d), dp);
             }
-        }
-        if (!whole && bad[now]) {
-            const auto seen = [&](int j) { return range_at[j].has(key); };
-            careful_product<T, DB>(dv, s, do_tile, LD, half, seen);
-            careful_product<T, DB>(dk, dp, q_tile, LD, half, seen);
-            continue;
-        }
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
-            const Frag<T> w = result_frag<T>(s, m), g = result_frag<T>(dp, m);
+            for (int b4 = 0; b4 < 4; ++b4) {
+                const int r = 32 * mb + 8 * b4 + 4 * half;
+                const Vec<float, 4> lse2 = *(const Vec<float, 4> *)&lse_of[now][r], delta = *(const Vec<float, 4> *)&delta_of[now][r];
 #pragma unroll
-            for (int db = 0; db < DB; ++db) {
-                dv[db] = mma(column_frag(do_tile, LD, m, db, lane), w, dv[db]);
-                dk[db] = mma(column_frag(q_tile, LD, m, db, lane), g, dk[db]);
+                for (int t = 0; t < 4; ++t) {
+                    const int i = 4 * b4 + t;
+                    const float w = __builtin_amdgcn_exp2f(s[i] * p.scale2 - lse2[t]);
+                    s[i] = w;
+                    dp[i] = w * (dp[i] - delta[t]);
+                }
+            }
+            if (!whole)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const bool sees = range_at[now][32 * mb + result_row(i, half)].has(key);
+                    s[i] = sees ? s[i] : 0.0f;
+                    dp[i] = sees ? dp[i] : 0.0f;
+                }
+            if (careful) {
+                const auto seen = [&](int j) { return range_at[now][32 * mb + j].has(key); };
+                careful_product<T, DP, DB>(dv, s, do_tile, 32 * mb, half, seen);
+                careful_product<T, DP, DB>(dk, dp, q_tile, 32 * mb, half, seen);
+                continue;
+            }
+#pragma unroll
+            for (int m = 0; m < 2; ++m) {
+                const Frag<T> w = result_frag<T>(s, m), g = result_frag<T>(dp, m);
+#pragma unroll
+                for (int db = 0; db < DB; ++db) {
+                    dv[db] = mma(column_frag<T, DP>(do_tile, 2 * mb + m, db, lane), w, dv[db]);
+                    dk[db] = mma(column_frag<T, DP>(q_tile, 2 * mb + m, db, lane), g, dk[db]);
+                }
             }
         }
     }
@@ -859,11 +955,20 @@ int check(const hp_attend_args_t *a, int call) {
     return HP_OK;
 }
 
+// n / by = (n * factor) >> (32 + shift) for n < 2^31: factor = ceil(2^(32 + shift) / by) with 2^shift < by <= 2^(shift + 1)
+// is off by less than by / 2^(32 + shift) of itself, which n times stays below 1 / by.
+Divisor divisor(uint32_t by) {
+    uint32_t shift = 0;
+    while (((uint64_t)2 << shift) < by) ++shift;
+    return Divisor{by, (uint32_t)((((uint64_t)1 << (32 + shift)) + by - 1) / by), shift};
+}
+
 Attend params_of(const hp_attend_args_t &a) {
     Attend p{};
     p.rows = a.rows, p.keys = a.keys;
     p.heads_q = a.heads_q, p.heads_k = a.heads_k, p.group = a.heads_q / a.heads_k, p.dim = a.dim;
     p.splits = 1, p.m_total = (int32_t)(a.rows * p.group);
+    p.by_group = divisor((uint32_t)p.group);
     p.scale = a.scale, p.scale2 = a.scale * kLog2e;
     p.q = a.q, p.k = a.k, p.v = a.v, p.out = a.out, p.dout = a.dout, p.dq = a.dq, p.dk = a.dk, p.dv = a.dv;
     p.ranges = a.ranges, p.lse = a.lse;
@@ -874,11 +979,27 @@ bool failed() { return hip_failed(hipGetLastError()); }
 
 enum Kernel { kForward, kStep, kDq, kDkv };
 
+// Whether a tensor's rows are whole aligned 16-byte pieces, and a tile of 64 of them (each with its heads) lies within
+// the reach of a buffer's 32-bit offsets.
+bool exact(const hp_heads_t &t, int size, int32_t dim, int32_t heads) {
+    const int64_t piece = 16 / size;
+    if (dim % piece || misaligned(t.data, 16) || t.row_stride % piece || t.head_stride % piece || t.row_stride < 0 || t.head_stride < 0) return false;
+    const int64_t most = ((int64_t)1 << 30) / size;
+    return t.row_stride <= most / 64 && t.head_stride <= most / heads;
+}
+
+template <class T, int DP, bool EXACT> void launch(Kernel what, const Attend &p, const dim3 &grid, hipStream_t s) {
+    if (what == kForward) attend_forward_kernel<T, DP, EXACT><<<grid, kBlock, 0, s>>>(p);
+    else if (what == kStep) attend_step_kernel<T, DP, EXACT><<<grid, kStepWaves<T, DP> * kWave, 0, s>>>(p);
+    else if (what == kDq) attend_dq_kernel<T, DP, EXACT><<<grid, kBlock, 0, s>>>(p);
+    else attend_dkv_kernel<T, DP, EXACT><<<grid, kBlock, 0, s>>>(p);
+}
+
 template <class T, int DP> void launch(Kernel what, const Attend &p, const dim3 &grid, hipStream_t s) {
-    if (what == kForward) attend_forward_kernel<T, DP><<<grid, kBlock, 0, s>>>(p);
-    else if (what == kStep) attend_step_kernel<T, DP><<<grid, kStepWaves<T, DP> * kWave, 0, s>>>(p);
-    else if (what == kDq) attend_dq_kernel<T, DP><<<grid, kBlock, 0, s>>>(p);
-    else attend_dkv_kernel<T, DP><<<grid, kBlock, 0, s>>>(p);
+    const int size = sizeof(T);
+    const bool whole = what == kDkv ? exact(p.q, size, p.dim, p.group) && exact(p.dout, size, p.dim, p.group) : exact(p.k, size, p.dim, 1) && exact(p.v, size, p.dim, 1);
+    if (whole) launch<T, DP, true>(what, p, grid, s);
+    else launch<T, DP, false>(what, p, grid, s);
 }
 
 template <class T> void launch(Kernel what, const Attend &p, const dim3 &grid, hipStream_t s) {
