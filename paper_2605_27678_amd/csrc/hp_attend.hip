@@ -708,7 +708,7 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock, DP *
 
 // dk and dv of 128 states over a part of the rows that see them: the same products with the roles exchanged, 32 rows M
 // in LDS at a time, lanes that hold the states.
-template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock, DP * sizeof(T) <= 256 ? 2 : 1) void attend_dkv_kernel(Attend p) {
+template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock) void attend_dkv_kernel(Attend p) {
     constexpr int NM = kTileRows<T, DP>, NB = NM / 32, DB = DP / 32, DS = DP / 16;
     constexpr bool kHold = kHoldState<T, DP>;
     __shared__ __attribute__((aligned(16))) T q_tiles[2][NM * DP], do_tiles[2][NM * DP];
@@ -768,44 +768,44 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock, DP *
     last = __builtin_amdgcn_readfirstlane(last_tile);
     const int count = last >= 0 ? last + 1 - first : 0;
     const int begin = last >= 0 ? first + (int)((int64_t)count * split / p.splits) : 0, end = last >= 0 ? first + (int)((int64_t)count * (split + 1) / p.splits) : 0;
-    auto next_of = [&](int t) {                          // the next tile with something to add
-        for (; t < end; ++t) {
-            const int4 b = bounds_at(t);
-            if (block0 < b.y && block_end > b.x) break;
-        }
-        return t;
-    };
     typedef Loader<T, DP, NM, kBlock, EXACT> Load;
+    // A row's numbers are loaded ahead of its tile, and so wait with it, not with the next one: they go to LDS when the
+    // tile's turn comes.
+    float next_lse = 0.0f, next_delta = 0.0f;
+    Range next_range{0, 0};
+    int4 next_b = {};
     auto fetch = [&](int t, int stage) {
-        Load::fetch_m(q_tiles[stage], p.q, t * NM, p.m_total, p.by_group, state_head * p.group, p.dim, tid);
-        Load::fetch_m(do_tiles[stage], p.dout, t * NM, p.m_total, p.by_group, state_head * p.group, p.dim, tid);
+        next_b = bounds_at(t);
         if (tid < NM) {
             const Place at = place_of(p, t * NM + tid, state_head);
             const int64_t out_row = (int64_t)at.row * p.heads_q + at.head;
-            lse_of[stage][tid] = p.lse[out_row] * kLog2e;
-            delta_of[stage][tid] = p.delta[out_row];
-            range_at[stage][tid] = at.valid ? range_of(p, at.row) : Range{0, 0};
+            next_lse = p.lse[out_row] * kLog2e;
+            next_delta = p.delta[out_row];
+            next_range = at.valid ? range_of(p, at.row) : Range{0, 0};
         }
+        Load::fetch_m(q_tiles[stage], p.q, t * NM, p.m_total, p.by_group, state_head * p.group, p.dim, tid);
+        Load::fetch_m(do_tiles[stage], p.dout, t * NM, p.m_total, p.by_group, state_head * p.group, p.dim, tid);
     };
-    int tile = next_of(begin), stage = 0;
-    if (tile < end) fetch(tile, 0);
-    while (tile < end) {
-        const int4 b = bounds_at(tile);
+    if (begin < end) fetch(begin, 0);
+    for (int tile = begin, stage = 0; tile < end; ++tile, stage ^= 1) {
         const T *q_tile = q_tiles[stage], *do_tile = do_tiles[stage];
-        const bool whole = key0 >= b.z && key0 + 32 <= b.w, meets = key0 < b.y && key0 + 32 > b.x;
+        const int now = stage;
         arrived();
+        if (tid < NM) {
+            lse_of[now][tid] = next_lse;
+            delta_of[now][tid] = next_delta;
+            range_at[now][tid] = next_range;
+        }
+        const int4 b = next_b;
+        const bool whole = key0 >= b.z && key0 + 32 <= b.w, meets = key0 < b.y && key0 + 32 > b.x;
         __syncthreads();
-        const int next = next_of(tile + 1);
-        if (next < end) fetch(next, stage ^ 1);
-        tile = next;
+        if (tile + 1 < end) fetch(tile + 1, stage ^ 1);
         if (tid == 0) bad[stage ^ 1] = 0;
         if (!(block0 >= b.z && block0 + 32 * kWaves <= b.w)) {
             const bool one = not_finite<T, DP, NM>(q_tile, tid), other = not_finite<T, DP, NM>(do_tile, tid);
             if (one || other) bad[stage] = 1;
             __syncthreads();
         }
-        const int now = stage;
-        stage ^= 1;
         if (!meets) continue;
         const bool careful = !whole && bad[now];
 #pragma unroll
