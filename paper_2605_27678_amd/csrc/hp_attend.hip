@@ -16,11 +16,12 @@
 // left operand comes from V as it lies in memory, by the transposing LDS load (four keys of one channel in a lane).
 //
 // A row must not feel what it does not see, and 0 * inf is NaN: scores are masked by selection, and where a tile of
-// states that not all rows of a wave see holds an infinity or NaN, its product is made value by value instead
-// (careful_product).
+// states that not all rows of a wave see holds an infinity or NaN, the workgroup begins again and makes the products of
+// such tiles value by value (careful_product).
 #include <cfloat>
 #include <climits>
 #include <cmath>
+#include <type_traits>
 
 #include "hp_device.hpp"
 #include "hp_operators.h"
@@ -38,6 +39,13 @@ constexpr int kStepKeys = 32 * kWaves;              // states that a workgroup o
 
 typedef float Acc __attribute__((ext_vector_type(16)));
 template <class T> using Frag = Vec<T, 8>;
+
+// Behind a pass: whether it met what only a careful one takes right.  That one is code of its own, made from the start
+// again: beside the product in one loop it cost the registers of a second result.
+__device__ __forceinline__ bool again(const int *bad) {
+    __syncthreads();
+    return __builtin_amdgcn_readfirstlane(*bad) != 0;
+}
 
 // Division of numbers below 2^31 by one that a launch keeps.
 struct Divisor {
@@ -153,10 +161,10 @@ __device__ __forceinline__ float2 both_halves(float x) {
 }
 
 // Whether any of the tile's values is an infinity or NaN, as far as this lane looks.
-template <class T, int DP, int ROWS> __device__ __forceinline__ bool not_finite(const T *tile, int tid) {
+template <class T, int DP, int ROWS, int THREADS = kBlock> __device__ __forceinline__ bool not_finite(const T *tile, int tid) {
     typedef uint32_t Piece __attribute__((ext_vector_type(4)));
     bool bad = false;
-    for (int e = tid; e < ROWS * Tile<T, DP>::kPieces; e += kBlock) {
+    for (int e = tid; e < ROWS * Tile<T, DP>::kPieces; e += THREADS) {
         const Piece v = *(const Piece *)(tile + e * Tile<T, DP>::kPiece);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -194,8 +202,10 @@ __device__ __forceinline__ void arrived() { __builtin_amdgcn_s_waitcnt(0x0f70); 
 
 template <class T, int DP, int ROWS, int THREADS, bool EXACT> struct Loader {
     typedef Tile<T, DP> L;
-    static constexpr int kEach = ROWS * L::kPieces / THREADS;
-    static_assert(ROWS * L::kPieces % THREADS == 0, "a tile is the same number of pieces for every lane");
+    static constexpr int kAll = ROWS * L::kPieces, kEach = (kAll + THREADS - 1) / THREADS;
+    static_assert(kAll % kWave == 0, "every wave loads whole or not");
+    // whether the lane's wave has pieces in round n
+    static __device__ __forceinline__ bool loads(int n, int tid) { return (n + 1) * THREADS <= kAll || __builtin_amdgcn_readfirstlane(n * THREADS + tid) < kAll; }
     static __device__ __forceinline__ void piece(T *tile, int n, const T *p, int valid, int tid) {
         *(Vec<T, L::kPiece> *)(tile + (n * THREADS + tid) * L::kPiece) = load<L::kPiece>(p, valid);
     }
@@ -223,10 +233,12 @@ template <class T, int DP, int ROWS, int THREADS, bool EXACT> struct Loader {
         if constexpr (EXACT) {
             const auto from = buffer(first);
 #pragma unroll
-            for (int n = 0; n < kEach; ++n) direct(tile, n, from, (n * THREADS + tid) / L::kPieces < left ? offsets[n] : kOutside, tid);
+            for (int n = 0; n < kEach; ++n)
+                if (loads(n, tid)) direct(tile, n, from, (n * THREADS + tid) / L::kPieces < left ? offsets[n] : kOutside, tid);
         } else {
 #pragma unroll
             for (int n = 0; n < kEach; ++n) {
+                if (!loads(n, tid)) continue;
                 const int e = n * THREADS + tid, row = e / L::kPieces, c = L::piece_of(row, e % L::kPieces);
                 piece(tile, n, first + row * row_stride + c * L::kPiece, row < left ? dim - c * L::kPiece : 0, tid);
             }
@@ -239,6 +251,7 @@ template <class T, int DP, int ROWS, int THREADS, bool EXACT> struct Loader {
         const auto from = buffer(first);
 #pragma unroll
         for (int n = 0; n < kEach; ++n) {
+            if (!loads(n, tid)) continue;
             const int e = n * THREADS + tid, r = e / L::kPieces, c = L::piece_of(r, e % L::kPieces), m = m0 + r;
             const int row = group(m), head = m - row * (int)group.by;
             if constexpr (EXACT) {
@@ -373,14 +386,14 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock, DP *
     constexpr int NK = kTileRows<T, DP>, NB = NK / 32, DB = DP / 32, DS = DP / 16;
     __shared__ __attribute__((aligned(16))) T k_tiles[2][NK * DP], v_tiles[2][NK * DP];
     __shared__ Bounds slots[kWaves];
-    __shared__ int bad[2];                           // by turns: the next tile's is cleared where all are done with the last
+    __shared__ int bad;
     const int tid = (int)threadIdx.x, lane = tid % kWave, wave = tid / kWave, half = lane / 32, col = lane % 32;
     const int state_head = (int)blockIdx.y, split = (int)blockIdx.z;
     // later rows tend to see more: they begin first
     const Place at = place_of(p, ((int)gridDim.x - 1 - (int)blockIdx.x) * kTileM + 32 * wave + col, state_head);
     const Range see = range_of(p, at.row);
     const Bounds own = over_columns(bounds_of(see, at.valid));
-    if (tid < 2) bad[tid] = 0;
+    if (tid == 0) bad = 0;
     const Bounds any = over_waves(own, slots, wave, lane);
     Frag<T> q[DS];
 #pragma unroll
@@ -400,6 +413,7 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock, DP *
         ks.fetch(k_tiles[stage], address<const T>(p.k, key0, state_head), p.k.row_stride, any.end - key0, p.dim, tid);
         vs.fetch(v_tiles[stage], address<const T>(p.v, key0, state_head), p.v.row_stride, any.end - key0, p.dim, tid);
     };
+    const auto pass = [&](auto careful) {
     if (begin < end) fetch(begin);
     for (int tile = begin; tile < end; ++tile) {
         const int key0 = any.first + tile * NK, stage = tile & 1;
@@ -407,11 +421,7 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock, DP *
         arrived();
         __syncthreads();                             // this tile is there, and the last one's readers are done
         if (tile + 1 < end) fetch(tile + 1);
-        if (tid == 0) bad[stage ^ 1] = 0;
-        if (!any.covers(key0, key0 + NK)) {
-            if (not_finite<T, DP, NK>(v_tile, tid)) bad[stage] = 1;
-            __syncthreads();
-        }
+        if (!careful && !any.covers(key0, key0 + NK) && not_finite<T, DP, NK>(v_tile, tid)) bad = 1;
         if (!own.meets(key0, key0 + NK)) continue;
         Acc s[NB];
 #pragma unroll
@@ -428,7 +438,7 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock, DP *
                 for (int i = 0; i < 16; ++i)
                     s[b][i] = see.has(key0 + 32 * b + result_row(i, half)) ? s[b][i] : -INFINITY;
         soften(run, s, acc, p.scale2);
-        if (!whole && bad[stage]) {
+        if (careful && !whole) {
 #pragma unroll
             for (int b = 0; b < NB; ++b)
                 careful_product<T, DP, DB>(acc, s[b], v_tile, 32 * b, half, [&](int j) { return see.has(key0 + 32 * b + j); });
@@ -440,6 +450,14 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock, DP *
 #pragma unroll
             for (int db = 0; db < DB; ++db) acc[db] = mma(column_frag<T, DP>(v_tile, k, db, lane), w, acc[db]);
         }
+    }
+    };
+    pass(std::false_type());
+    if (again(&bad)) {
+        run = Running();
+#pragma unroll
+        for (int db = 0; db < DB; ++db) acc[db] = Acc{};
+        pass(std::true_type());
     }
     const float2 two = both_halves(run.sum);
     const float sum = two.x + two.y;
@@ -611,14 +629,14 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock, DP *
     constexpr bool kHold = kHoldQuery<T, DP>;
     __shared__ __attribute__((aligned(16))) T k_tiles[2][NK * DP], v_tiles[2][NK * DP];
     __shared__ Bounds slots[kWaves];
-    __shared__ int bad[2];                           // by turns: the one of the next tile is cleared where all are done with the last
+    __shared__ int bad;
     const int tid = (int)threadIdx.x, lane = tid % kWave, wave = tid / kWave, half = lane / 32, col = lane % 32;
     const int state_head = (int)blockIdx.y, split = (int)blockIdx.z;
     const int tile_m = (int)gridDim.x - 1 - (int)blockIdx.x;
     const Place at = place_of(p, tile_m * kTileM + 32 * wave + col, state_head);
     const Range see = range_of(p, at.row);
     const Bounds own = over_columns(bounds_of(see, at.valid));
-    if (tid < 2) bad[tid] = 0;
+    if (tid == 0) bad = 0;
     const Bounds any = over_waves(own, slots, wave, lane);
     const T *q_at = address<const T>(p.q, at.row, at.head), *do_at = address<const T>(p.dout, at.row, at.head);
     auto frag = [&](const T *from, int s) {
@@ -659,6 +677,7 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock, DP *
         ks.fetch(k_tiles[stage], address<const T>(p.k, key0, state_head), p.k.row_stride, any.end - key0, p.dim, tid);
         vs.fetch(v_tiles[stage], address<const T>(p.v, key0, state_head), p.v.row_stride, any.end - key0, p.dim, tid);
     };
+    const auto pass = [&](auto careful) {
     if (begin < end) fetch(begin);
     for (int tile = begin; tile < end; ++tile) {
         const int key0 = any.first + tile * NK, stage = tile & 1;
@@ -666,11 +685,7 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock, DP *
         arrived();
         __syncthreads();
         if (tile + 1 < end) fetch(tile + 1);
-        if (tid == 0) bad[stage ^ 1] = 0;
-        if (!any.covers(key0, key0 + NK)) {
-            if (not_finite<T, DP, NK>(k_tile, tid)) bad[stage] = 1;
-            __syncthreads();
-        }
+        if (!careful && !any.covers(key0, key0 + NK) && not_finite<T, DP, NK>(k_tile, tid)) bad = 1;
         if (!own.meets(key0, key0 + NK)) continue;
         const bool whole = own.covers(key0, key0 + NK);
 #pragma unroll
@@ -686,7 +701,7 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock, DP *
                 const float w = __builtin_amdgcn_exp2f(s[i] * p.scale2 - lse2) * (dp[i] - delta);
                 s[i] = whole || see.has(key0 + 32 * b + result_row(i, half)) ? w : 0.0f;
             }
-            if (!whole && bad[stage]) {
+            if (careful && !whole) {
                 careful_product<T, DP, DB>(acc, s, k_tile, 32 * b, half, [&](int j) { return see.has(key0 + 32 * b + j); });
                 continue;
             }
@@ -698,6 +713,13 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock, DP *
             }
         }
     }
+    };
+    pass(std::false_type());
+    if (again(&bad)) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db) acc[db] = Acc{};
+        pass(std::true_type());
+    }
     if (!at.valid) return;
     if (see.empty())
 #pragma unroll
@@ -706,19 +728,27 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock, DP *
     else store_result(address<T>(p.dq, at.row, at.head), acc, p.scale, p.dim, half);
 }
 
-// dk and dv of 128 states over a part of the rows that see them: the same products with the roles exchanged, 32 rows M
-// in LDS at a time, lanes that hold the states.
-template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock) void attend_dkv_kernel(Attend p) {
-    constexpr int NM = kTileRows<T, DP>, NB = NM / 32, DB = DP / 32, DS = DP / 16;
-    constexpr bool kHold = kHoldState<T, DP>;
+// dk and dv of some states over a part of the rows that see them: the same products with the roles exchanged, rows M in
+// LDS a tile at a time, lanes that hold the states.  In bf16 two waves share 32 states, one for dv and one for dk: each
+// makes the weights for itself (five products instead of four), but holds one result, so that two waves fit a SIMD and
+// one's exponentials and LDS reads run beside the other's products.  Binary32 is bound by its products: four, in one wave.
+template <class T> constexpr bool kPairs = sizeof(T) == 2;
+template <class T, int DP> constexpr int kStateWaves = kPairs<T> && DP > 128 ? 2 : 4;           // that share out a workgroup's states
+template <class T, int DP> constexpr int kStateBlock = 32 * kStateWaves<T, DP>;
+template <class T, int DP> constexpr int kStateThreads = kStateWaves<T, DP> * kWave * (kPairs<T> ? 2 : 1);
+
+template <class T, int DP, bool EXACT> __global__ __launch_bounds__((kStateThreads<T, DP>)) void attend_dkv_kernel(Attend p) {
+    constexpr int NM = kTileRows<T, DP>, NB = NM / 32, DB = DP / 32, DS = DP / 16, kThreads = kStateThreads<T, DP>, kStates = kStateBlock<T, DP>;
+    constexpr bool kHold = kHoldState<T, DP>, kTwo = !kPairs<T>;
     __shared__ __attribute__((aligned(16))) T q_tiles[2][NM * DP], do_tiles[2][NM * DP];
     __shared__ __attribute__((aligned(16))) float lse_of[2][NM], delta_of[2][NM];
     __shared__ Range range_at[2][NM];
-    __shared__ int bad[2], first_tile, last_tile;
-    const int tid = (int)threadIdx.x, lane = tid % kWave, wave = tid / kWave, half = lane / 32, col = lane % 32;
+    __shared__ int bad, first_tile, last_tile;
+    const int tid = (int)threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), half = lane / 32, col = lane % 32;
     const int state_head = (int)blockIdx.y, split = (int)blockIdx.z;
-    const int block0 = (int)blockIdx.x * 32 * kWaves, block_end = min(block0 + 32 * kWaves, (int)p.keys);
-    const int key0 = block0 + 32 * wave, key = key0 + col;
+    const int block0 = (int)blockIdx.x * kStates, block_end = min(block0 + kStates, (int)p.keys);
+    const bool makes_dk = kTwo || wave >= kStateWaves<T, DP>;                // or dv, or both
+    const int key0 = block0 + 32 * (wave % kStateWaves<T, DP>), key = key0 + col;
     const bool valid = key < p.keys;
     const T *k_at = address<const T>(p.k, valid ? key : p.keys - 1, state_head), *v_at = address<const T>(p.v, valid ? key : p.keys - 1, state_head);
     auto frag = [&](const T *from, int s) {
@@ -732,7 +762,7 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock) void
             k[s] = frag(k_at, s);
             v[s] = frag(v_at, s);
         }
-    Acc dk[DB] = {}, dv[DB] = {};
+    Acc acc[DB] = {}, dv[kTwo ? DB : 1] = {};                                // dk or dv; dk and dv
     // the first and last tile of rows M that see any of the block's states
     const int m_tiles = (p.m_total + NM - 1) / NM;
     auto bounds_at = [&](int t) {
@@ -748,11 +778,11 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock) void
     if (tid == 0) {
         first_tile = INT_MAX;
         last_tile = -1;
-        bad[0] = bad[1] = 0;
+        bad = 0;
     }
     __syncthreads();
     int first = INT_MAX, last = -1;
-    for (int t = tid; t < m_tiles; t += kBlock) {
+    for (int t = tid; t < m_tiles; t += kThreads) {
         const int4 b = bounds_at(t);
         if (block0 < b.y && block_end > b.x) {
             first = min(first, t);
@@ -768,66 +798,66 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock) void
     last = __builtin_amdgcn_readfirstlane(last_tile);
     const int count = last >= 0 ? last + 1 - first : 0;
     const int begin = last >= 0 ? first + (int)((int64_t)count * split / p.splits) : 0, end = last >= 0 ? first + (int)((int64_t)count * (split + 1) / p.splits) : 0;
-    typedef Loader<T, DP, NM, kBlock, EXACT> Load;
+    typedef Loader<T, DP, NM, kThreads, EXACT> Load;
     // A row's numbers are loaded ahead of its tile, and so wait with it, not with the next one: they go to LDS when the
     // tile's turn comes.
     float next_lse = 0.0f, next_delta = 0.0f;
-    Range next_range{0, 0};
+    int2 next_range = {};
     int4 next_b = {};
     auto fetch = [&](int t, int stage) {
         next_b = bounds_at(t);
         if (tid < NM) {
             const Place at = place_of(p, t * NM + tid, state_head);
             const int64_t out_row = (int64_t)at.row * p.heads_q + at.head;
-            next_lse = p.lse[out_row] * kLog2e;
+            next_lse = p.lse[out_row];
             next_delta = p.delta[out_row];
-            next_range = at.valid ? range_of(p, at.row) : Range{0, 0};
+            next_range = p.ranges ? *(const int2 *)(p.ranges + 2 * (int64_t)at.row) : make_int2(0, (int)p.keys);
+            if (!at.valid) next_range.y = INT_MIN;
         }
         Load::fetch_m(q_tiles[stage], p.q, t * NM, p.m_total, p.by_group, state_head * p.group, p.dim, tid);
         Load::fetch_m(do_tiles[stage], p.dout, t * NM, p.m_total, p.by_group, state_head * p.group, p.dim, tid);
     };
+    const auto pass = [&](auto careful) {
     if (begin < end) fetch(begin, 0);
     for (int tile = begin, stage = 0; tile < end; ++tile, stage ^= 1) {
         const T *q_tile = q_tiles[stage], *do_tile = do_tiles[stage];
         const int now = stage;
         arrived();
         if (tid < NM) {
-            lse_of[now][tid] = next_lse;
+            lse_of[now][tid] = next_lse * kLog2e;
             delta_of[now][tid] = next_delta;
-            range_at[now][tid] = next_range;
+            range_at[now][tid] = Range{max(next_range.x, 0), min(next_range.y, (int)p.keys)};
         }
         const int4 b = next_b;
         const bool whole = key0 >= b.z && key0 + 32 <= b.w, meets = key0 < b.y && key0 + 32 > b.x;
         __syncthreads();
         if (tile + 1 < end) fetch(tile + 1, stage ^ 1);
-        if (tid == 0) bad[stage ^ 1] = 0;
-        if (!(block0 >= b.z && block0 + 32 * kWaves <= b.w)) {
-            const bool one = not_finite<T, DP, NM>(q_tile, tid), other = not_finite<T, DP, NM>(do_tile, tid);
-            if (one || other) bad[stage] = 1;
-            __syncthreads();
+        if (!careful && !(block0 >= b.z && block0 + kStates <= b.w)) {
+            const bool one = not_finite<T, DP, NM, kThreads>(q_tile, tid), other = not_finite<T, DP, NM, kThreads>(do_tile, tid);
+            if (one || other) bad = 1;
         }
         if (!meets) continue;
-        const bool careful = !whole && bad[now];
 #pragma unroll
         for (int mb = 0; mb < NB; ++mb) {
             Acc s = {}, dp = {};
 #pragma unroll
-            for (int d = 0; d < DS; ++d) {
-                s = mma(row_frag<T, DP>(q_tile, 32 * mb + col, d, half), kHold ? k[kHold ? d : 0] : frag(k_at, d), s);
-                dp = mma(row_frag<T, DP>(do_tile, 32 * mb + col, d, half), kHold ? v[kHold ? d : 0] : frag(v_at, d), dp);
-            }
+            for (int d = 0; d < DS; ++d) s = mma(row_frag<T, DP>(q_tile, 32 * mb + col, d, half), kHold ? k[kHold ? d : 0] : frag(k_at, d), s);
+            if (makes_dk)
+#pragma unroll
+                for (int d = 0; d < DS; ++d) dp = mma(row_frag<T, DP>(do_tile, 32 * mb + col, d, half), kHold ? v[kHold ? d : 0] : frag(v_at, d), dp);
 #pragma unroll
             for (int b4 = 0; b4 < 4; ++b4) {
-                const int r = 32 * mb + 8 * b4 + 4 * half;
-                const Vec<float, 4> lse2 = *(const Vec<float, 4> *)&lse_of[now][r], delta = *(const Vec<float, 4> *)&delta_of[now][r];
+                const Vec<float, 4> lse2 = *(const Vec<float, 4> *)&lse_of[now][32 * mb + 8 * b4 + 4 * half];
 #pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const int i = 4 * b4 + t;
-                    const float w = __builtin_amdgcn_exp2f(s[i] * p.scale2 - lse2[t]);
-                    s[i] = w;
-                    dp[i] = w * (dp[i] - delta[t]);
-                }
+                for (int t = 0; t < 4; ++t) s[4 * b4 + t] = __builtin_amdgcn_exp2f(s[4 * b4 + t] * p.scale2 - lse2[t]);
             }
+            if (makes_dk)
+#pragma unroll
+                for (int b4 = 0; b4 < 4; ++b4) {
+                    const Vec<float, 4> delta = *(const Vec<float, 4> *)&delta_of[now][32 * mb + 8 * b4 + 4 * half];
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) dp[4 * b4 + t] = s[4 * b4 + t] * (dp[4 * b4 + t] - delta[t]);
+                }
             if (!whole)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
@@ -835,31 +865,48 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock) void
                     s[i] = sees ? s[i] : 0.0f;
                     dp[i] = sees ? dp[i] : 0.0f;
                 }
-            if (careful) {
-                const auto seen = [&](int j) { return range_at[now][32 * mb + j].has(key); };
-                careful_product<T, DP, DB>(dv, s, do_tile, 32 * mb, half, seen);
-                careful_product<T, DP, DB>(dk, dp, q_tile, 32 * mb, half, seen);
-                continue;
-            }
-#pragma unroll
-            for (int m = 0; m < 2; ++m) {
-                const Frag<T> w = result_frag<T>(s, m), g = result_frag<T>(dp, m);
-#pragma unroll
-                for (int db = 0; db < DB; ++db) {
-                    dv[db] = mma(column_frag<T, DP>(do_tile, 2 * mb + m, db, lane), w, dv[db]);
-                    dk[db] = mma(column_frag<T, DP>(q_tile, 2 * mb + m, db, lane), g, dk[db]);
+            const auto add = [&](auto &to, const Acc &x, const T *tile) {
+                if (careful && !whole) {
+                    careful_product<T, DP>(to, x, tile, 32 * mb, half, [&](int j) { return range_at[now][32 * mb + j].has(key); });
+                    return;
                 }
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    const Frag<T> w = result_frag<T>(x, m);
+#pragma unroll
+                    for (int db = 0; db < DB; ++db) to[db] = mma(column_frag<T, DP>(tile, 2 * mb + m, db, lane), w, to[db]);
+                }
+            };
+            if constexpr (kTwo) {
+                add(dv, s, do_tile);
+                add(acc, dp, q_tile);
+            } else {
+                add(acc, makes_dk ? dp : s, makes_dk ? q_tile : do_tile);
             }
         }
     }
+    };
+    pass(std::false_type());
+    if (again(&bad)) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db) acc[db] = Acc{};
+        if constexpr (kTwo)
+#pragma unroll
+            for (int db = 0; db < DB; ++db) dv[db] = Acc{};
+        pass(std::true_type());
+    }
     if (!valid) return;
-    if (p.splits > 1) {
-        const int64_t at = ((split * p.keys + key) * p.heads_k + state_head) * p.dim;
-        store_result(p.part_k + at, dk, p.scale, p.dim, half);
-        store_result(p.part_v + at, dv, 1.0f, p.dim, half);
+    const auto leave = [&](const auto &x, const hp_heads_t &to, float *part, float scale) {
+        if (p.splits > 1) store_result(part + ((split * p.keys + key) * p.heads_k + state_head) * p.dim, x, scale, p.dim, half);
+        else store_result(address<T>(to, key, state_head), x, scale, p.dim, half);
+    };
+    if constexpr (kTwo) {
+        leave(acc, p.dk, p.part_k, p.scale);
+        leave(dv, p.dv, p.part_v, 1.0f);
+    } else if (makes_dk) {
+        leave(acc, p.dk, p.part_k, p.scale);
     } else {
-        store_result(address<T>(p.dk, key, state_head), dk, p.scale, p.dim, half);
-        store_result(address<T>(p.dv, key, state_head), dv, 1.0f, p.dim, half);
+        leave(acc, p.dv, p.part_v, 1.0f);
     }
 }
 
@@ -889,7 +936,7 @@ int32_t parts_of(int64_t blocks, int64_t want, int64_t length, int64_t least, in
 }
 
 struct Plan {
-    int64_t blocks_m, blocks_k;                     // of 128 rows M, of 128 states
+    int64_t blocks_m, blocks_k;                     // of 128 rows M, of the states that a workgroup takes
     int32_t splits, splits_dq, splits_dkv, splits_step;
 };
 
@@ -897,7 +944,8 @@ Plan plan_of(const hp_attend_args_t &a) {
     Plan n;
     const int64_t group = a.heads_q / a.heads_k, m = a.rows * group;
     n.blocks_m = (m + kTileM - 1) / kTileM;
-    n.blocks_k = (a.keys + 32 * kWaves - 1) / (32 * kWaves);
+    const int64_t states = a.dtype == HP_F32 || a.dim <= 128 ? 128 : 64;
+    n.blocks_k = (a.keys + states - 1) / states;
     const int64_t one = n.blocks_m * a.heads_k > 0 ? n.blocks_m * a.heads_k : 1, two = n.blocks_k * a.heads_k > 0 ? n.blocks_k * a.heads_k : 1;
     n.splits = parts_of(one, 2 * kComputeUnits, a.keys, 256, 32);
     n.splits_dq = parts_of(one, kComputeUnits, a.keys, 256, 32);
@@ -992,10 +1040,11 @@ template <class T, int DP, bool EXACT> void launch(Kernel what, const Attend &p,
     if (what == kForward) attend_forward_kernel<T, DP, EXACT><<<grid, kBlock, 0, s>>>(p);
     else if (what == kStep) attend_step_kernel<T, DP, EXACT><<<grid, kStepWaves<T, DP> * kWave, 0, s>>>(p);
     else if (what == kDq) attend_dq_kernel<T, DP, EXACT><<<grid, kBlock, 0, s>>>(p);
-    else attend_dkv_kernel<T, DP, EXACT><<<grid, kBlock, 0, s>>>(p);
+    else attend_dkv_kernel<T, DP, EXACT><<<grid, kStateThreads<T, DP>, 0, s>>>(p);
 }
 
 template <class T, int DP> void launch(Kernel what, const Attend &p, const dim3 &grid, hipStream_t s) {
+    static_assert(kStateBlock<T, DP> == (sizeof(T) == 4 || DP <= 128 ? 128 : 64), "as plan_of() counts");
     const int size = sizeof(T);
     const bool whole = what == kDkv ? exact(p.q, size, p.dim, p.group) && exact(p.dout, size, p.dim, p.group) : exact(p.k, size, p.dim, 1) && exact(p.v, size, p.dim, 1);
     if (whole) launch<T, DP, true>(what, p, grid, s);
