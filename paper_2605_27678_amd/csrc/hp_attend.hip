@@ -16,8 +16,9 @@
 // left operand comes from V as it lies in memory, by the transposing LDS load (four keys of one channel in a lane).
 //
 // A row must not feel what it does not see, and 0 * inf is NaN: scores are masked by selection, and where a tile of
-// states that not all rows of a wave see holds an infinity or NaN, the workgroup begins again and makes the products of
-// such tiles value by value (careful_product).
+// states that not all rows of a wave see holds an infinity or NaN, the workgroup begins again in a function of its own,
+// which makes the products of such tiles value by value (careful_product).  Beside the loop that is there for speed, that
+// code cost it registers, and loads from scratch memory wait for the tiles on their way.
 #include <cfloat>
 #include <climits>
 #include <cmath>
@@ -40,17 +41,16 @@ constexpr int kStepKeys = 32 * kWaves;              // states that a workgroup o
 typedef float Acc __attribute__((ext_vector_type(16)));
 template <class T> using Frag = Vec<T, 8>;
 
-// Behind a pass: whether it met what only a careful one takes right.  That one is code of its own, made from the start
-// again: beside the product in one loop it cost the registers of a second result.
+// Whether a pass met what only the careful one takes right.
 __device__ __forceinline__ bool again(const int *bad) {
     __syncthreads();
     return __builtin_amdgcn_readfirstlane(*bad) != 0;
 }
 
-// Division of numbers below 2^31 by one that a launch keeps.
+// Division of numbers below 2^30 by one that a launch keeps.
 struct Divisor {
     uint32_t by, factor, shift;
-    __device__ __forceinline__ int operator()(int n) const { return (int)(by == 1 ? (uint32_t)n : __umulhi((uint32_t)n, factor) >> shift); }
+    __device__ __forceinline__ int operator()(int n) const { return (int)(__umulhi(2u * (uint32_t)n, factor) >> shift); }
 };
 
 struct Attend {
@@ -62,8 +62,9 @@ struct Attend {
     const int32_t *ranges;
     float *lse;
     float *part, *part_lse;                         // [splits][rows * heads_q][dim], [splits][rows * heads_q]
-    float *delta;                                   // [rows * heads_q]
+    float *info;                                    // [4][heads_k][m_lines]: lse2, delta, first and end of what a row M sees
     int4 *bounds;                                   // of each 32 rows M
+    int32_t m_lines, reserved;                      // rows M, filled up to whole workgroups
     float *part_k, *part_v;                         // [splits][keys * heads_k][dim]
 };
 
@@ -380,21 +381,39 @@ template <class T, int DB> __device__ __forceinline__ void store_result(T *to, c
 
 template <class T, int DP> constexpr int kTileRows = DP * sizeof(T) <= 256 ? 64 : 32;
 
-// One workgroup: 128 rows M against a part of what they see.  Two tiles of states in LDS: while one is worked on the next
-// is on its way.
-template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock, DP * sizeof(T) <= 256 ? 2 : 1) void attend_forward_kernel(Attend p) {
+// Tiles in LDS, two in turn: while one is worked on the next is on its way.
+template <class T, int DP, int ROWS> struct Tiles {
+    __attribute__((aligned(16))) T a[2][ROWS * DP];
+    __attribute__((aligned(16))) T b[2][ROWS * DP];
+};
+
+template <class T, int DP> struct QueryLds {
+    Tiles<T, DP, kTileRows<T, DP>> tiles;            // states k and v
+    Bounds slots[kWaves];
+    int bad;
+};
+
+// One after the other, with the stage as a constant: addresses in LDS are then one register and a number.
+template <class Step> __device__ __forceinline__ void in_turn(int begin, int end, const Step &step) {
+    for (int tile = begin; tile < end; tile += 2) {
+        step(tile, std::integral_constant<int, 0>());
+        if (tile + 1 < end) step(tile + 1, std::integral_constant<int, 1>());
+    }
+}
+
+template <class T, int DP> __device__ void forward_careful(const Attend *p, QueryLds<T, DP> *lds);
+
+// One workgroup: 128 rows M against a part of what they see.
+template <class T, int DP, bool EXACT, bool CAREFUL> __device__ __forceinline__ void forward_block(const Attend &p, QueryLds<T, DP> &lds) {
     constexpr int NK = kTileRows<T, DP>, NB = NK / 32, DB = DP / 32, DS = DP / 16;
-    __shared__ __attribute__((aligned(16))) T k_tiles[2][NK * DP], v_tiles[2][NK * DP];
-    __shared__ Bounds slots[kWaves];
-    __shared__ int bad;
     const int tid = (int)threadIdx.x, lane = tid % kWave, wave = tid / kWave, half = lane / 32, col = lane % 32;
     const int state_head = (int)blockIdx.y, split = (int)blockIdx.z;
     // later rows tend to see more: they begin first
     const Place at = place_of(p, ((int)gridDim.x - 1 - (int)blockIdx.x) * kTileM + 32 * wave + col, state_head);
     const Range see = range_of(p, at.row);
     const Bounds own = over_columns(bounds_of(see, at.valid));
-    if (tid == 0) bad = 0;
-    const Bounds any = over_waves(own, slots, wave, lane);
+    if (tid == 0) lds.bad = 0;
+    const Bounds any = over_waves(own, lds.slots, wave, lane);
     Frag<T> q[DS];
 #pragma unroll
     for (int s = 0; s < DS; ++s) {
@@ -408,21 +427,20 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock, DP *
     Loader<T, DP, NK, kBlock, EXACT> ks, vs;
     ks.plan(p.k.row_stride, p.dim, tid);
     vs.plan(p.v.row_stride, p.dim, tid);
-    auto fetch = [&](int tile) {
-        const int key0 = any.first + tile * NK, stage = tile & 1;
-        ks.fetch(k_tiles[stage], address<const T>(p.k, key0, state_head), p.k.row_stride, any.end - key0, p.dim, tid);
-        vs.fetch(v_tiles[stage], address<const T>(p.v, key0, state_head), p.v.row_stride, any.end - key0, p.dim, tid);
+    const auto fetch = [&](int tile, int stage) {
+        const int key0 = any.first + tile * NK;
+        ks.fetch(lds.tiles.a[stage], address<const T>(p.k, key0, state_head), p.k.row_stride, any.end - key0, p.dim, tid);
+        vs.fetch(lds.tiles.b[stage], address<const T>(p.v, key0, state_head), p.v.row_stride, any.end - key0, p.dim, tid);
     };
-    const auto pass = [&](auto careful) {
-    if (begin < end) fetch(begin);
-    for (int tile = begin; tile < end; ++tile) {
-        const int key0 = any.first + tile * NK, stage = tile & 1;
-        const T *k_tile = k_tiles[stage], *v_tile = v_tiles[stage];
+    if (begin < end) fetch(begin, 0);
+    in_turn(begin, end, [&](int tile, auto stage) {
+        const int key0 = any.first + tile * NK;
+        const T *k_tile = lds.tiles.a[stage], *v_tile = lds.tiles.b[stage];
         arrived();
         __syncthreads();                             // this tile is there, and the last one's readers are done
-        if (tile + 1 < end) fetch(tile + 1);
-        if (!careful && !any.covers(key0, key0 + NK) && not_finite<T, DP, NK>(v_tile, tid)) bad = 1;
-        if (!own.meets(key0, key0 + NK)) continue;
+        if (tile + 1 < end) fetch(tile + 1, 1 - stage);
+        if (!CAREFUL && !any.covers(key0, key0 + NK) && not_finite<T, DP, NK>(v_tile, tid)) lds.bad = 1;
+        if (!own.meets(key0, key0 + NK)) return;
         Acc s[NB];
 #pragma unroll
         for (int b = 0; b < NB; ++b) s[b] = Acc{};
@@ -438,11 +456,11 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock, DP *
                 for (int i = 0; i < 16; ++i)
                     s[b][i] = see.has(key0 + 32 * b + result_row(i, half)) ? s[b][i] : -INFINITY;
         soften(run, s, acc, p.scale2);
-        if (careful && !whole) {
+        if (CAREFUL && !whole) {
 #pragma unroll
             for (int b = 0; b < NB; ++b)
                 careful_product<T, DP, DB>(acc, s[b], v_tile, 32 * b, half, [&](int j) { return see.has(key0 + 32 * b + j); });
-            continue;
+            return;
         }
 #pragma unroll
         for (int k = 0; k < 2 * NB; ++k) {
@@ -450,15 +468,9 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock, DP *
 #pragma unroll
             for (int db = 0; db < DB; ++db) acc[db] = mma(column_frag<T, DP>(v_tile, k, db, lane), w, acc[db]);
         }
-    }
-    };
-    pass(std::false_type());
-    if (again(&bad)) {
-        run = Running();
-#pragma unroll
-        for (int db = 0; db < DB; ++db) acc[db] = Acc{};
-        pass(std::true_type());
-    }
+    });
+    if constexpr (!CAREFUL)
+        if (again(&lds.bad)) return forward_careful<T, DP>((const Attend *)__builtin_amdgcn_kernarg_segment_ptr(), &lds);
     const float2 two = both_halves(run.sum);
     const float sum = two.x + two.y;
     const bool none = see.empty() || sum == 0.0f;
@@ -476,6 +488,16 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock, DP *
     }
     store_result(address<T>(p.out, at.row, at.head), acc, inv, p.dim, half);
     if (p.lse && half == 0) p.lse[out_row] = lse2 * kLn2;
+}
+
+template <class T, int DP> __device__ __attribute__((noinline)) void forward_careful(const Attend *at, QueryLds<T, DP> *lds) {
+    const Attend p = *at;
+    forward_block<T, DP, false, true>(p, *lds);
+}
+
+template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock, DP * sizeof(T) <= 256 ? 2 : 1) void attend_forward_kernel(Attend p) {
+    __shared__ QueryLds<T, DP> lds;
+    forward_block<T, DP, EXACT, false>(p, lds);
 }
 
 // One workgroup: up to 32 heads of one row against a part of what the row sees.  The waves take 32 states each on their
@@ -623,23 +645,22 @@ template <class T> __global__ __launch_bounds__(kBlock) void attend_join_kernel(
 template <class T, int DP> constexpr bool kHoldQuery = DP * sizeof(T) <= 512;
 template <class T, int DP> constexpr bool kHoldState = DP * sizeof(T) <= 256;
 
-// dq of 128 rows M over a part of what they see; delta and the rows' bounds for the other kernel on the way.
-template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock, DP * sizeof(T) <= 256 ? 2 : 1) void attend_dq_kernel(Attend p) {
+template <class T, int DP> __device__ void dq_careful(const Attend *p, QueryLds<T, DP> *lds);
+
+// dq of 128 rows M over a part of what they see; on the way, what the other kernel has to know of the rows.
+template <class T, int DP, bool EXACT, bool CAREFUL> __device__ __forceinline__ void dq_block(const Attend &p, QueryLds<T, DP> &lds) {
     constexpr int NK = kTileRows<T, DP>, NB = NK / 32, DB = DP / 32, DS = DP / 16;
     constexpr bool kHold = kHoldQuery<T, DP>;
-    __shared__ __attribute__((aligned(16))) T k_tiles[2][NK * DP], v_tiles[2][NK * DP];
-    __shared__ Bounds slots[kWaves];
-    __shared__ int bad;
     const int tid = (int)threadIdx.x, lane = tid % kWave, wave = tid / kWave, half = lane / 32, col = lane % 32;
     const int state_head = (int)blockIdx.y, split = (int)blockIdx.z;
-    const int tile_m = (int)gridDim.x - 1 - (int)blockIdx.x;
-    const Place at = place_of(p, tile_m * kTileM + 32 * wave + col, state_head);
+    const int tile_m = (int)gridDim.x - 1 - (int)blockIdx.x, line = tile_m * kTileM + 32 * wave + col;
+    const Place at = place_of(p, line, state_head);
     const Range see = range_of(p, at.row);
     const Bounds own = over_columns(bounds_of(see, at.valid));
-    if (tid == 0) bad = 0;
-    const Bounds any = over_waves(own, slots, wave, lane);
+    if (tid == 0) lds.bad = 0;
+    const Bounds any = over_waves(own, lds.slots, wave, lane);
     const T *q_at = address<const T>(p.q, at.row, at.head), *do_at = address<const T>(p.dout, at.row, at.head);
-    auto frag = [&](const T *from, int s) {
+    const auto frag = [&](const T *from, int s) {
         const int d = 16 * s + 8 * half;
         return load<8>(from + d, p.dim - d);
     };
@@ -658,35 +679,41 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock, DP *
     const float2 two = both_halves(delta);
     delta = two.x + two.y;
     const int64_t out_row = (int64_t)at.row * p.heads_q + at.head;
-    if (split == 0) {
-        if (at.valid && half == 0) p.delta[out_row] = delta;
+    const float lse2 = p.lse[out_row] * kLog2e;
+    if (!CAREFUL && split == 0) {
+        if (half == 0) {
+            // rows that are not there see nothing
+            const int64_t each = (int64_t)p.heads_k * p.m_lines, to = (int64_t)state_head * p.m_lines + line;
+            p.info[to] = lse2;
+            p.info[each + to] = delta;
+            ((int *)p.info)[2 * each + to] = at.valid ? see.lo : 0;
+            ((int *)p.info)[3 * each + to] = at.valid ? see.hi : 0;
+        }
         // rows that see nothing, or are not there, keep the states' kernel from taking 32 rows for unmasked
         const bool all = __all(at.valid && !see.empty());
         if (state_head == 0 && lane == 0)
             p.bounds[tile_m * kWaves + wave] = make_int4(own.first, own.end, all ? own.all : INT_MAX, all ? own.all_end : INT_MIN);
     }
-    const float lse2 = p.lse[out_row] * kLog2e;
     Acc acc[DB] = {};
     const int tiles = any.end > any.first ? (any.end - any.first + NK - 1) / NK : 0;
     const int begin = (int)((int64_t)tiles * split / p.splits), end = (int)((int64_t)tiles * (split + 1) / p.splits);
     Loader<T, DP, NK, kBlock, EXACT> ks, vs;
     ks.plan(p.k.row_stride, p.dim, tid);
     vs.plan(p.v.row_stride, p.dim, tid);
-    auto fetch = [&](int tile) {
-        const int key0 = any.first + tile * NK, stage = tile & 1;
-        ks.fetch(k_tiles[stage], address<const T>(p.k, key0, state_head), p.k.row_stride, any.end - key0, p.dim, tid);
-        vs.fetch(v_tiles[stage], address<const T>(p.v, key0, state_head), p.v.row_stride, any.end - key0, p.dim, tid);
+    const auto fetch = [&](int tile, int stage) {
+        const int key0 = any.first + tile * NK;
+        ks.fetch(lds.tiles.a[stage], address<const T>(p.k, key0, state_head), p.k.row_stride, any.end - key0, p.dim, tid);
+        vs.fetch(lds.tiles.b[stage], address<const T>(p.v, key0, state_head), p.v.row_stride, any.end - key0, p.dim, tid);
     };
-    const auto pass = [&](auto careful) {
-    if (begin < end) fetch(begin);
-    for (int tile = begin; tile < end; ++tile) {
-        const int key0 = any.first + tile * NK, stage = tile & 1;
-        const T *k_tile = k_tiles[stage], *v_tile = v_tiles[stage];
+    if (begin < end) fetch(begin, 0);
+    in_turn(begin, end, [&](int tile, auto stage) {
+        const int key0 = any.first + tile * NK;
+        const T *k_tile = lds.tiles.a[stage], *v_tile = lds.tiles.b[stage];
         arrived();
         __syncthreads();
-        if (tile + 1 < end) fetch(tile + 1);
-        if (!careful && !any.covers(key0, key0 + NK) && not_finite<T, DP, NK>(k_tile, tid)) bad = 1;
-        if (!own.meets(key0, key0 + NK)) continue;
+        if (tile + 1 < end) fetch(tile + 1, 1 - stage);
+        if (!CAREFUL && !any.covers(key0, key0 + NK) && not_finite<T, DP, NK>(k_tile, tid)) lds.bad = 1;
+        if (!own.meets(key0, key0 + NK)) return;
         const bool whole = own.covers(key0, key0 + NK);
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
@@ -697,11 +724,11 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock, DP *
                 dp = mma(row_frag<T, DP>(v_tile, 32 * b + col, d, half), kHold ? dout[kHold ? d : 0] : frag(do_at, d), dp);
             }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float w = __builtin_amdgcn_exp2f(s[i] * p.scale2 - lse2) * (dp[i] - delta);
-                s[i] = whole || see.has(key0 + 32 * b + result_row(i, half)) ? w : 0.0f;
-            }
-            if (careful && !whole) {
+            for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] * p.scale2 - lse2) * (dp[i] - delta);
+            if (!whole)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = see.has(key0 + 32 * b + result_row(i, half)) ? s[i] : 0.0f;
+            if (CAREFUL && !whole) {
                 careful_product<T, DP, DB>(acc, s, k_tile, 32 * b, half, [&](int j) { return see.has(key0 + 32 * b + j); });
                 continue;
             }
@@ -712,20 +739,25 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock, DP *
                 for (int db = 0; db < DB; ++db) acc[db] = mma(column_frag<T, DP>(k_tile, 2 * b + k, db, lane), w, acc[db]);
             }
         }
-    }
-    };
-    pass(std::false_type());
-    if (again(&bad)) {
-#pragma unroll
-        for (int db = 0; db < DB; ++db) acc[db] = Acc{};
-        pass(std::true_type());
-    }
+    });
+    if constexpr (!CAREFUL)
+        if (again(&lds.bad)) return dq_careful<T, DP>((const Attend *)__builtin_amdgcn_kernarg_segment_ptr(), &lds);
     if (!at.valid) return;
     if (see.empty())
 #pragma unroll
         for (int db = 0; db < DB; ++db) acc[db] = Acc{};
     if (p.splits > 1) store_result(p.part + (split * p.rows * p.heads_q + out_row) * p.dim, acc, p.scale, p.dim, half);
     else store_result(address<T>(p.dq, at.row, at.head), acc, p.scale, p.dim, half);
+}
+
+template <class T, int DP> __device__ __attribute__((noinline)) void dq_careful(const Attend *at, QueryLds<T, DP> *lds) {
+    const Attend p = *at;
+    dq_block<T, DP, false, true>(p, *lds);
+}
+
+template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock, DP * sizeof(T) <= 256 ? 2 : 1) void attend_dq_kernel(Attend p) {
+    __shared__ QueryLds<T, DP> lds;
+    dq_block<T, DP, EXACT, false>(p, lds);
 }
 
 // dk and dv of some states over a part of the rows that see them: the same products with the roles exchanged, rows M in
@@ -737,13 +769,17 @@ template <class T, int DP> constexpr int kStateWaves = kPairs<T> && DP > 128 ? 2
 template <class T, int DP> constexpr int kStateBlock = 32 * kStateWaves<T, DP>;
 template <class T, int DP> constexpr int kStateThreads = kStateWaves<T, DP> * kWave * (kPairs<T> ? 2 : 1);
 
-template <class T, int DP, bool EXACT> __global__ __launch_bounds__((kStateThreads<T, DP>)) void attend_dkv_kernel(Attend p) {
+template <class T, int DP> struct StateLds {
+    Tiles<T, DP, kTileRows<T, DP>> tiles;            // rows M of q and dout
+    __attribute__((aligned(16))) float info[2][256]; // of the rows: lse2, delta, first, end, one behind the other
+    int bad, first_tile, last_tile;
+};
+
+template <class T, int DP> __device__ void dkv_careful(const Attend *p, StateLds<T, DP> *lds);
+
+template <class T, int DP, bool EXACT, bool CAREFUL> __device__ __forceinline__ void dkv_block(const Attend &p, StateLds<T, DP> &lds) {
     constexpr int NM = kTileRows<T, DP>, NB = NM / 32, DB = DP / 32, DS = DP / 16, kThreads = kStateThreads<T, DP>, kStates = kStateBlock<T, DP>;
     constexpr bool kHold = kHoldState<T, DP>, kTwo = !kPairs<T>;
-    __shared__ __attribute__((aligned(16))) T q_tiles[2][NM * DP], do_tiles[2][NM * DP];
-    __shared__ __attribute__((aligned(16))) float lse_of[2][NM], delta_of[2][NM];
-    __shared__ Range range_at[2][NM];
-    __shared__ int bad, first_tile, last_tile;
     const int tid = (int)threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), half = lane / 32, col = lane % 32;
     const int state_head = (int)blockIdx.y, split = (int)blockIdx.z;
     const int block0 = (int)blockIdx.x * kStates, block_end = min(block0 + kStates, (int)p.keys);
@@ -751,7 +787,7 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__((kStateThrea
     const int key0 = block0 + 32 * (wave % kStateWaves<T, DP>), key = key0 + col;
     const bool valid = key < p.keys;
     const T *k_at = address<const T>(p.k, valid ? key : p.keys - 1, state_head), *v_at = address<const T>(p.v, valid ? key : p.keys - 1, state_head);
-    auto frag = [&](const T *from, int s) {
+    const auto frag = [&](const T *from, int s) {
         const int d = 16 * s + 8 * half;
         return load<8>(from + d, valid ? p.dim - d : 0);
     };
@@ -765,20 +801,24 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__((kStateThrea
     Acc acc[DB] = {}, dv[kTwo ? DB : 1] = {};                                // dk or dv; dk and dv
     // the first and last tile of rows M that see any of the block's states
     const int m_tiles = (p.m_total + NM - 1) / NM;
-    auto bounds_at = [&](int t) {
-        int4 b = p.bounds[t * NB];
+    const auto bounds_at = [&](int t) {
+        // written by the kernel before: as constant memory it is read without a place in the queue of the tiles
+        typedef __attribute__((address_space(4))) const Vec<int, 4> *Constant;
+        const Constant at = (Constant)(uintptr_t)p.bounds;
+        const Vec<int, 4> one = at[t * NB];
+        int4 b = make_int4(one[0], one[1], one[2], one[3]);
         if (NB > 1 && (t * NB + 1) * 32 < p.m_total) {
-            const int4 o = p.bounds[t * NB + 1];
-            b = make_int4(min(b.x, o.x), max(b.y, o.y), max(b.z, o.z), min(b.w, o.w));
+            const Vec<int, 4> two = at[t * NB + 1];
+            b = make_int4(min(b.x, two[0]), max(b.y, two[1]), max(b.z, two[2]), min(b.w, two[3]));
         } else if (NB > 1) {
             b.z = INT_MAX, b.w = INT_MIN;                // rows that are not there see nothing
         }
         return b;
     };
     if (tid == 0) {
-        first_tile = INT_MAX;
-        last_tile = -1;
-        bad = 0;
+        lds.first_tile = INT_MAX;
+        lds.last_tile = -1;
+        lds.bad = 0;
     }
     __syncthreads();
     int first = INT_MAX, last = -1;
@@ -790,53 +830,49 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__((kStateThrea
         }
     }
     if (last >= 0) {
-        atomicMin(&first_tile, first);
-        atomicMax(&last_tile, last);
+        atomicMin(&lds.first_tile, first);
+        atomicMax(&lds.last_tile, last);
     }
     __syncthreads();
-    first = __builtin_amdgcn_readfirstlane(first_tile);
-    last = __builtin_amdgcn_readfirstlane(last_tile);
+    first = __builtin_amdgcn_readfirstlane(lds.first_tile);
+    last = __builtin_amdgcn_readfirstlane(lds.last_tile);
     const int count = last >= 0 ? last + 1 - first : 0;
     const int begin = last >= 0 ? first + (int)((int64_t)count * split / p.splits) : 0, end = last >= 0 ? first + (int)((int64_t)count * (split + 1) / p.splits) : 0;
     typedef Loader<T, DP, NM, kThreads, EXACT> Load;
-    // A row's numbers are loaded ahead of its tile, and so wait with it, not with the next one: they go to LDS when the
-    // tile's turn comes.
-    float next_lse = 0.0f, next_delta = 0.0f;
-    int2 next_range = {};
     int4 next_b = {};
-    auto fetch = [&](int t, int stage) {
+    const auto fetch = [&](int t, int stage) {
         next_b = bounds_at(t);
-        if (tid < NM) {
-            const Place at = place_of(p, t * NM + tid, state_head);
-            const int64_t out_row = (int64_t)at.row * p.heads_q + at.head;
-            next_lse = p.lse[out_row];
-            next_delta = p.delta[out_row];
-            next_range = p.ranges ? *(const int2 *)(p.ranges + 2 * (int64_t)at.row) : make_int2(0, (int)p.keys);
-            if (!at.valid) next_range.y = INT_MIN;
+        if (wave == 0) {                                 // four runs of NM numbers, 16 bytes a lane
+            const int run = lane / (NM / 4), piece = lane % (NM / 4);
+            const uint32_t at = (uint32_t)run * (uint32_t)p.heads_k * (uint32_t)p.m_lines * 4 + piece * 16;
+            const auto from = Load::buffer(p.info + (int64_t)state_head * p.m_lines + (int64_t)t * NM);
+            if constexpr (CAREFUL) {
+                if (run < 4) {
+                    const int64_t far = (int64_t)run * p.heads_k * p.m_lines + (int64_t)state_head * p.m_lines + (int64_t)t * NM + piece * 4;
+                    *(Vec<float, 4> *)&lds.info[stage][4 * lane] = *(const Vec<float, 4> *)(p.info + far);
+                }
+            } else {
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)lds.info[stage], 16, (int)(run < 4 ? at : kOutside), 0, 0, 0);
+            }
         }
-        Load::fetch_m(q_tiles[stage], p.q, t * NM, p.m_total, p.by_group, state_head * p.group, p.dim, tid);
-        Load::fetch_m(do_tiles[stage], p.dout, t * NM, p.m_total, p.by_group, state_head * p.group, p.dim, tid);
+        Load::fetch_m(lds.tiles.a[stage], p.q, t * NM, p.m_total, p.by_group, state_head * p.group, p.dim, tid);
+        Load::fetch_m(lds.tiles.b[stage], p.dout, t * NM, p.m_total, p.by_group, state_head * p.group, p.dim, tid);
     };
-    const auto pass = [&](auto careful) {
     if (begin < end) fetch(begin, 0);
-    for (int tile = begin, stage = 0; tile < end; ++tile, stage ^= 1) {
-        const T *q_tile = q_tiles[stage], *do_tile = do_tiles[stage];
-        const int now = stage;
-        arrived();
-        if (tid < NM) {
-            lse_of[now][tid] = next_lse * kLog2e;
-            delta_of[now][tid] = next_delta;
-            range_at[now][tid] = Range{max(next_range.x, 0), min(next_range.y, (int)p.keys)};
-        }
+    in_turn(begin, end, [&](int tile, auto stage) {
+        const T *q_tile = lds.tiles.a[stage], *do_tile = lds.tiles.b[stage];
+        const float *info = lds.info[stage];
         const int4 b = next_b;
         const bool whole = key0 >= b.z && key0 + 32 <= b.w, meets = key0 < b.y && key0 + 32 > b.x;
+        arrived();
         __syncthreads();
-        if (tile + 1 < end) fetch(tile + 1, stage ^ 1);
-        if (!careful && !(block0 >= b.z && block0 + kStates <= b.w)) {
+        if (tile + 1 < end) fetch(tile + 1, 1 - stage);
+        if (!CAREFUL && !(block0 >= b.z && block0 + kStates <= b.w)) {
             const bool one = not_finite<T, DP, NM, kThreads>(q_tile, tid), other = not_finite<T, DP, NM, kThreads>(do_tile, tid);
-            if (one || other) bad = 1;
+            if (one || other) lds.bad = 1;
         }
-        if (!meets) continue;
+        if (!meets) return;
+        const auto sees = [&](int row) { return key >= ((const int *)info)[2 * NM + row] && key < ((const int *)info)[3 * NM + row]; };
 #pragma unroll
         for (int mb = 0; mb < NB; ++mb) {
             Acc s = {}, dp = {};
@@ -847,27 +883,27 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__((kStateThrea
                 for (int d = 0; d < DS; ++d) dp = mma(row_frag<T, DP>(do_tile, 32 * mb + col, d, half), kHold ? v[kHold ? d : 0] : frag(v_at, d), dp);
 #pragma unroll
             for (int b4 = 0; b4 < 4; ++b4) {
-                const Vec<float, 4> lse2 = *(const Vec<float, 4> *)&lse_of[now][32 * mb + 8 * b4 + 4 * half];
+                const Vec<float, 4> lse2 = *(const Vec<float, 4> *)(info + 32 * mb + 8 * b4 + 4 * half);
 #pragma unroll
                 for (int t = 0; t < 4; ++t) s[4 * b4 + t] = __builtin_amdgcn_exp2f(s[4 * b4 + t] * p.scale2 - lse2[t]);
             }
             if (makes_dk)
 #pragma unroll
                 for (int b4 = 0; b4 < 4; ++b4) {
-                    const Vec<float, 4> delta = *(const Vec<float, 4> *)&delta_of[now][32 * mb + 8 * b4 + 4 * half];
+                    const Vec<float, 4> delta = *(const Vec<float, 4> *)(info + NM + 32 * mb + 8 * b4 + 4 * half);
 #pragma unroll
                     for (int t = 0; t < 4; ++t) dp[4 * b4 + t] = s[4 * b4 + t] * (dp[4 * b4 + t] - delta[t]);
                 }
             if (!whole)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const bool sees = range_at[now][32 * mb + result_row(i, half)].has(key);
-                    s[i] = sees ? s[i] : 0.0f;
-                    dp[i] = sees ? dp[i] : 0.0f;
+                    const bool seen = sees(32 * mb + result_row(i, half));
+                    s[i] = seen ? s[i] : 0.0f;
+                    dp[i] = seen ? dp[i] : 0.0f;
                 }
             const auto add = [&](auto &to, const Acc &x, const T *tile) {
-                if (careful && !whole) {
-                    careful_product<T, DP>(to, x, tile, 32 * mb, half, [&](int j) { return range_at[now][32 * mb + j].has(key); });
+                if (CAREFUL && !whole) {
+                    careful_product<T, DP>(to, x, tile, 32 * mb, half, [&](int j) { return sees(32 * mb + j); });
                     return;
                 }
 #pragma unroll
@@ -880,21 +916,15 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__((kStateThrea
             if constexpr (kTwo) {
                 add(dv, s, do_tile);
                 add(acc, dp, q_tile);
+            } else if (makes_dk) {
+                add(acc, dp, q_tile);
             } else {
-                add(acc, makes_dk ? dp : s, makes_dk ? q_tile : do_tile);
+                add(acc, s, do_tile);
             }
         }
-    }
-    };
-    pass(std::false_type());
-    if (again(&bad)) {
-#pragma unroll
-        for (int db = 0; db < DB; ++db) acc[db] = Acc{};
-        if constexpr (kTwo)
-#pragma unroll
-            for (int db = 0; db < DB; ++db) dv[db] = Acc{};
-        pass(std::true_type());
-    }
+    });
+    if constexpr (!CAREFUL)
+        if (again(&lds.bad)) return dkv_careful<T, DP>((const Attend *)__builtin_amdgcn_kernarg_segment_ptr(), &lds);
     if (!valid) return;
     const auto leave = [&](const auto &x, const hp_heads_t &to, float *part, float scale) {
         if (p.splits > 1) store_result(part + ((split * p.keys + key) * p.heads_k + state_head) * p.dim, x, scale, p.dim, half);
@@ -908,6 +938,16 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__((kStateThrea
     } else {
         leave(acc, p.dv, p.part_v, 1.0f);
     }
+}
+
+template <class T, int DP> __device__ __attribute__((noinline)) void dkv_careful(const Attend *at, StateLds<T, DP> *lds) {
+    const Attend p = *at;
+    dkv_block<T, DP, false, true>(p, *lds);
+}
+
+template <class T, int DP, bool EXACT> __global__ __launch_bounds__((kStateThreads<T, DP>)) void attend_dkv_kernel(Attend p) {
+    __shared__ StateLds<T, DP> lds;
+    dkv_block<T, DP, EXACT, false>(p, lds);
 }
 
 // Adds parts [splits][rows * heads][dim] up, in order: a wave a row and head.
@@ -957,12 +997,14 @@ Plan plan_of(const hp_attend_args_t &a) {
 
 int64_t align16(int64_t n) { return (n + 15) / 16 * 16; }
 
+int64_t info_bytes(const hp_attend_args_t &a, const Plan &n) { return 16 * a.heads_k * n.blocks_m * kTileM; }
+
 int64_t workspace_of(const hp_attend_args_t &a, int call) {
     const Plan n = plan_of(a);
     const int64_t outs = a.rows * a.heads_q, states = a.keys * a.heads_k;
     if (call == HP_ATTEND_BACKWARD) {
         const int64_t parts = 4 * a.dim * (n.splits_dq > 1 ? n.splits_dq * outs : 0), parts_kv = 4 * a.dim * (n.splits_dkv > 1 ? 2 * n.splits_dkv * states : 0);
-        return align16(4 * outs) + align16(16 * n.blocks_m * kWaves) + (parts > parts_kv ? parts : parts_kv);
+        return info_bytes(a, n) + align16(16 * n.blocks_m * kWaves) + (parts > parts_kv ? parts : parts_kv);
     }
     const int32_t splits = call == HP_ATTEND_STEP ? n.splits_step : n.splits;
     return splits > 1 ? align16(4 * splits * outs) + 4 * splits * outs * a.dim : 0;
@@ -977,7 +1019,7 @@ int check_sizes(const hp_attend_args_t *a) {
     if (a->heads_q % a->heads_k || a->heads_q > 16384) return HP_ELAYOUT;
     if (a->rows < 0 || a->keys < 0) return HP_EINVAL;
     // rows M, states and lanes of a launch are counted in 32 bits, with tiles to spare
-    if (a->rows > (1 << 30) / (a->heads_q / a->heads_k) || a->keys > INT_MAX - 1024) return HP_ELAYOUT;
+    if (a->rows > ((1 << 30) - 1024) / (a->heads_q / a->heads_k) || a->keys > INT_MAX - 1024) return HP_ELAYOUT;
     return HP_OK;
 }
 
@@ -1003,12 +1045,12 @@ int check(const hp_attend_args_t *a, int call) {
     return HP_OK;
 }
 
-// n / by = (n * factor) >> (32 + shift) for n < 2^31: factor = ceil(2^(32 + shift) / by) with 2^shift < by <= 2^(shift + 1)
-// is off by less than by / 2^(32 + shift) of itself, which n times stays below 1 / by.
+// n / by = (2n * factor) >> (32 + shift) for n < 2^30, with factor = ceil(2^(31 + shift) / by) and 2^shift the least power of
+// two that is not below by / 2: what the ceiling adds to the quotient is less than n / 2^(31 + shift) <= 1 / by.
 Divisor divisor(uint32_t by) {
     uint32_t shift = 0;
     while (((uint64_t)2 << shift) < by) ++shift;
-    return Divisor{by, (uint32_t)((((uint64_t)1 << (32 + shift)) + by - 1) / by), shift};
+    return Divisor{by, (uint32_t)((((uint64_t)1 << (31 + shift)) + by - 1) / by), shift};
 }
 
 Attend params_of(const hp_attend_args_t &a) {
@@ -1121,9 +1163,10 @@ int hp_cross_attend_backward(const hp_attend_args_t *a, void *stream) {
     const hipStream_t s = (hipStream_t)stream;
     Attend p = params_of(*a);
     char *ws = (char *)a->workspace;
-    p.delta = (float *)ws;
-    p.bounds = (int4 *)(ws + align16(4 * a->rows * a->heads_q));
-    float *parts = (float *)(ws + align16(4 * a->rows * a->heads_q) + align16(16 * n.blocks_m * kWaves));
+    p.info = (float *)ws;
+    p.m_lines = (int32_t)(n.blocks_m * kTileM);
+    p.bounds = (int4 *)(ws + info_bytes(*a, n));
+    float *parts = (float *)(ws + info_bytes(*a, n) + align16(16 * n.blocks_m * kWaves));
     if (a->rows > 0) {
         p.splits = n.splits_dq;
         p.part = parts;
