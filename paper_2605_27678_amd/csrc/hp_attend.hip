@@ -769,6 +769,8 @@ template <class T, int DP> constexpr int kStateWaves = kPairs<T> && DP > 128 ? 2
 template <class T, int DP> constexpr int kStateBlock = 32 * kStateWaves<T, DP>;
 template <class T, int DP> constexpr int kStateThreads = kStateWaves<T, DP> * kWave * (kPairs<T> ? 2 : 1);
 
+enum { kPartBoth, kPartDk, kPartDv };
+
 template <class T, int DP> struct StateLds {
     Tiles<T, DP, kTileRows<T, DP>> tiles;            // rows M of q and dout
     __attribute__((aligned(16))) float info[2][256]; // of the rows: lse2, delta, first, end, one behind the other
@@ -791,13 +793,6 @@ template <class T, int DP, bool EXACT, bool CAREFUL> __device__ __forceinline__ 
         const int d = 16 * s + 8 * half;
         return load<8>(from + d, valid ? p.dim - d : 0);
     };
-    Frag<T> k[kHold ? DS : 1], v[kHold ? DS : 1];
-    if constexpr (kHold)
-#pragma unroll
-        for (int s = 0; s < DS; ++s) {
-            k[s] = frag(k_at, s);
-            v[s] = frag(v_at, s);
-        }
     Acc acc[DB] = {}, dv[kTwo ? DB : 1] = {};                                // dk or dv; dk and dv
     // the first and last tile of rows M that see any of the block's states
     const int m_tiles = (p.m_total + NM - 1) / NM;
@@ -858,6 +853,16 @@ template <class T, int DP, bool EXACT, bool CAREFUL> __device__ __forceinline__ 
         Load::fetch_m(lds.tiles.a[stage], p.q, t * NM, p.m_total, p.by_group, state_head * p.group, p.dim, tid);
         Load::fetch_m(lds.tiles.b[stage], p.dout, t * NM, p.m_total, p.by_group, state_head * p.group, p.dim, tid);
     };
+    // A loop for each part: the waves of one make as many turns, and so meet as many barriers, as those of the other.
+    const auto work = [&](auto part) {
+    constexpr bool kDv = part != kPartDk, kDk = part != kPartDv;
+    Frag<T> k[kHold ? DS : 1], v[kHold && kDk ? DS : 1];
+    if constexpr (kHold)
+#pragma unroll
+        for (int s = 0; s < DS; ++s) {
+            k[s] = frag(k_at, s);
+            if constexpr (kDk) v[s] = frag(v_at, s);
+        }
     if (begin < end) fetch(begin, 0);
     in_turn(begin, end, [&](int tile, auto stage) {
         const T *q_tile = lds.tiles.a[stage], *do_tile = lds.tiles.b[stage];
@@ -878,7 +883,7 @@ template <class T, int DP, bool EXACT, bool CAREFUL> __device__ __forceinline__ 
             Acc s = {}, dp = {};
 #pragma unroll
             for (int d = 0; d < DS; ++d) s = mma(row_frag<T, DP>(q_tile, 32 * mb + col, d, half), kHold ? k[kHold ? d : 0] : frag(k_at, d), s);
-            if (makes_dk)
+            if constexpr (kDk)
 #pragma unroll
                 for (int d = 0; d < DS; ++d) dp = mma(row_frag<T, DP>(do_tile, 32 * mb + col, d, half), kHold ? v[kHold ? d : 0] : frag(v_at, d), dp);
 #pragma unroll
@@ -887,7 +892,7 @@ template <class T, int DP, bool EXACT, bool CAREFUL> __device__ __forceinline__ 
 #pragma unroll
                 for (int t = 0; t < 4; ++t) s[4 * b4 + t] = __builtin_amdgcn_exp2f(s[4 * b4 + t] * p.scale2 - lse2[t]);
             }
-            if (makes_dk)
+            if constexpr (kDk)
 #pragma unroll
                 for (int b4 = 0; b4 < 4; ++b4) {
                     const Vec<float, 4> delta = *(const Vec<float, 4> *)(info + NM + 32 * mb + 8 * b4 + 4 * half);
@@ -898,8 +903,8 @@ template <class T, int DP, bool EXACT, bool CAREFUL> __device__ __forceinline__ 
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
                     const bool seen = sees(32 * mb + result_row(i, half));
-                    s[i] = seen ? s[i] : 0.0f;
-                    dp[i] = seen ? dp[i] : 0.0f;
+                    if constexpr (kDv) s[i] = seen ? s[i] : 0.0f;
+                    if constexpr (kDk) dp[i] = seen ? dp[i] : 0.0f;
                 }
             const auto add = [&](auto &to, const Acc &x, const T *tile) {
                 if (CAREFUL && !whole) {
@@ -913,16 +918,15 @@ template <class T, int DP, bool EXACT, bool CAREFUL> __device__ __forceinline__ 
                     for (int db = 0; db < DB; ++db) to[db] = mma(column_frag<T, DP>(tile, 2 * mb + m, db, lane), w, to[db]);
                 }
             };
-            if constexpr (kTwo) {
-                add(dv, s, do_tile);
-                add(acc, dp, q_tile);
-            } else if (makes_dk) {
-                add(acc, dp, q_tile);
-            } else {
-                add(acc, s, do_tile);
-            }
+            if constexpr (kDv && kDk) add(dv, s, do_tile);
+            else if constexpr (kDv) add(acc, s, do_tile);
+            if constexpr (kDk) add(acc, dp, q_tile);
         }
     });
+    };
+    if constexpr (kTwo) work(std::integral_constant<int, kPartBoth>());
+    else if (makes_dk) work(std::integral_constant<int, kPartDk>());
+    else work(std::integral_constant<int, kPartDv>());
     if constexpr (!CAREFUL)
         if (again(&lds.bad)) return dkv_careful<T, DP>((const Attend *)__builtin_amdgcn_kernarg_segment_ptr(), &lds);
     if (!valid) return;
