@@ -199,7 +199,14 @@ __device__ __forceinline__ void careful_product(Acc (&acc)[DB], const Acc &p, co
 // buffer's bounds and comes as zeros; the caller waits (arrived()) before the barrier behind which the tile is read.
 // Other rows pass through registers at once.
 constexpr uint32_t kOutside = 0x80000000u;
-__device__ __forceinline__ void arrived() { __builtin_amdgcn_s_waitcnt(0x0f70); }            // vmcnt(0)
+constexpr int but(int loads) { return (loads & 15) | 0x0f70 | (loads >> 4) << 14; }            // s_waitcnt vmcnt(loads)
+__device__ __forceinline__ void arrived() { __builtin_amdgcn_s_waitcnt(but(0)); }
+// All loads of this wave but those of the last `tiles` tiles, EACH of them a tile.
+template <int EACH> __device__ __forceinline__ void arrived_but(int tiles) {
+    if (tiles <= 0) __builtin_amdgcn_s_waitcnt(but(0));
+    else if (tiles == 1) __builtin_amdgcn_s_waitcnt(but(EACH));
+    else __builtin_amdgcn_s_waitcnt(but(2 * EACH));
+}
 
 template <class T, int DP, int ROWS, int THREADS, bool EXACT> struct Loader {
     typedef Tile<T, DP> L;
@@ -245,11 +252,27 @@ template <class T, int DP, int ROWS, int THREADS, bool EXACT> struct Loader {
             }
         }
     }
-    // Rows M of the matrix that a state head's query heads make.
-    static __device__ __forceinline__ void fetch_m(T *tile, const hp_heads_t &x, int m0, int m_total, const Divisor &group, int head0, int dim, int tid) {
+    // Rows M of the matrix that a state head's query heads make.  Where a tile is whole query rows, as for every group that
+    // is a power of two, its places are the same for all tiles; otherwise each tile's are worked out for it.
+    static __device__ __forceinline__ bool regular(const Divisor &group) { return group.by <= ROWS && ROWS % group.by == 0; }
+    __device__ __forceinline__ void plan_m(const hp_heads_t &x, const Divisor &group, int dim, int tid) {
+        if constexpr (EXACT)
+#pragma unroll
+            for (int n = 0; n < kEach; ++n) {
+                const int e = n * THREADS + tid, r = e / L::kPieces, c = L::piece_of(r, e % L::kPieces), row = group(r), head = r - row * (int)group.by;
+                offsets[n] = c * L::kPiece < dim ? (uint32_t)((row * (int)x.row_stride + head * (int)x.head_stride) * (int)sizeof(T)) + c * 16 : kOutside;
+            }
+    }
+    __device__ __forceinline__ void fetch_m(T *tile, const hp_heads_t &x, int m0, int m_total, const Divisor &group, int head0, int dim, int tid) const {
         const int row0 = __builtin_amdgcn_readfirstlane(group(m0));
         const T *first = (const T *)x.data + row0 * x.row_stride + (int64_t)head0 * x.head_stride;
         const auto from = buffer(first);
+        if (EXACT && regular(group)) {
+#pragma unroll
+            for (int n = 0; n < kEach; ++n)
+                if (loads(n, tid)) direct(tile, n, from, (n * THREADS + tid) / L::kPieces < m_total - m0 ? offsets[EXACT ? n : 0] : kOutside, tid);
+            return;
+        }
 #pragma unroll
         for (int n = 0; n < kEach; ++n) {
             if (!loads(n, tid)) continue;
@@ -382,9 +405,9 @@ template <class T, int DB> __device__ __forceinline__ void store_result(T *to, c
 template <class T, int DP> constexpr int kTileRows = DP * sizeof(T) <= 256 ? 64 : 32;
 
 // Tiles in LDS, two in turn: while one is worked on the next is on its way.
-template <class T, int DP, int ROWS> struct Tiles {
-    __attribute__((aligned(16))) T a[2][ROWS * DP];
-    __attribute__((aligned(16))) T b[2][ROWS * DP];
+template <class T, int DP, int ROWS, int STAGES = 2> struct Tiles {
+    __attribute__((aligned(16))) T a[STAGES][ROWS * DP];
+    __attribute__((aligned(16))) T b[STAGES][ROWS * DP];
 };
 
 template <class T, int DP> struct QueryLds {
@@ -394,10 +417,15 @@ template <class T, int DP> struct QueryLds {
 };
 
 // One after the other, with the stage as a constant: addresses in LDS are then one register and a number.
-template <class Step> __device__ __forceinline__ void in_turn(int begin, int end, const Step &step) {
-    for (int tile = begin; tile < end; tile += 2) {
-        step(tile, std::integral_constant<int, 0>());
-        if (tile + 1 < end) step(tile + 1, std::integral_constant<int, 1>());
+// (Not where that makes more of them than there are registers: beyond 64 KiB.)
+template <int STAGES = 2, class Step> __device__ __forceinline__ void in_turn(int begin, int end, const Step &step) {
+    if constexpr (STAGES == 2) {
+        for (int tile = begin; tile < end; tile += 2) {
+            step(tile, std::integral_constant<int, 0>());
+            if (tile + 1 < end) step(tile + 1, std::integral_constant<int, 1>());
+        }
+    } else {
+        for (int tile = begin, stage = 0; tile < end; ++tile, stage = stage + 1 < STAGES ? stage + 1 : 0) step(tile, stage);
     }
 }
 
@@ -771,9 +799,12 @@ template <class T, int DP> constexpr int kStateThreads = kStateWaves<T, DP> * kW
 
 enum { kPartBoth, kPartDk, kPartDv };
 
+// A workgroup's registers leave a compute unit no second one that would work while this one waits: its tiles are
+// asked for three ahead.
+template <class T, int DP> constexpr int kStateStages = kTileRows<T, DP> * DP * sizeof(T) <= 16384 ? 4 : 2;
 template <class T, int DP> struct StateLds {
-    Tiles<T, DP, kTileRows<T, DP>> tiles;            // rows M of q and dout
-    __attribute__((aligned(16))) float info[2][256]; // of the rows: lse2, delta, first, end, one behind the other
+    Tiles<T, DP, kTileRows<T, DP>, kStateStages<T, DP>> tiles;                // rows M of q and dout
+    __attribute__((aligned(16))) float info[kStateStages<T, DP>][256];        // of the rows: lse2, delta, first, end, one behind the other
     int bad, first_tile, last_tile;
 };
 
@@ -834,9 +865,11 @@ template <class T, int DP, bool EXACT, bool CAREFUL> __device__ __forceinline__ 
     const int count = last >= 0 ? last + 1 - first : 0;
     const int begin = last >= 0 ? first + (int)((int64_t)count * split / p.splits) : 0, end = last >= 0 ? first + (int)((int64_t)count * (split + 1) / p.splits) : 0;
     typedef Loader<T, DP, NM, kThreads, EXACT> Load;
+    Load qs, dos;
+    qs.plan_m(p.q, p.by_group, p.dim, tid);
+    dos.plan_m(p.dout, p.by_group, p.dim, tid);
     int4 next_b = {};
     const auto fetch = [&](int t, int stage) {
-        next_b = bounds_at(t);
         if (wave == 0) {                                 // four runs of NM numbers, 16 bytes a lane
             const int run = lane / (NM / 4), piece = lane % (NM / 4);
             const uint32_t at = (uint32_t)run * (uint32_t)p.heads_k * (uint32_t)p.m_lines * 4 + piece * 16;
@@ -850,8 +883,8 @@ template <class T, int DP, bool EXACT, bool CAREFUL> __device__ __forceinline__ 
                 __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)lds.info[stage], 16, (int)(run < 4 ? at : kOutside), 0, 0, 0);
             }
         }
-        Load::fetch_m(lds.tiles.a[stage], p.q, t * NM, p.m_total, p.by_group, state_head * p.group, p.dim, tid);
-        Load::fetch_m(lds.tiles.b[stage], p.dout, t * NM, p.m_total, p.by_group, state_head * p.group, p.dim, tid);
+        qs.fetch_m(lds.tiles.a[stage], p.q, t * NM, p.m_total, p.by_group, state_head * p.group, p.dim, tid);
+        dos.fetch_m(lds.tiles.b[stage], p.dout, t * NM, p.m_total, p.by_group, state_head * p.group, p.dim, tid);
     };
     // A loop for each part: the waves of one make as many turns, and so meet as many barriers, as those of the other.
     const auto work = [&](auto part) {
@@ -863,15 +896,21 @@ template <class T, int DP, bool EXACT, bool CAREFUL> __device__ __forceinline__ 
             k[s] = frag(k_at, s);
             if constexpr (kDk) v[s] = frag(v_at, s);
         }
-    if (begin < end) fetch(begin, 0);
-    in_turn(begin, end, [&](int tile, auto stage) {
+    constexpr int kStages = CAREFUL ? 2 : kStateStages<T, DP>;
+    if (begin < end) next_b = bounds_at(begin);
+    for (int n = 0; n < kStages - 1; ++n)
+        if (begin + n < end) fetch(begin + n, n);
+    in_turn<kStages>(begin, end, [&](int tile, auto stage) {
         const T *q_tile = lds.tiles.a[stage], *do_tile = lds.tiles.b[stage];
         const float *info = lds.info[stage];
         const int4 b = next_b;
         const bool whole = key0 >= b.z && key0 + 32 <= b.w, meets = key0 < b.y && key0 + 32 > b.x;
-        arrived();
+        if constexpr (!EXACT || kStages == 2) arrived();
+        else if (wave == 0) arrived_but<2 * Load::kEach + 1>(min(end - tile, kStages - 1) - 1);
+        else arrived_but<2 * Load::kEach>(min(end - tile, kStages - 1) - 1);
         __syncthreads();
-        if (tile + 1 < end) fetch(tile + 1, 1 - stage);
+        if (tile + 1 < end) next_b = bounds_at(tile + 1);
+        if (tile + kStages - 1 < end) fetch(tile + kStages - 1, (stage + kStages - 1) % kStages);
         if (!CAREFUL && !(block0 >= b.z && block0 + kStates <= b.w)) {
             const bool one = not_finite<T, DP, NM, kThreads>(q_tile, tid), other = not_finite<T, DP, NM, kThreads>(do_tile, tid);
             if (one || other) lds.bad = 1;
@@ -993,7 +1032,7 @@ Plan plan_of(const hp_attend_args_t &a) {
     const int64_t one = n.blocks_m * a.heads_k > 0 ? n.blocks_m * a.heads_k : 1, two = n.blocks_k * a.heads_k > 0 ? n.blocks_k * a.heads_k : 1;
     n.splits = parts_of(one, 2 * kComputeUnits, a.keys, 256, 32);
     n.splits_dq = parts_of(one, kComputeUnits, a.keys, 256, 32);
-    n.splits_dkv = parts_of(two, 2 * kComputeUnits, m, 256, 32);
+    n.splits_dkv = parts_of(two, 5 * kComputeUnits, m, 256, 32);
     const int64_t each = a.rows * a.heads_k * ((group + 31) / 32);
     n.splits_step = parts_of(each > 0 ? each : 1, 8 * kComputeUnits, a.keys, kStepKeys, 64);
     return n;
