@@ -145,6 +145,18 @@ template <class T, int DP> __device__ __forceinline__ Frag<T> column_frag(const 
     }
 }
 
+// Tells the scheduler how the code before this goes: `ahead` LDS reads, then `products` matrix instructions with the
+// remaining reads between them, `each` after every one.  Left to itself it reads one operand, waits and multiplies.
+template <int READS, int PRODUCTS, int AHEAD, int EACH> __device__ __forceinline__ void stream() {
+    constexpr int kProduct = 0x8, kRead = 0x100;
+    __builtin_amdgcn_sched_group_barrier(kRead, AHEAD < READS ? AHEAD : READS, 0);
+#pragma unroll
+    for (int n = 0; n < PRODUCTS; ++n) {
+        __builtin_amdgcn_sched_group_barrier(kProduct, 1, 0);
+        if (AHEAD + n * EACH < READS) __builtin_amdgcn_sched_group_barrier(kRead, EACH, 0);
+    }
+}
+
 // Eight of a result's rows as the right operand of the next product.
 template <class T> __device__ __forceinline__ Frag<T> result_frag(const Acc &r, int eighths) {
     Frag<T> f;
@@ -476,6 +488,7 @@ template <class T, int DP, bool EXACT, bool CAREFUL> __device__ __forceinline__ 
         for (int d = 0; d < DS; ++d)
 #pragma unroll
             for (int b = 0; b < NB; ++b) s[b] = mma(row_frag<T, DP>(k_tile, 32 * b + col, d, half), q[d], s[b]);
+        if constexpr (sizeof(T) == 2) stream<NB * DS, NB * DS, 6, 1>();
         const bool whole = own.covers(key0, key0 + NK);
         if (!whole)
 #pragma unroll
@@ -496,6 +509,7 @@ template <class T, int DP, bool EXACT, bool CAREFUL> __device__ __forceinline__ 
 #pragma unroll
             for (int db = 0; db < DB; ++db) acc[db] = mma(column_frag<T, DP>(v_tile, k, db, lane), w, acc[db]);
         }
+        if constexpr (sizeof(T) == 2) stream<4 * NB * DB, 2 * NB * DB, 6, 2>();
     });
     if constexpr (!CAREFUL)
         if (again(&lds.bad)) return forward_careful<T, DP>((const Attend *)__builtin_amdgcn_kernarg_segment_ptr(), &lds);
@@ -751,6 +765,7 @@ template <class T, int DP, bool EXACT, bool CAREFUL> __device__ __forceinline__ 
                 s = mma(row_frag<T, DP>(k_tile, 32 * b + col, d, half), kHold ? q[kHold ? d : 0] : frag(q_at, d), s);
                 dp = mma(row_frag<T, DP>(v_tile, 32 * b + col, d, half), kHold ? dout[kHold ? d : 0] : frag(do_at, d), dp);
             }
+            if constexpr (sizeof(T) == 2) stream<2 * DS, 2 * DS, 6, 1>();
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(s[i] * p.scale2 - lse2) * (dp[i] - delta);
             if (!whole)
@@ -766,6 +781,7 @@ template <class T, int DP, bool EXACT, bool CAREFUL> __device__ __forceinline__ 
 #pragma unroll
                 for (int db = 0; db < DB; ++db) acc[db] = mma(column_frag<T, DP>(k_tile, 2 * b + k, db, lane), w, acc[db]);
             }
+            if constexpr (sizeof(T) == 2) stream<4 * DB, 2 * DB, 6, 2>();
         }
     });
     if constexpr (!CAREFUL)
@@ -925,6 +941,7 @@ template <class T, int DP, bool EXACT, bool CAREFUL> __device__ __forceinline__ 
             if constexpr (kDk)
 #pragma unroll
                 for (int d = 0; d < DS; ++d) dp = mma(row_frag<T, DP>(do_tile, 32 * mb + col, d, half), kHold ? v[kHold ? d : 0] : frag(v_at, d), dp);
+            if constexpr (sizeof(T) == 2) stream<kDk ? 2 * DS : DS, kDk ? 2 * DS : DS, 6, 1>();
 #pragma unroll
             for (int b4 = 0; b4 < 4; ++b4) {
                 const Vec<float, 4> lse2 = *(const Vec<float, 4> *)(info + 32 * mb + 8 * b4 + 4 * half);
@@ -956,6 +973,7 @@ template <class T, int DP, bool EXACT, bool CAREFUL> __device__ __forceinline__ 
 #pragma unroll
                     for (int db = 0; db < DB; ++db) to[db] = mma(column_frag<T, DP>(tile, 2 * mb + m, db, lane), w, to[db]);
                 }
+                if constexpr (sizeof(T) == 2) stream<4 * DB, 2 * DB, 6, 2>();
             };
             if constexpr (kDv && kDk) add(dv, s, do_tile);
             else if constexpr (kDv) add(acc, s, do_tile);
