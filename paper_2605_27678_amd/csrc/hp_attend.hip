@@ -546,7 +546,7 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__(kBlock, DP *
 // own, without waiting for one another, and join at the end.
 // Waves of a workgroup, and tiles that each has on their way or in work: as LDS has room for.
 template <class T, int DP> constexpr int kStepWaves = DP * sizeof(T) <= 512 ? 4 : 2;
-template <class T, int DP> constexpr int kStepStages = DP * sizeof(T) <= 256 ? 2 : 1;
+template <class T, int DP> constexpr int kStepStages = DP * sizeof(T) <= 128 ? 2 : 1;
 
 template <class T, int DP, bool EXACT> __global__ __launch_bounds__((kStepWaves<T, DP> * kWave)) void attend_step_kernel(Attend p) {
     constexpr int kWaves = kStepWaves<T, DP>, kStages = kStepStages<T, DP>, DB = DP / 32, DS = DP / 16;

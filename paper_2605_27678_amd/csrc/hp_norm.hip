@@ -235,9 +235,9 @@ struct Finish {
     float *sums;                // hidden values of A for the one gate of all channels, or NULL
 };
 
-constexpr int kColumns = 32, kLines = 8;                   // of a finishing workgroup
+constexpr int kColumns = 32, kLines = 32;                  // of a finishing workgroup
 
-// Adds the lines up: a workgroup takes 32 columns, each of 8 rows of lanes every eighth line, in ascending order.
+// Adds the lines up: a workgroup takes 32 columns, each of its 32 rows of lanes every 32nd line, in ascending order.
 template <class T> __global__ __launch_bounds__(kColumns * kLines) void norm_finish_kernel(Finish f) {
     __shared__ float part[2][kLines][kColumns];
     const int c = (int)threadIdx.x % kColumns, l = (int)threadIdx.x / kColumns, col = (int)blockIdx.x * kColumns + c;
@@ -283,14 +283,14 @@ template <class T> __global__ __launch_bounds__(1024) void norm_gate_kernel(cons
     *(T *)dgate = (T)s;
 }
 
-// How many waves hold a row: as few as keep it within two vectors a lane (three where the registers of eight waves still
-// hold that: the backward of 12288 values of 2 bytes), so that weights, sums and the next row's values stay in registers too.
+// How many waves hold a row: as few as keep it within two or three vectors a lane, so that weights, sums and the next row's
+// values stay in registers too.  Rows of more than 1536 vectors have lanes of four and eight, and spill.
 struct Shape {
     int waves, chunks;
 };
 Shape shape_of(int hidden, int vec) {
     const int lanes = (hidden + vec - 1) / vec;            // that one vector each would take
-    for (const Shape s : {Shape{1, 1}, Shape{1, 2}, Shape{4, 1}, Shape{4, 2}, Shape{8, 2}, Shape{8, 3}, Shape{16, 2}, Shape{16, 4}})
+    for (const Shape s : {Shape{1, 1}, Shape{1, 2}, Shape{4, 1}, Shape{4, 2}, Shape{4, 3}, Shape{8, 2}, Shape{8, 3}, Shape{16, 2}, Shape{16, 4}})
         if (lanes <= s.waves * kWave * s.chunks) return s;
     return {16, 8};
 }
@@ -315,7 +315,8 @@ template <class T> void launch(const Norm &p, const Shape &s, bool backward, int
         else launch<T, 1, 2>(p, backward, blocks, stream);
     } else if (s.waves == 4) {
         if (s.chunks == 1) launch<T, 4, 1>(p, backward, blocks, stream);
-        else launch<T, 4, 2>(p, backward, blocks, stream);
+        else if (s.chunks == 2) launch<T, 4, 2>(p, backward, blocks, stream);
+        else launch<T, 4, 3>(p, backward, blocks, stream);
     } else if (s.waves == 8) {
         if (s.chunks == 2) launch<T, 8, 2>(p, backward, blocks, stream);
         else launch<T, 8, 3>(p, backward, blocks, stream);

@@ -27,43 +27,49 @@ struct RotaryParams {
     const int32_t *positions;
     int32_t n_tensors, n_heads;               // of all tensors together
     int32_t dim, half, n_axes, inverse;
-    int32_t units, copies, per_row, rows_per_block;   // lanes: pairs / VEC, channels behind them / VEC, of a row, and rows of a block
+    int32_t units, copies, per_row, rows_per_block;   // lanes of a head, those of them that copy, lanes of a row, and rows of a block
     int32_t axis_end[HP_ROTARY_MAX_AXES];
     int32_t heads[HP_ROTARY_MAX_TENSORS];
     hp_heads_t x[HP_ROTARY_MAX_TENSORS], out[HP_ROTARY_MAX_TENSORS];
 };
 
-// One lane: VEC pairs of one row, in kHeads heads (or VEC copied channels there).
-// Consecutive lanes take consecutive pairs, then the next heads: a wave reads
-// runs of half a head.
+// One lane: a vector of VEC channels and the one that they turn with, VEC pairs, or VEC interleaved channels, VEC / 2
+// pairs, or VEC copied channels; of one row, in kHeads heads.  Consecutive lanes take consecutive vectors, then the next
+// heads, so that a wave reads and writes runs of a head or half a head.
 template <class T, int VEC, bool INTERLEAVED> __global__ __launch_bounds__(kThreads) void rotary_kernel(RotaryParams p) {
     const int item = (int)blockIdx.y * kThreads + (int)threadIdx.x;
     const int in_block = p.rows_per_block > 1 ? item / p.per_row : 0;
     const int at_row = item - in_block * p.per_row;
     if (in_block >= p.rows_per_block || at_row >= p.per_row) return;
     const int group = at_row / p.units, u = at_row - group * p.units;
+    constexpr int PAIRS = INTERLEAVED ? VEC / 2 : VEC;
     const int turned = p.units - p.copies;
+    const int behind = 2 * p.half + (u - turned) * VEC;                        // a copying lane's first channel
     for (int64_t block = blockIdx.x; block * p.rows_per_block < p.rows; block += gridDim.x) {
         const int64_t row = block * p.rows_per_block + in_block;
         if (row >= p.rows) break;
-        float c[VEC], s[VEC];
+        float c[PAIRS], s[PAIRS];
         if (u < turned) {
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) c[j] = s[j] = __builtin_nanf("");
-            if (p.n_axes == 1) {
-                const int64_t pos = p.positions[row];
+            for (int j = 0; j < PAIRS; ++j) c[j] = s[j] = __builtin_nanf("");
+            const auto axis_of = [&](int i) {
+                int axis = 0;
+                for (int a = 0; a < HP_ROTARY_MAX_AXES - 1; ++a) axis += a < p.n_axes - 1 && i >= p.axis_end[a];
+                return axis;
+            };
+            const int axis0 = axis_of(u * PAIRS);
+            if (PAIRS == 1 || axis_of(u * PAIRS + PAIRS - 1) == axis0) {       // all but the few lanes at an axis's border
+                const int64_t pos = p.positions[axis0 * p.axis_stride + row];
                 if (pos >= 0 && pos < p.table_rows) {
-                    const Vec<float, 2 * VEC> t = load<2 * VEC>(p.table + (pos * p.half + u * VEC) * 2, 2 * VEC);
+                    const Vec<float, 2 * PAIRS> t = load<2 * PAIRS>(p.table + (pos * p.half + u * PAIRS) * 2, 2 * PAIRS);
 #pragma unroll
-                    for (int j = 0; j < VEC; ++j) c[j] = t[2 * j], s[j] = t[2 * j + 1];
+                    for (int j = 0; j < PAIRS; ++j) c[j] = t[2 * j], s[j] = t[2 * j + 1];
                 }
             } else {
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    const int i = u * VEC + j;
-                    int axis = 0;
-                    while (axis < p.n_axes - 1 && i >= p.axis_end[axis]) ++axis;
-                    const int64_t pos = p.positions[axis * p.axis_stride + row];
+                for (int j = 0; j < PAIRS; ++j) {
+                    const int i = u * PAIRS + j;
+                    const int64_t pos = p.positions[axis_of(i) * p.axis_stride + row];
                     if (pos >= 0 && pos < p.table_rows) {
                         const Vec<float, 2> t = load<2>(p.table + (pos * p.half + i) * 2, 2);
                         c[j] = t[0], s[j] = t[1];
@@ -72,7 +78,7 @@ template <class T, int VEC, bool INTERLEAVED> __global__ __launch_bounds__(kThre
             }
             if (p.inverse)
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) s[j] = -s[j];
+                for (int j = 0; j < PAIRS; ++j) s[j] = -s[j];
         }
         Vec<T, VEC> a[kHeads], b[kHeads];
         T *to[kHeads];
@@ -86,58 +92,52 @@ template <class T, int VEC, bool INTERLEAVED> __global__ __launch_bounds__(kThre
             const T *from = (const T *)p.x[t].data + row * p.x[t].row_stride + h * p.x[t].head_stride;
             to[k] = (T *)p.out[t].data + row * p.out[t].row_stride + h * p.out[t].head_stride;
             if (u >= turned) {
-                a[k] = load<VEC>(from + 2 * p.half + (u - turned) * VEC, VEC);
-            } else if constexpr (INTERLEAVED) {
-                a[k] = load<VEC>(from + 2 * u * VEC, VEC);
-                b[k] = load<VEC>(from + 2 * u * VEC + VEC, VEC);
+                a[k] = load<VEC>(from + behind, p.dim - behind);
             } else {
                 a[k] = load<VEC>(from + u * VEC, VEC);
-                b[k] = load<VEC>(from + p.half + u * VEC, VEC);
+                if constexpr (!INTERLEAVED) b[k] = load<VEC>(from + p.half + u * VEC, VEC);
             }
         }
 #pragma unroll
         for (int k = 0; k < kHeads; ++k) {
             if (!to[k]) continue;
             if (u >= turned) {
-                store<VEC>(to[k] + 2 * p.half + (u - turned) * VEC, a[k], VEC);
+                store<VEC>(to[k] + behind, a[k], p.dim - behind);
                 continue;
             }
             Vec<T, VEC> ra, rb;
-            if constexpr (INTERLEAVED) {           // 2 * VEC channels in a row: pair j is channels 2j, 2j + 1 of them
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    const int e = 2 * j, o = e + 1;
-                    const float xa = e < VEC ? at<VEC, T>(a[k], e) : at<VEC, T>(b[k], e - VEC);
-                    const float xb = o < VEC ? at<VEC, T>(a[k], o) : at<VEC, T>(b[k], o - VEC);
-                    const float ya = xa * c[j] - xb * s[j], yb = xb * c[j] + xa * s[j];
-                    if (e < VEC) put<VEC, T>(ra, e, ya); else put<VEC, T>(rb, e - VEC, ya);
-                    if (o < VEC) put<VEC, T>(ra, o, yb); else put<VEC, T>(rb, o - VEC, yb);
-                }
-                store<VEC>(to[k] + 2 * u * VEC, ra, VEC);
-                store<VEC>(to[k] + 2 * u * VEC + VEC, rb, VEC);
-            } else {
-#pragma unroll
-                for (int j = 0; j < VEC; ++j) {
-                    const float xa = at<VEC, T>(a[k], j), xb = at<VEC, T>(b[k], j);
-                    put<VEC, T>(ra, j, xa * c[j] - xb * s[j]);
-                    put<VEC, T>(rb, j, xb * c[j] + xa * s[j]);
-                }
-                store<VEC>(to[k] + u * VEC, ra, VEC);
-                store<VEC>(to[k] + p.half + u * VEC, rb, VEC);
+            for (int j = 0; j < PAIRS; ++j) {
+                const float xa = at<VEC, T>(a[k], INTERLEAVED ? 2 * j : j), xb = INTERLEAVED ? at<VEC, T>(a[k], 2 * j + 1) : at<VEC, T>(b[k], j);
+                const float ya = xa * c[j] - xb * s[j], yb = xb * c[j] + xa * s[j];
+                put<VEC, T>(ra, INTERLEAVED ? 2 * j : j, ya);
+                if constexpr (INTERLEAVED) put<VEC, T>(ra, 2 * j + 1, yb);
+                else put<VEC, T>(rb, j, yb);
             }
+            store<VEC>(to[k] + u * VEC, ra, VEC);
+            if constexpr (!INTERLEAVED) store<VEC>(to[k] + p.half + u * VEC, rb, VEC);
         }
     }
 }
 
-template <class T, int VEC> void launch(RotaryParams &p, bool interleaved, bool copies, hipStream_t stream) {
-    p.copies = copies ? (p.dim - 2 * p.half) / VEC : 0;
-    p.units = p.half / VEC + p.copies;
+template <class T, int VEC, bool INTERLEAVED> void launch(RotaryParams &p, bool copies, hipStream_t stream) {
+    p.copies = copies ? (p.dim - 2 * p.half + VEC - 1) / VEC : 0;
+    p.units = (INTERLEAVED ? 2 * p.half : p.half) / VEC + p.copies;
     p.per_row = p.units * ((p.n_heads + kHeads - 1) / kHeads);
     p.rows_per_block = p.per_row >= kThreads ? 1 : kThreads / p.per_row;
     const int64_t blocks = (p.rows + p.rows_per_block - 1) / p.rows_per_block;
     const dim3 grid((uint32_t)(blocks < (1 << 22) ? blocks : (1 << 22)), p.per_row > kThreads ? (p.per_row + kThreads - 1) / kThreads : 1);
-    if (interleaved) rotary_kernel<T, VEC, true><<<grid, kThreads, 0, stream>>>(p);
-    else rotary_kernel<T, VEC, false><<<grid, kThreads, 0, stream>>>(p);
+    rotary_kernel<T, VEC, INTERLEAVED><<<grid, kThreads, 0, stream>>>(p);
+}
+
+// The widest lanes that divide the channels they turn, 16 bytes at most.
+template <class T> void launch(RotaryParams &p, bool interleaved, bool copies, hipStream_t stream) {
+    const int run = interleaved ? 2 * p.half : p.half;
+    if constexpr (sizeof(T) == 2)
+        if (run % 8 == 0) return interleaved ? launch<T, 8, true>(p, copies, stream) : launch<T, 8, false>(p, copies, stream);
+    if (run % 4 == 0) return interleaved ? launch<T, 4, true>(p, copies, stream) : launch<T, 4, false>(p, copies, stream);
+    if (run % 2 == 0) return interleaved ? launch<T, 2, true>(p, copies, stream) : launch<T, 2, false>(p, copies, stream);
+    launch<T, 1, false>(p, copies, stream);            // an odd half: interleaved runs are even
 }
 
 struct TableParams {
@@ -241,20 +241,9 @@ int hp_rotary(const hp_rotary_args_t *a, void *stream) {
     p.dim = a->dim;
     p.n_axes = a->n_axes;
     p.inverse = a->inverse != 0;
-    // The widest lanes that divide the pairs and the channels behind them, 16 bytes at most.
-    const bool copies = !in_place && a->dim > a->rot, inter = a->interleaved != 0;
-    const int all = p.half | (copies ? a->dim - a->rot : 0);
-    const hipStream_t s = (hipStream_t)stream;
-    if (a->dtype == HP_BF16) {
-        if (all % 8 == 0) launch<__bf16, 8>(p, inter, copies, s);
-        else if (all % 4 == 0) launch<__bf16, 4>(p, inter, copies, s);
-        else if (all % 2 == 0) launch<__bf16, 2>(p, inter, copies, s);
-        else launch<__bf16, 1>(p, inter, copies, s);
-    } else {
-        if (all % 4 == 0) launch<float, 4>(p, inter, copies, s);
-        else if (all % 2 == 0) launch<float, 2>(p, inter, copies, s);
-        else launch<float, 1>(p, inter, copies, s);
-    }
+    const bool copies = !in_place && a->dim > a->rot;
+    if (a->dtype == HP_BF16) launch<__bf16>(p, a->interleaved != 0, copies, (hipStream_t)stream);
+    else launch<float>(p, a->interleaved != 0, copies, (hipStream_t)stream);
     return hip_failed(hipGetLastError()) ? HP_EHIP : HP_OK;
 }
 
