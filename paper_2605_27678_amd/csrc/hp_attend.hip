@@ -19,6 +19,15 @@
 // states that not all rows of a wave see holds an infinity or NaN, the workgroup begins again in a function of its own,
 // which makes the products of such tiles value by value (careful_product).  Beside the loop that is there for speed, that
 // code cost it registers, and loads from scratch memory wait for the tiles on their way.
+//
+// What bounds it.  A wave reads 1 KiB of LDS for each product of 32 x 32 x 16, which takes LDS as long (at 128 bytes a cycle)
+// as the matrix units: both, and the exponentials, are busy for 30 to 45 % of the time each, and only waves at different
+// places overlap them - two a SIMD, which is what registers allow.  Heads of 128 in bf16 on an MI355X, counting what is seen:
+// forward 1.0 PFLOP/s (8192 rows of 32 heads, 4032 states each: 0.54 ms) and 0.92 (16384 rows of 10 heads against up to 40139:
+// 1.85 ms); dq 0.6 ms and dk, dv 1.3 ms of 2.16 for 8192 rows of 32 heads against up to 5760 states (8192^3 by the library:
+// 1.18 PFLOP/s).  Single tokens are bound by memory: 64 rows of 64 heads against 576 to 6404 states 4.8 TB/s (a large copy:
+// 5.2).  Tried and left: 64-row tiles in one loop with the other block's exponentials among the products (the backward of
+// states spills: 4.7 ms), raised priority for the waves in a product (no change).
 #include <cfloat>
 #include <climits>
 #include <cmath>
@@ -656,24 +665,34 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__((kStepWaves<
     }
 }
 
-// Joins the parts of each row and head: a wave each.
+// Joins the parts of each row and head, a workgroup each: the lanes of a wave hold a part's statistics each (there are
+// at most 64), the waves take every fourth part.  One wave going through the parts one behind the other took 45 us of
+// the 54 for one token against 8000 states in 62 parts.
+constexpr int kMostParts = kWave;
 template <class T> __global__ __launch_bounds__(kBlock) void attend_join_kernel(Attend p) {
-    const int64_t n = p.rows * p.heads_q, at = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave;
-    const int lane = (int)threadIdx.x % kWave;
-    if (at >= n) return;
+    __shared__ __attribute__((aligned(16))) float half_done[kWaves][HP_ATTEND_MAX_DIM];
+    const int64_t n = p.rows * p.heads_q, at = blockIdx.x;
+    const int lane = (int)threadIdx.x % kWave, wave = (int)threadIdx.x / kWave;
     const int64_t row = at / p.heads_q;
     const int head = (int)(at - row * p.heads_q);
-    float top = -INFINITY, sum = 0.0f;
-    for (int s = 0; s < p.splits; ++s) top = fmaxf(top, p.part_lse[s * n + at]);
+    const float lse2 = lane < p.splits ? p.part_lse[lane * n + at] : -INFINITY;
+    float top = lse2;
+#pragma unroll
+    for (int d = kWave / 2; d; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
+    const float mine = lse2 == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(lse2 - top);      // nothing seen in this part; NaN stays
+    const float sum = wave_sum(mine);
     Vec<float, 4> acc = {};
     const int d = 4 * lane;
-    for (int s = 0; s < p.splits; ++s) {
-        const float lse2 = p.part_lse[s * n + at];
-        if (lse2 == -INFINITY) continue;                            // nothing seen in this part (a NaN is not skipped)
-        const float w = __builtin_amdgcn_exp2f(lse2 - top);
-        sum += w;
-        acc += w * load<4>(p.part + (s * n + at) * p.dim + d, p.dim - d);
+#pragma unroll 4
+    for (int s = wave; s < p.splits; s += kWaves) {
+        const float w = __shfl(mine, s);
+        const Vec<float, 4> part = load<4>(p.part + (s * n + at) * p.dim + d, p.dim - d);
+        if (w != 0.0f) acc += w * part;
     }
+    if (d < HP_ATTEND_MAX_DIM) *(Vec<float, 4> *)&half_done[wave][d] = acc;
+    __syncthreads();
+    if (wave) return;
+    for (int w = 1; w < kWaves; ++w) acc += *(const Vec<float, 4> *)&half_done[w][d];
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     Vec<T, 4> o;
 #pragma unroll
@@ -1018,6 +1037,7 @@ template <class T> __global__ __launch_bounds__(kBlock) void attend_sum_kernel(c
     if (at >= n || d >= dim) return;
     const int64_t row = at / heads;
     Vec<float, 4> acc = {};
+#pragma unroll 4
     for (int s = 0; s < splits; ++s) acc += load<4>(part + (s * n + at) * dim + d, dim - d);
     Vec<T, 4> o;
 #pragma unroll
@@ -1048,11 +1068,18 @@ Plan plan_of(const hp_attend_args_t &a) {
     const int64_t states = a.dtype == HP_F32 || a.dim <= 128 ? 128 : 64;
     n.blocks_k = (a.keys + states - 1) / states;
     const int64_t one = n.blocks_m * a.heads_k > 0 ? n.blocks_m * a.heads_k : 1, two = n.blocks_k * a.heads_k > 0 ? n.blocks_k * a.heads_k : 1;
+    // 256 rows of 32 heads against 4032 states: 42 us with 256 workgroups, 44 with 512, 57 with 1024; 512 rows of 10 heads
+    // against 40139: 162, 166, 151; 2048 against 4032: 137, 137, 200.
     n.splits = parts_of(one, 2 * kComputeUnits, a.keys, 256, 32);
     n.splits_dq = parts_of(one, kComputeUnits, a.keys, 256, 32);
+    // States early in a sequence are seen by more rows than late ones: workgroups enough to even that out (8192 rows of 32
+    // heads against 5760 states, forward and backward: 2.56 ms with 256, 2.28 with 1024, 2.25 with 1280, 2.31 with 3000).
     n.splits_dkv = parts_of(two, 5 * kComputeUnits, m, 256, 32);
     const int64_t each = a.rows * a.heads_k * ((group + 31) / 32);
-    n.splits_step = parts_of(each > 0 ? each : 1, 8 * kComputeUnits, a.keys, kStepKeys, 64);
+    // Few rows: as many workgroups as run at once (8 rows of 8 state heads against 3000 states: 24 us with 512, 33 with
+    // 2048).  More rows: several times that, so that requests of unequal lengths even out (64 rows of 8 heads against 576 to
+    // 6404 states: 191 us with 2048; of equal ones it costs 4 %, 173 to 180).
+    n.splits_step = parts_of(each > 0 ? each : 1, each <= kComputeUnits / 2 ? 2 * kComputeUnits : 8 * kComputeUnits, a.keys, kStepKeys, kMostParts);
     return n;
 }
 
@@ -1177,7 +1204,7 @@ int forward(const hp_attend_args_t &a, Kernel what, const dim3 &grid, hipStream_
     launch(what, a.dtype, p, grid, s);
     if (failed()) return HP_EHIP;
     if (p.splits > 1) {
-        const uint32_t blocks = (uint32_t)((p.rows * p.heads_q + kWaves - 1) / kWaves);
+        const uint32_t blocks = (uint32_t)(p.rows * p.heads_q);
         if (a.dtype == HP_BF16) attend_join_kernel<__bf16><<<blocks, kBlock, 0, s>>>(p);
         else attend_join_kernel<float><<<blocks, kBlock, 0, s>>>(p);
         if (failed()) return HP_EHIP;
