@@ -1162,7 +1162,7 @@ enum Kernel { kForward, kStep, kDq, kDkv };
 bool exact(const hp_heads_t &t, int size, int32_t dim, int32_t heads) {
     const int64_t piece = 16 / size;
     if (dim % piece || misaligned(t.data, 16) || t.row_stride % piece || t.head_stride % piece || t.row_stride < 0 || t.head_stride < 0) return false;
-    const int64_t most = ((int64_t)1 << 30) / size;
+    const int64_t most = ((int64_t)1 << 29) / size;      // rows and heads together: less than 2^31 bytes
     return t.row_stride <= most / 64 && t.head_stride <= most / heads;
 }
 
