@@ -665,14 +665,17 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__((kStepWaves<
     }
 }
 
-// Joins the parts of each row and head, a workgroup each: the lanes of a wave hold a part's statistics each (there are
-// at most 64), the waves take every fourth part.  One wave going through the parts one behind the other took 45 us of
-// the 54 for one token against 8000 states in 62 parts.
-constexpr int kMostParts = kWave;
+// Joins the parts of each row and head: the lanes of a wave hold a part's statistics each (there are at most 64).  Many
+// parts are a workgroup's, its waves take every fourth: one wave going through them one behind the other took 45 us of the
+// 54 for one token against 8000 states in 62 parts.  Few are a wave's: 49200 rows and heads of two parts 19 us, with
+// a workgroup each 48.
+constexpr int kMostParts = kWave, kFewParts = 8;
 template <class T> __global__ __launch_bounds__(kBlock) void attend_join_kernel(Attend p) {
     __shared__ __attribute__((aligned(16))) float half_done[kWaves][HP_ATTEND_MAX_DIM];
-    const int64_t n = p.rows * p.heads_q, at = blockIdx.x;
     const int lane = (int)threadIdx.x % kWave, wave = (int)threadIdx.x / kWave;
+    const bool few = p.splits <= kFewParts;
+    const int64_t n = p.rows * p.heads_q, at = few ? (int64_t)blockIdx.x * kWaves + wave : blockIdx.x;
+    if (at >= n) return;                                            // whole waves, and only where each works by itself
     const int64_t row = at / p.heads_q;
     const int head = (int)(at - row * p.heads_q);
     const float lse2 = lane < p.splits ? p.part_lse[lane * n + at] : -INFINITY;
@@ -684,15 +687,17 @@ template <class T> __global__ __launch_bounds__(kBlock) void attend_join_kernel(
     Vec<float, 4> acc = {};
     const int d = 4 * lane;
 #pragma unroll 4
-    for (int s = wave; s < p.splits; s += kWaves) {
+    for (int s = few ? 0 : wave; s < p.splits; s += few ? 1 : kWaves) {
         const float w = __shfl(mine, s);
         const Vec<float, 4> part = load<4>(p.part + (s * n + at) * p.dim + d, p.dim - d);
         if (w != 0.0f) acc += w * part;
     }
-    if (d < HP_ATTEND_MAX_DIM) *(Vec<float, 4> *)&half_done[wave][d] = acc;
-    __syncthreads();
-    if (wave) return;
-    for (int w = 1; w < kWaves; ++w) acc += *(const Vec<float, 4> *)&half_done[w][d];
+    if (!few) {
+        *(Vec<float, 4> *)&half_done[wave][d] = acc;
+        __syncthreads();
+        if (wave) return;
+        for (int w = 1; w < kWaves; ++w) acc += *(const Vec<float, 4> *)&half_done[w][d];
+    }
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     Vec<T, 4> o;
 #pragma unroll
@@ -1204,7 +1209,8 @@ int forward(const hp_attend_args_t &a, Kernel what, const dim3 &grid, hipStream_
     launch(what, a.dtype, p, grid, s);
     if (failed()) return HP_EHIP;
     if (p.splits > 1) {
-        const uint32_t blocks = (uint32_t)(p.rows * p.heads_q);
+        const int64_t items = p.rows * p.heads_q;
+        const uint32_t blocks = (uint32_t)(p.splits <= kFewParts ? (items + kWaves - 1) / kWaves : items);
         if (a.dtype == HP_BF16) attend_join_kernel<__bf16><<<blocks, kBlock, 0, s>>>(p);
         else attend_join_kernel<float><<<blocks, kBlock, 0, s>>>(p);
         if (failed()) return HP_EHIP;
