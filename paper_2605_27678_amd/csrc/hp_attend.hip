@@ -71,7 +71,7 @@ struct Attend {
     const int32_t *ranges;
     float *lse;
     float *part, *part_lse;                         // [splits][rows * heads_q][dim], [splits][rows * heads_q]
-    float *info;                                    // [4][heads_k][m_lines]: lse2, delta, first and end of what a row M sees
+    float *info;                                    // [heads_k][m_lines / tile][4][tile]: lse2, delta, first and end of what a row M sees
     int4 *bounds;                                   // of each 32 rows M
     int32_t m_lines, reserved;                      // rows M, filled up to whole workgroups
     float *part_k, *part_v;                         // [splits][keys * heads_k][dim]
@@ -749,11 +749,11 @@ template <class T, int DP, bool EXACT, bool CAREFUL> __device__ __forceinline__ 
     if (!CAREFUL && split == 0) {
         if (half == 0) {
             // rows that are not there see nothing
-            const int64_t each = (int64_t)p.heads_k * p.m_lines, to = (int64_t)state_head * p.m_lines + line;
-            p.info[to] = lse2;
-            p.info[each + to] = delta;
-            ((int *)p.info)[2 * each + to] = at.valid ? see.lo : 0;
-            ((int *)p.info)[3 * each + to] = at.valid ? see.hi : 0;
+            float *to = p.info + 4 * ((int64_t)state_head * p.m_lines + line / NK * NK) + line % NK;
+            to[0] = lse2;
+            to[NK] = delta;
+            ((int *)to)[2 * NK] = at.valid ? see.lo : 0;
+            ((int *)to)[3 * NK] = at.valid ? see.hi : 0;
         }
         // rows that see nothing, or are not there, keep the states' kernel from taking 32 rows for unmasked
         const bool all = __all(at.valid && !see.empty());
@@ -910,17 +910,13 @@ template <class T, int DP, bool EXACT, bool CAREFUL> __device__ __forceinline__ 
     dos.plan_m(p.dout, p.by_group, p.dim, tid);
     int4 next_b = {};
     const auto fetch = [&](int t, int stage) {
-        if (wave == 0) {                                 // four runs of NM numbers, 16 bytes a lane
-            const int run = lane / (NM / 4), piece = lane % (NM / 4);
-            const uint32_t at = (uint32_t)run * (uint32_t)p.heads_k * (uint32_t)p.m_lines * 4 + piece * 16;
-            const auto from = Load::buffer(p.info + (int64_t)state_head * p.m_lines + (int64_t)t * NM);
+        if (wave == 0) {                                 // 4 NM numbers, 16 bytes a lane
+            const float *from = p.info + 4 * ((int64_t)state_head * p.m_lines + (int64_t)t * NM);
             if constexpr (CAREFUL) {
-                if (run < 4) {
-                    const int64_t far = (int64_t)run * p.heads_k * p.m_lines + (int64_t)state_head * p.m_lines + (int64_t)t * NM + piece * 4;
-                    *(Vec<float, 4> *)&lds.info[stage][4 * lane] = *(const Vec<float, 4> *)(p.info + far);
-                }
+                if (lane < NM) *(Vec<float, 4> *)&lds.info[stage][4 * lane] = *(const Vec<float, 4> *)(from + 4 * lane);
             } else {
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void *)lds.info[stage], 16, (int)(run < 4 ? at : kOutside), 0, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(Load::buffer(from), (__attribute__((address_space(3))) void *)lds.info[stage], 16,
+                                                         (int)(lane < NM ? 16u * lane : kOutside), 0, 0, 0);
             }
         }
         qs.fetch_m(lds.tiles.a[stage], p.q, t * NM, p.m_total, p.by_group, state_head * p.group, p.dim, tid);
