@@ -34,6 +34,7 @@
 #include <type_traits>
 
 #include "hp_device.hpp"
+#include "hp_meet.hpp"
 #include "hp_operators.h"
 
 #pragma clang fp contract(fast)
@@ -222,17 +223,18 @@ __device__ __forceinline__ void careful_product(Acc (&acc)[DB], const Acc &p, co
 constexpr uint32_t kOutside = 0x80000000u;
 constexpr int but(int loads) { return (loads & 15) | 0x0f70 | (loads >> 4) << 14; }            // s_waitcnt vmcnt(loads)
 __device__ __forceinline__ void arrived() { __builtin_amdgcn_s_waitcnt(but(0)); }
-// All loads of this wave but those of the last `tiles` tiles, EACH of them a tile.
+// All loads of this wave but those of the last `tiles` tiles, of which it makes EACH a tile.
 template <int EACH> __device__ __forceinline__ void arrived_but(int tiles) {
     if (tiles <= 0) __builtin_amdgcn_s_waitcnt(but(0));
-    else if (tiles == 1) __builtin_amdgcn_s_waitcnt(but(EACH));
-    else __builtin_amdgcn_s_waitcnt(but(2 * EACH));
+    else if (tiles == 1) __builtin_amdgcn_s_waitcnt(but(under_way(EACH, 1)));
+    else __builtin_amdgcn_s_waitcnt(but(under_way(EACH, 2)));
 }
 
 template <class T, int DP, int ROWS, int THREADS, bool EXACT> struct Loader {
     typedef Tile<T, DP> L;
     static constexpr int kAll = ROWS * L::kPieces, kEach = (kAll + THREADS - 1) / THREADS;
     static_assert(kAll % kWave == 0, "every wave loads whole or not");
+    static constexpr int kMost = loads_of_wave(kAll, THREADS, 0), kLeast = loads_of_wave(kAll, THREADS, THREADS / kWave - 1);
     // whether the lane's wave has pieces in round n
     static __device__ __forceinline__ bool loads(int n, int tid) { return (n + 1) * THREADS <= kAll || __builtin_amdgcn_readfirstlane(n * THREADS + tid) < kAll; }
     static __device__ __forceinline__ void piece(T *tile, int n, const T *p, int valid, int tid) {
@@ -942,8 +944,9 @@ template <class T, int DP, bool EXACT, bool CAREFUL> __device__ __forceinline__ 
         const int4 b = next_b;
         const bool whole = key0 >= b.z && key0 + 32 <= b.w, meets = key0 < b.y && key0 + 32 > b.x;
         if constexpr (!EXACT || kStages == 2) arrived();
-        else if (wave == 0) arrived_but<2 * Load::kEach + 1>(min(end - tile, kStages - 1) - 1);
-        else arrived_but<2 * Load::kEach>(min(end - tile, kStages - 1) - 1);
+        else if (wave == 0) arrived_but<2 * Load::kMost + 1>(min(end - tile, kStages - 1) - 1);      // the rows' numbers too
+        else if (Load::loads(Load::kEach - 1, tid)) arrived_but<2 * Load::kMost>(min(end - tile, kStages - 1) - 1);
+        else arrived_but<2 * Load::kLeast>(min(end - tile, kStages - 1) - 1);
         __syncthreads();
         if (tile + 1 < end) next_b = bounds_at(tile + 1);
         if (tile + kStages - 1 < end) fetch(tile + kStages - 1, (stage + kStages - 1) % kStages);

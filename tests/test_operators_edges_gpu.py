@@ -1,0 +1,62 @@
+"""Places of the operators where waves meet, values cancel or arguments only nearly fit, on the GPU."""
+import pytest
+import torch
+
+import operators_plain as plain
+import paper_2605_27678_amd as hp
+from operators_plain import BF16, F32, check
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+
+
+def rand(seed, *shape, dtype=BF16):
+    return torch.randn(shape, generator=torch.Generator(device=DEV).manual_seed(seed), device=DEV).to(dtype)
+
+
+def whole(seed, low, high, *shape):
+    """Whole numbers from low to high."""
+    return torch.randint(low, high + 1, shape, generator=torch.Generator(device=DEV).manual_seed(seed), device=DEV).to(BF16)
+
+
+def bytes_of(n):
+    return torch.empty(max(int(n), 16), dtype=torch.uint8, device=DEV)
+
+
+def attend_run(q, k, v, ranges, dout=None, scale=None, step=False):
+    rows, heads_q, _ = q.shape
+    got = {"out": torch.full_like(q, 7.0), "lse": torch.full((rows, heads_q), 7.0, dtype=F32, device=DEV)}
+    call = hp.hp_cross_attend_step if step else hp.hp_cross_attend
+    call(q, k, v, ranges, got["out"], lse=got["lse"], scale=scale, workspace=bytes_of(hp.hp_cross_attend_workspace(q, k, "step" if step else "forward")))
+    if dout is not None:
+        got.update({n: torch.full_like(t, 7.0) for n, t in (("dq", q), ("dk", k), ("dv", v))})
+        hp.hp_cross_attend_backward(q, k, v, ranges, got["out"], got["lse"], dout, got["dq"], got["dk"], got["dv"], scale=scale,
+                                    workspace=bytes_of(hp.hp_cross_attend_workspace(q, k, "backward")))
+    return got
+
+
+# ---- where waves meet ---------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dim", [64, 72, 80, 88, 96, 128, 256])
+def test_gradients_of_states_over_a_hundred_tiles_a_part(dim):
+    """Every tile of rows counts, and exactly: keys of zeros give each of 2048 states the weight 2^-11, values that come in
+    pairs of a number and its negative give out = 0, and all else is whole numbers, so that dv = 2^-11 sum dout and
+    dk = scale 2^-11 sum (dout . v) q are whole multiples of a power of two, whatever the order of their sums, and are
+    rounded once.  A piece of another tile in a sum would change it."""
+    rows, keys, heads_q, heads_k, scale = 16384, 2048, 32, 16, 0.125
+    q, dout = whole(1, -3, 3, rows, heads_q, dim), whole(2, -3, 3, rows, heads_q, dim)
+    k = torch.zeros(keys, heads_k, dim, dtype=BF16, device=DEV)
+    v = torch.zeros_like(k)
+    v[: keys // 2, :, 1:dim:13] = whole(3, -2, 2, keys // 2, heads_k, len(range(1, dim, 13)))
+    v[keys // 2:] = -v[: keys // 2]
+    got = attend_run(q, k, v, None, dout, scale)
+    assert not bool(got["out"].any()) and not bool(got["dq"].any())
+    group = heads_q // heads_k
+    for h in range(heads_k):
+        a, g = (t[:, h * group:(h + 1) * group].reshape(-1, dim).double() for t in (q, dout))
+        dp = g @ v[:, h].double().t().contiguous()
+        assert float(dp.abs().max()) <= 256                              # as bfloat16 holds them
+        dv, dk = g.sum(0) / keys, scale / keys * (dp.t().contiguous() @ a)
+        assert torch.equal(got["dv"][:, h], dv.to(BF16).expand(keys, dim)), f"dv of head {h}"
+        assert torch.equal(got["dk"][:, h], dk.to(BF16)), f"dk of head {h}"
