@@ -53,8 +53,7 @@ template <class T> using Frag = Vec<T, 8>;
 
 // Whether a pass met what only the careful one takes right.
 __device__ __forceinline__ bool again(const int *bad) {
-    __syncthreads();
-    return __builtin_amdgcn_readfirstlane(*bad) != 0;
+    return __builtin_amdgcn_readfirstlane(read_together(bad, [] { __syncthreads(); })) != 0;
 }
 
 // Division of numbers below 2^30 by one that a launch keeps.

@@ -11,4 +11,13 @@ constexpr int loads_of_wave(int pieces, int threads, int wave) { return pieces /
 // tiles after that one (loads end in the order in which they were made).
 constexpr int under_way(int each, int behind) { return behind > 0 ? each * behind : 0; }
 
+// A flag that any wave may have set, read by all of them alike: `meet` is the workgroup's barrier.  The second one keeps a
+// wave that goes on (and may clear the flag for what comes next) from those that have not read it yet.
+template <class Meet> constexpr int read_together(const int *flag, const Meet &meet) {
+    meet();
+    const int set = *flag;
+    meet();
+    return set;
+}
+
 }  // namespace hp

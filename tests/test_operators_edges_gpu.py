@@ -60,3 +60,27 @@ def test_gradients_of_states_over_a_hundred_tiles_a_part(dim):
         dv, dk = g.sum(0) / keys, scale / keys * (dp.t().contiguous() @ a)
         assert torch.equal(got["dv"][:, h], dv.to(BF16).expand(keys, dim)), f"dv of head {h}"
         assert torch.equal(got["dk"][:, h], dk.to(BF16)), f"dk of head {h}"
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("dim", [64, 96, 128, 256])
+def test_workgroups_that_begin_again_do_so_whole(dim, dtype):
+    """Samples of 48 rows and 80 states, so that every workgroup has tiles that not all of its rows see; one sample in two
+    holds values that are not finite, and the others' results are those of the calls without them."""
+    n, heads_q, heads_k = 40, 4, 2
+    rows, keys = 48 * n, 80 * n
+    q, k, v, dout = (rand(i, m, h, dim, dtype=dtype) for i, (m, h) in enumerate(((rows, heads_q), (keys, heads_k), (keys, heads_k), (rows, heads_q))))
+    sample = torch.arange(rows, device=DEV) // 48
+    ranges = torch.stack([80 * sample, 80 * (sample + 1)], 1).to(torch.int32)
+    good = attend_run(q, k, v, ranges, dout)
+    for t, each in ((q, 48), (dout, 48), (k, 80), (v, 80)):
+        part = t.view(n, each, *t.shape[1:])
+        part[1::2, ::7], part[1::2, 3::7] = float("nan"), float("inf")
+    for turn in range(3):
+        got = attend_run(q, k, v, ranges, dout)
+        for name, t in got.items():
+            a, b = (x.view(n, -1, *x.shape[1:])[::2].double() for x in (t, good[name]))
+            assert bool(torch.isfinite(a).all()), (turn, name)
+            # value by value instead of by matrix products: other sums of the same terms
+            off = 2 * plain.unit(dtype) * b.abs() + 2.0 ** -8 * (1 if dtype is BF16 else 2.0 ** -12)
+            assert bool(((a - b).abs() <= off).all()), (turn, name)

@@ -26,3 +26,13 @@ def test_waits_by_the_loads_of_other_waves_are_found(walk):
     """64 rows of 96 channels are 768 pieces for 512 lanes: half the waves make one load of a matrix, half two."""
     r = walk("loads", "1")
     assert r.returncode == 1 and "before it is there" in r.stdout, r.stdout + r.stderr
+
+
+def test_a_flag_is_read_by_all_waves_before_any_goes_on(walk):
+    r = walk("flag", "0")
+    assert r.returncode == 0 and r.stdout.strip() == "ok", r.stdout + r.stderr
+
+
+def test_a_flag_read_behind_one_barrier_alone_is_found(walk):
+    r = walk("flag", "1")
+    assert r.returncode == 1 and "read another flag" in r.stdout, r.stdout + r.stderr

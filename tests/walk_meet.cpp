@@ -1,14 +1,21 @@
 // Host-side check of how the waves of a workgroup meet over tiles in LDS (hp_meet.hpp, the kernels' own arithmetic):
 // built by tests/test_operators_meet.py with UBSan.
-// usage: walk_meet loads <mistake>
+// usage: walk_meet <loads|flag> <mistake>
 //   loads: every wave of workgroups of 128 to 1024 lanes asks for tiles three ahead, two matrices a tile and the rows'
 //   numbers by wave 0, and waits as the kernel does; no load of the tile that is then read may still be under way, and
 //   no fewer tiles than were asked for after it (so that asking ahead is not undone).  mistake: waits go by
 //   0: the wave's own loads; 1: those of the waves that make most.
+//   flag: threads in the place of waves read a flag, some of them late, and the first clears it as soon as it goes on; all
+//   have to have read the same.  mistake: the flag is read 0: as the kernels do; 1: behind one barrier and before none.
+#include <chrono>
+#include <condition_variable>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
 #include <deque>
+#include <mutex>
+#include <thread>
+#include <vector>
 
 #include "hp_meet.hpp"
 
@@ -40,10 +47,57 @@ static int check_loads(int mistake) {
     return 0;
 }
 
+class Barrier {
+    std::mutex m;
+    std::condition_variable all;
+    int waiting = 0, turn = 0;
+    const int n;
+
+  public:
+    explicit Barrier(int count) : n(count) {}
+    void meet() {
+        std::unique_lock<std::mutex> lock(m);
+        const int mine = turn;
+        if (++waiting == n) {
+            waiting = 0, ++turn;
+            all.notify_all();
+        } else {
+            all.wait(lock, [&] { return turn != mine; });
+        }
+    }
+};
+
+static int check_flag(int mistake) {
+    for (int late = 0; late < 4; ++late) {                        // the wave that is held up behind every barrier
+        constexpr int kWaves = 4;
+        Barrier barrier(kWaves);
+        int flag = 1, got[kWaves] = {};
+        std::vector<std::thread> waves;
+        for (int w = 0; w < kWaves; ++w)
+            waves.emplace_back([&, w] {
+                const auto meet = [&] {
+                    barrier.meet();
+                    if (w == late) std::this_thread::sleep_for(std::chrono::milliseconds(100));
+                };
+                if (mistake) {
+                    meet();
+                    got[w] = __atomic_load_n(&flag, __ATOMIC_RELAXED);
+                } else {
+                    got[w] = hp::read_together(&flag, meet);
+                }
+                if (w == 0) __atomic_store_n(&flag, 0, __ATOMIC_RELAXED);
+            });
+        for (std::thread &t : waves) t.join();
+        for (int w = 0; w < kWaves; ++w) CHECK(got[w] == 1, "wave %d, with wave %d late, read another flag than wave 0", w, late);
+    }
+    return 0;
+}
+
 int main(int argc, char **argv) {
     if (argc != 3) return 2;
     int rc = 2;
     if (!std::strcmp(argv[1], "loads")) rc = check_loads(std::atoi(argv[2]));
+    if (!std::strcmp(argv[1], "flag")) rc = check_flag(std::atoi(argv[2]));
     if (rc == 0) std::printf("ok\n");
     return rc;
 }
