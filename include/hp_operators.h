@@ -166,7 +166,9 @@ int64_t hp_gated_norm_workspace(int64_t rows, int32_t hidden);
  * What a row does not see has no influence on it, whatever the values there are
  * (infinities and NaN included).  Rows next to each other should see much the
  * same states: up to 128 / group of them share the pass over what any of them sees.
- *   q, out: [rows, heads_q, dim]; k, v: [keys, heads_k, dim]; dim 1..256.
+ *   q, out: [rows, heads_q, dim]; k, v: [keys, heads_k, dim]; dim 1..256, heads_q up to
+ *           16384 and a multiple of heads_k.  rows * heads_q / heads_k up to 2^30 - 1024,
+ *           keys up to 2^31 - 1025 (HP_ELAYOUT).
  *   lse:    binary32 [rows, heads_q], may be NULL: receives the natural logarithm
  *           of the sum of exponentials, -inf for an empty row.
  *   scale:  > 0.
@@ -195,7 +197,8 @@ int hp_cross_attend_step(const hp_attend_args_t *args, void *stream);
 /* hp_cross_attend_backward - gradients of hp_cross_attend (or _step) from its
  * inputs, out, lse and the gradient dout of out.  dq, dk and dv are overwritten
  * whole: states that no row sees get zeros.  Heads that share a state head add up
- * in binary32.  Workspace: hp_cross_attend_workspace(args, HP_ATTEND_BACKWARD). */
+ * in binary32.  In bf16 keys up to 2^30 - 1024 (HP_ELAYOUT).
+ * Workspace: hp_cross_attend_workspace(args, HP_ATTEND_BACKWARD). */
 int hp_cross_attend_backward(const hp_attend_args_t *args, void *stream);
 
 #define HP_ATTEND_FORWARD  0

@@ -1103,7 +1103,7 @@ int64_t workspace_of(const hp_attend_args_t &a, int call) {
 
 bool misaligned(const void *p, int to) { return (uintptr_t)p % to != 0; }
 
-int check_sizes(const hp_attend_args_t *a) {
+int check_sizes(const hp_attend_args_t *a, int call) {
     if (!a) return HP_EINVAL;
     if (a->dtype != HP_BF16 && a->dtype != HP_F32) return HP_EINVAL;
     if (a->dim < 1 || a->dim > HP_ATTEND_MAX_DIM || a->heads_k < 1 || a->heads_q < 1) return HP_EINVAL;
@@ -1111,11 +1111,13 @@ int check_sizes(const hp_attend_args_t *a) {
     if (a->rows < 0 || a->keys < 0) return HP_EINVAL;
     // rows M, states and lanes of a launch are counted in 32 bits, with tiles to spare
     if (a->rows > ((1 << 30) - 1024) / (a->heads_q / a->heads_k) || a->keys > INT_MAX - 1024) return HP_ELAYOUT;
+    // the backward of states has 4 lanes a state in bf16 (in binary32 2)
+    if (call == HP_ATTEND_BACKWARD && a->dtype == HP_BF16 && a->keys > (1 << 30) - 1024) return HP_ELAYOUT;
     return HP_OK;
 }
 
 int check(const hp_attend_args_t *a, int call) {
-    if (const int rc = check_sizes(a)) return rc;
+    if (const int rc = check_sizes(a, call)) return rc;
     if (!(a->scale > 0) || !std::isfinite(a->scale) || !std::isfinite(a->scale * kLog2e)) return HP_EINVAL;
     const int size = a->dtype == HP_BF16 ? 2 : 4;
     const bool back = call == HP_ATTEND_BACKWARD;
@@ -1228,7 +1230,7 @@ int add_up(const float *part, int splits, int dtype, int64_t rows, int heads, in
 extern "C" {
 
 int64_t hp_cross_attend_workspace(const hp_attend_args_t *a, int32_t call) {
-    if (const int rc = check_sizes(a)) return rc;
+    if (const int rc = check_sizes(a, call)) return rc;
     if (call < HP_ATTEND_FORWARD || call > HP_ATTEND_BACKWARD) return HP_EINVAL;
     return workspace_of(*a, call);
 }

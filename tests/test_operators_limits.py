@@ -1,0 +1,36 @@
+"""Sizes and layouts that the operators' calls refuse before anything is launched (so without a GPU)."""
+import ctypes as C
+
+import pytest
+
+from paper_2605_27678_amd import operators as ops
+from paper_2605_27678_amd.binding import HP_ELAYOUT, HP_OK
+
+A = 1 << 20                                       # an address that no refused call looks at
+
+
+def heads(p=A, row=64, head=8):
+    return ops.hp_heads_t(p, row, head)
+
+
+def attend_args(**kw):
+    d = dict(dtype=0, heads_q=8, heads_k=2, dim=64, rows=4, keys=6, scale=0.125, q=heads(), k=heads(), v=heads(), out=heads(), ranges=A, lse=A,
+             workspace=A, workspace_bytes=1 << 60, dout=heads(), dq=heads(), dk=heads(), dv=heads())
+    return ops.hp_attend_args_t(**{**d, **kw})
+
+
+def workspace(call, **kw):
+    return ops._lib().hp_cross_attend_workspace(C.byref(attend_args(**kw)), call)
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_backward_refuses_states_whose_lanes_pass_32_bits(dim):
+    """Four lanes a state in bf16, two in binary32; a launch has less than 2^32 of them."""
+    L, most = ops._lib(), (1 << 30) - 1024
+    for keys in (most + 1, 1 << 30, (1 << 31) - 1025):
+        assert L.hp_cross_attend_backward(C.byref(attend_args(keys=keys, dim=dim)), None) == HP_ELAYOUT
+        assert workspace(2, keys=keys, dim=dim) == HP_ELAYOUT
+        assert workspace(2, keys=keys, dim=dim, dtype=1) > 0
+        assert workspace(0, keys=keys, dim=dim) >= 0 and workspace(1, keys=keys, dim=dim) >= 0
+    assert workspace(2, keys=most, dim=dim) > 0
+    assert L.hp_cross_attend(C.byref(attend_args(keys=1 << 30, dim=dim, rows=0)), None) == HP_OK
