@@ -191,7 +191,8 @@ int hp_cross_attend(const hp_attend_args_t *args, void *stream);
 
 /* hp_cross_attend_step - the same function for rows that have nothing in common,
  * as the single tokens of many requests against a cache of their states: every
- * row makes its own pass over its range, long ranges in several parts. */
+ * row makes its own pass over its range, long ranges in several parts.  Up to
+ * 2^23 rows (HP_ELAYOUT). */
 int hp_cross_attend_step(const hp_attend_args_t *args, void *stream);
 
 /* hp_cross_attend_backward - gradients of hp_cross_attend (or _step) from its

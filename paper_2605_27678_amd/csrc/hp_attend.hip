@@ -1113,6 +1113,8 @@ int check_sizes(const hp_attend_args_t *a, int call) {
     if (a->rows > ((1 << 30) - 1024) / (a->heads_q / a->heads_k) || a->keys > INT_MAX - 1024) return HP_ELAYOUT;
     // the backward of states has 4 lanes a state in bf16 (in binary32 2)
     if (call == HP_ATTEND_BACKWARD && a->dtype == HP_BF16 && a->keys > (1 << 30) - 1024) return HP_ELAYOUT;
+    // single tokens have 256 lanes a row
+    if (call == HP_ATTEND_STEP && a->rows > 1 << 23) return HP_ELAYOUT;
     return HP_OK;
 }
 
@@ -1244,7 +1246,6 @@ int hp_cross_attend(const hp_attend_args_t *a, void *stream) {
 
 int hp_cross_attend_step(const hp_attend_args_t *a, void *stream) {
     if (const int rc = check(a, HP_ATTEND_STEP)) return rc;
-    if (a->rows > 1 << 23) return HP_ELAYOUT;
     if (a->rows == 0) return HP_OK;
     const Plan n = plan_of(*a);
     const int32_t parts = (a->heads_q / a->heads_k + 31) / 32;

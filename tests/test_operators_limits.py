@@ -34,3 +34,13 @@ def test_backward_refuses_states_whose_lanes_pass_32_bits(dim):
         assert workspace(0, keys=keys, dim=dim) >= 0 and workspace(1, keys=keys, dim=dim) >= 0
     assert workspace(2, keys=most, dim=dim) > 0
     assert L.hp_cross_attend(C.byref(attend_args(keys=1 << 30, dim=dim, rows=0)), None) == HP_OK
+
+
+def test_the_scratch_memory_of_single_tokens_is_refused_where_the_call_is():
+    most = 1 << 23
+    for rows, code in ((most, None), (most + 1, HP_ELAYOUT), (1 << 27, HP_ELAYOUT)):
+        size = workspace(1, rows=rows)
+        assert size >= 0 if code is None else size == code
+        if code is not None:
+            assert ops._lib().hp_cross_attend_step(C.byref(attend_args(rows=rows)), None) == code
+    assert workspace(0, rows=most + 1) >= 0
