@@ -115,7 +115,7 @@ int hp_rotary(const hp_rotary_args_t *args, void *stream);
  * z goes by h before its rounding.  rstd (binary32 [2, rows], may be NULL)
  * receives the factors 1/sqrt(..) of y and of h, 1 where there is no norm.
  * h or z may be NULL if not wanted (not both).  h may be x or y in place, z may
- * be x or y; other overlaps are not allowed. */
+ * be x or y, with the same stride (HP_EINVAL); other overlaps are not allowed. */
 typedef struct hp_norm_args {
     int32_t dtype;
     int32_t gate_size, gate_tanh, unit_offset;
@@ -135,7 +135,8 @@ int hp_gated_norm(const hp_norm_args_t *args, void *stream);
 /* hp_gated_norm_backward - gradients of the above.  `f` is the forward's struct
  * (its h and z are not read; rstd, filled by the forward, is needed).
  *   dh, dz: gradients of h and z [rows, hidden]; one of them may be NULL (zero).
- *   dx, dy: [rows, hidden], each may be NULL; dx may be dh or dz in place, dy too.
+ *   dx, dy: [rows, hidden], each may be NULL; dx may be dh or dz in place, with the
+ *     same stride (HP_EINVAL), dy too.
  *   dw_post, dgate, dw_pre: of the weights' shapes and type, overwritten; each may
  *     be NULL.  Sums over rows are in binary32, in an order that follows from the
  *     sizes alone.

@@ -336,6 +336,12 @@ template <class T> void launch(const Norm &p, const Shape &s, bool backward, int
 
 bool misaligned(const void *p, int to) { return (uintptr_t)p % to != 0; }
 
+// Whether rows written in the place of others that are read lie elsewhere than these: a row would be overwritten before
+// another group of waves has read it.
+bool crosses(const Norm &p, const void *from, int64_t from_stride, const void *to, int64_t to_stride) {
+    return to && from == to && from_stride != to_stride && p.rows > 1;
+}
+
 // Checks what both calls read and fills in the kernels' struct.
 int take(const hp_norm_args_t *a, Norm *p) {
     if (!a) return HP_EINVAL;
@@ -387,6 +393,8 @@ int hp_gated_norm(const hp_norm_args_t *a, void *stream) {
     if (a->rows == 0) return HP_OK;
     if (!a->h && !a->z) return HP_EINVAL;
     p.h = a->h, p.z = a->z, p.hs = a->h_stride, p.zs = a->z_stride;
+    if (crosses(p, p.x, p.xs, p.h, p.hs) || crosses(p, p.y, p.ys, p.h, p.hs)) return HP_EINVAL;
+    if (crosses(p, p.x, p.xs, p.z, p.zs) || crosses(p, p.y, p.ys, p.z, p.zs)) return HP_EINVAL;
     const Shape s = shape_of(p.hidden, 16 / size);
     const int64_t blocks = blocks_of(p.rows, s, false);
     if (a->dtype == HP_BF16) launch<__bf16>(p, s, false, blocks, (hipStream_t)stream);
@@ -414,6 +422,8 @@ int hp_gated_norm_backward(const hp_norm_args_t *a, const hp_norm_grads_t *g, vo
     if (a->rows > 0 && (!a->rstd || (!g->dh && !g->dz))) return HP_EINVAL;
     p.dh = g->dh, p.dz = g->dz, p.dx = g->dx, p.dy = g->dy;
     p.dhs = g->dh_stride, p.dzs = g->dz_stride, p.dxs = g->dx_stride, p.dys = g->dy_stride;
+    if (crosses(p, p.dh, p.dhs, p.dx, p.dxs) || crosses(p, p.dz, p.dzs, p.dx, p.dxs)) return HP_EINVAL;
+    if (crosses(p, p.dh, p.dhs, p.dy, p.dys) || crosses(p, p.dz, p.dzs, p.dy, p.dys)) return HP_EINVAL;
     p.partial = sums ? (float *)g->workspace : nullptr;
     const hipStream_t st = (hipStream_t)stream;
     const Shape s = shape_of(p.hidden, 16 / size);

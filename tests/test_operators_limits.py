@@ -4,7 +4,7 @@ import ctypes as C
 import pytest
 
 from paper_2605_27678_amd import operators as ops
-from paper_2605_27678_amd.binding import HP_ELAYOUT, HP_OK
+from paper_2605_27678_amd.binding import HP_EINVAL, HP_ELAYOUT, HP_OK
 
 A = 1 << 20                                       # an address that no refused call looks at
 
@@ -44,3 +44,29 @@ def test_the_scratch_memory_of_single_tokens_is_refused_where_the_call_is():
         if code is not None:
             assert ops._lib().hp_cross_attend_step(C.byref(attend_args(rows=rows)), None) == code
     assert workspace(0, rows=most + 1) >= 0
+
+
+# ---- norms in place ------------------------------------------------------------------------------------------------
+
+B = 2 * A
+NORM = dict(dtype=0, gate_size=1, rows=4, hidden=64, residual_scale=1.0, eps=1e-6, x=A, y=B, x_stride=64, y_stride=80, h=3 * A, z=4 * A,
+            h_stride=64, z_stride=64, w_post=5 * A, w_pre=6 * A, rstd=7 * A)
+
+
+@pytest.mark.parametrize("kw", [dict(h=A, h_stride=65), dict(h=B), dict(z=A, z_stride=128), dict(z=B), dict(h=A, z=B, z_stride=-80),
+                                dict(x_stride=0, h=A)])
+def test_norm_in_place_goes_by_the_same_strides(kw):
+    """A row's result would stand where another row is still to be read."""
+    L = ops._lib()
+    call = lambda **more: L.hp_gated_norm(C.byref(ops.hp_norm_args_t(**{**NORM, **kw, **more})), None)  # noqa: E731
+    assert call() == HP_EINVAL and call(rows=0) == HP_OK
+
+
+@pytest.mark.parametrize("kw", [dict(dx=A, dx_stride=63), dict(dx=B), dict(dy=A, dy_stride=128), dict(dy=B)])
+def test_norm_gradients_in_place_go_by_the_same_strides(kw):
+    grads = dict(dh=A, dz=B, dh_stride=64, dz_stride=80, dx=3 * A, dy=4 * A, dx_stride=64, dy_stride=64)
+    f = {**NORM, "x": 8 * A, "y": 9 * A}
+    L = ops._lib()
+    call = lambda **more: L.hp_gated_norm_backward(C.byref(ops.hp_norm_args_t(**{**f, **more})),  # noqa: E731
+                                                   C.byref(ops.hp_norm_grads_t(**{**grads, **kw})), None)
+    assert call() == HP_EINVAL and call(rows=0) == HP_OK
