@@ -266,8 +266,10 @@ template <class T> __global__ __launch_bounds__(kColumns * kLines) void norm_fin
     if (f.gate) {
         t = (float)((const T *)f.gate)[f.gate_size > 1 ? col : 0];
         if (f.gate_tanh) {
+            // 1 - tanh^2 without the difference, which has no bits left from gates of 9 on: 4 e / (1 + e)^2, e = exp(-2 |gate|)
+            const float e = expf(-2.0f * fabsf(t));
+            slope = 4.0f * e / ((1.0f + e) * (1.0f + e));
             t = tanhf(t);
-            slope = 1.0f - t * t;
         }
     }
     const float w1 = f.w1 ? (float)((const T *)f.w1)[col] + (f.unit_offset ? 1.0f : 0.0f) : 1.0f;

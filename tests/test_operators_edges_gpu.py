@@ -84,3 +84,58 @@ def test_workgroups_that_begin_again_do_so_whole(dim, dtype):
             # value by value instead of by matrix products: other sums of the same terms
             off = 2 * plain.unit(dtype) * b.abs() + 2.0 ** -8 * (1 if dtype is BF16 else 2.0 ** -12)
             assert bool(((a - b).abs() <= off).all()), (turn, name)
+
+
+# ---- where values cancel ------------------------------------------------------------------------------------------------
+
+def gate_gradient(x, y, w_post, gate, w_pre, scale, dh, dz, eps=1e-6):
+    """(exact, bound) of the gradient of tanh(gate) in 64 bits: sums over rows (and channels, for one gate) of
+    D y r1 w1 slope, slope = 1 - tanh^2 = (2 / (e^g + e^-g))^2.  A term is a few products of numbers that carry the roundings
+    of sums over a row - a lane's up to 64 values, six steps over a wave, 16 waves - and passes, on its way, its group's
+    rows, every 32nd line, 32 of these sums and, for one gate, every 1024th channel and 21 more."""
+    a, b, w1, w2, g = (t.double() for t in (x, y, w_post, w_pre, gate))
+    slope = (2 / (g.exp() + (-g).exp())).square()
+    r1 = 1 / (b.square().mean(-1, keepdim=True) + eps).sqrt()
+    n = b * r1 * w1
+    h = scale * a + g.tanh() * n
+    r2 = 1 / (h.square().mean(-1, keepdim=True) + eps).sqrt()
+    d = dz.double() * w2 * r2
+    whole = dh.double() + d - h * r2.square() * (h * d).mean(-1, keepdim=True)
+    most = dh.double().abs() + d.abs() + h.abs() * r2.square() * (h * d).abs().mean(-1, keepdim=True)
+    e, m = (whole * n).sum(0) * slope, (most * n.abs()).sum(0) * slope
+    if gate.numel() == 1:
+        e, m = e.sum().view(1), m.sum().view(1)
+    rows, hidden = x.shape
+    ways = 8 * plain.sums(86) + plain.sums(rows // 256 + rows // 32 + 33 + hidden // 1024 + 24)
+    return e, plain.unit(x.dtype) * e.abs() + ways * m
+
+
+def gate_case(rows, hidden, dtype, gate):
+    """The whole gradient of a training step, with dh along the block's output so that the sum for one gate does not cancel."""
+    x, y, dz = rand(1, rows, hidden, dtype=dtype), rand(2, rows, hidden, dtype=dtype), rand(4, rows, hidden, dtype=dtype)
+    dh = (y.float() + 0.5 * rand(3, rows, hidden, dtype=F32)).to(dtype)
+    w1, w2 = (1 + 0.1 * rand(5 + i, hidden, dtype=F32).to(dtype) for i in range(2))
+    h, z, dx, dy = (torch.empty_like(x) for _ in range(4))
+    rstd, dgate = torch.empty(2, rows, dtype=F32, device=DEV), torch.full_like(gate, 7.0)
+    hp.hp_gated_norm(x, y, h, z, w1, gate, w2, gate_tanh=True, residual_scale=0.5, rstd=rstd)
+    hp.hp_gated_norm_backward(dh, dz, x, y, rstd, w1, gate, w2, dx, dy, None, dgate, None, gate_tanh=True, residual_scale=0.5,
+                              workspace=bytes_of(hp.hp_gated_norm_workspace(rows, hidden)))
+    return (dgate, *gate_gradient(x, y, w1, gate, w2, 0.5, dh, dz))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("gate", [0.0, 0.25, -1.0, 4.0, -8.0, 12.0, -40.0, 100.0])
+def test_the_gradient_of_a_gate_far_from_zero(gate, dtype):
+    for size in (1, 328):
+        dgate, exact, bound = gate_case(37, 328, dtype, torch.full((size,), gate, dtype=dtype, device=DEV))
+        check(f"dgate of {size}", dgate, exact, bound, 1e-37)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,hidden", [(1, 64), (3, 7), (65, 512), (33, 1000), (5, 2305), (300, 4096), (17, 5120), (2500, 512), (6, 8193),
+                                         (700, 12288), (2, 32768)])
+def test_the_gradient_of_one_gate_for_all_channels(rows, hidden, dtype):
+    dgate, exact, bound = gate_case(rows, hidden, dtype, torch.full((1,), 0.75, dtype=dtype, device=DEV))
+    # what a gradient without the slope (0.60 here), or of nine rows in ten, would be is out of bounds
+    assert float(bound) < 0.05 * float(exact.abs())
+    check("dgate", dgate, exact, bound)
