@@ -243,7 +243,7 @@ bool norm_args(PyObject *const *p, Checks &c, hp_norm_args_t *a) {
     const at::Tensor *gate = c.take(p[3], 1, true, true), *w2 = c.shaped(p[4], x->sizes().slice(1), true, true);
     const int64_t lines[2] = {2, a->rows};
     const at::Tensor *rstd = c.shaped(p[9], at::IntArrayRef(lines, 2), true, true, at::kFloat);
-    if (!c.ok || (gate && gate->numel() > INT32_MAX)) return false;
+    if (!c.ok || (gate && (gate->numel() < 1 || gate->numel() > INT32_MAX))) return false;
     if (y) a->y = at_of(y), a->y_stride = y->stride(0);
     a->w_post = at_of(w1), a->gate = at_of(gate), a->w_pre = at_of(w2), a->rstd = (float *)at_of(rstd);
     a->gate_size = gate ? (int32_t)gate->numel() : 0;

@@ -251,6 +251,8 @@ def _norm_args(x, y, w_post, gate, w_pre, gate_tanh, residual_scale, unit_offset
             setattr(a, name, _ptr(_tensor(w, name, (hidden,), like=x, contiguous=True)))
     if gate is not None:
         _tensor(gate, "gate", (None,), like=x, contiguous=True)
+        if not gate.numel():                             # its address would be that of no gate
+            raise ValueError("gate: no values, need one or one a channel")
         a.gate, a.gate_size = _ptr(gate), gate.numel()
     if rstd is not None:
         a.rstd = _ptr(_tensor(rstd, "rstd", (2, rows), dtype=torch.float32, contiguous=True))

@@ -5,6 +5,7 @@ import torch
 import operators_plain as plain
 import paper_2605_27678_amd as hp
 from operators_plain import BF16, F32, check
+from paper_2605_27678_amd import operators as ops
 
 pytestmark = pytest.mark.gpu
 
@@ -139,3 +140,26 @@ def test_the_gradient_of_one_gate_for_all_channels(rows, hidden, dtype):
     # what a gradient without the slope (0.60 here), or of nine rows in ten, would be is out of bounds
     assert float(bound) < 0.05 * float(exact.abs())
     check("dgate", dgate, exact, bound)
+
+
+# ---- arguments that only nearly fit ---------------------------------------------------------------------------------------
+
+@pytest.fixture(params=["extension", "python"])
+def way(request, monkeypatch):
+    """Calls by the extension, and by Python, which takes what the extension leaves to it."""
+    if request.param == "python":
+        monkeypatch.setattr(ops, "_fast", False)
+
+
+def test_a_gate_without_values_is_no_missing_gate(way):
+    x, y, w, none = rand(1, 5, 64), rand(2, 5, 64), torch.ones(64, dtype=BF16, device=DEV), torch.empty(0, dtype=BF16, device=DEV)
+    h, z, rstd = torch.full_like(x, 7.0), torch.full_like(x, 7.0), torch.full((2, 5), 7.0, device=DEV)
+    with pytest.raises(ValueError, match="gate"):
+        hp.hp_gated_norm(x, y, h, z, w, none, w, rstd=rstd)
+    dx, dy = torch.full_like(x, 7.0), torch.full_like(x, 7.0)
+    with pytest.raises(ValueError, match="gate"):
+        hp.hp_gated_norm_backward(x, y, x, y, rstd, w, none, w, dx, dy, None, None, None)
+    with pytest.raises(ValueError, match="gate"):
+        hp.gated_norm(x, y, w, none, w)
+    for t in (h, z, dx, dy, rstd):
+        assert bool((t == 7.0).all())
