@@ -187,6 +187,7 @@ int entries(PyObject *list, PyObject **out, int cap) {
     return (int)n;
 }
 
+// An object that is neither leaves Python's error set.
 bool truth(PyObject *o) { return PyObject_IsTrue(o) > 0; }
 
 // rotary(fn, xs, outs, table, positions, interleaved, inverse, sections, stream)
@@ -228,6 +229,7 @@ PyObject *rotary(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
         if (args[7] != Py_None) a.axis_stride = pos->stride(0);
         a.positions = (const int32_t *)at_of(pos);
         a.dtype = c.dtype(), a.interleaved = truth(args[5]), a.inverse = truth(args[6]);
+        if (PyErr_Occurred()) return false;
         *rc = without_gil([&] { return ((int (*)(const hp_rotary_args_t *, void *))fn)(&a, stream); });
         return true;
     });

@@ -163,3 +163,16 @@ def test_a_gate_without_values_is_no_missing_gate(way):
         hp.gated_norm(x, y, w, none, w)
     for t in (h, z, dx, dy, rstd):
         assert bool((t == 7.0).all())
+
+
+def test_switches_that_are_neither_true_nor_false(way):
+    x, table = rand(1, 5, 2, 16), torch.ones(8, 8, 2, device=DEV)
+    pos, out, both = torch.arange(5, dtype=torch.int32, device=DEV), torch.full((5, 2, 16), 7.0, dtype=BF16, device=DEV), torch.tensor([True, False])
+    for how in (dict(interleaved=both), dict(inverse=both), dict(interleaved=both, inverse=both)):
+        with pytest.raises(RuntimeError, match="ambiguous"):
+            hp.hp_rotary([x], [out], table, pos, **how)
+    w, h = torch.ones(16, dtype=BF16, device=DEV), torch.full((5, 16), 7.0, dtype=BF16, device=DEV)
+    for how in (dict(gate_tanh=both), dict(unit_offset=both)):
+        with pytest.raises(RuntimeError, match="ambiguous"):
+            hp.hp_gated_norm(x[:, 0], x[:, 1], h, None, w, **how)
+    assert bool((out == 7.0).all()) and bool((h == 7.0).all())
