@@ -232,8 +232,11 @@ int hp_rotary(const hp_rotary_args_t *a, void *stream) {
         if (a->heads[t] < 0 || a->heads[t] > 4096) return HP_EINVAL;
         if (a->rows > 0 && a->heads[t] > 0 && (!a->x[t].data || !a->out[t].data)) return HP_EINVAL;
         if (misaligned(a->x[t].data, size) || misaligned(a->out[t].data, size)) return HP_EALIGN;
-        const bool same = a->x[t].data == a->out[t].data;
-        if (same && (a->x[t].row_stride != a->out[t].row_stride || a->x[t].head_stride != a->out[t].head_stride)) return HP_EINVAL;
+        // strides that no address goes by do not count: empty tensors, single rows and single heads
+        const bool same = a->x[t].data == a->out[t].data, some = a->rows > 0 && a->heads[t] > 0;
+        if (same && some && ((a->rows > 1 && a->x[t].row_stride != a->out[t].row_stride) ||
+                             (a->heads[t] > 1 && a->x[t].head_stride != a->out[t].head_stride)))
+            return HP_EINVAL;
         in_place = in_place && same;
         n_heads += a->heads[t];
         p.heads[t] = a->heads[t];

@@ -70,3 +70,20 @@ def test_norm_gradients_in_place_go_by_the_same_strides(kw):
     call = lambda **more: L.hp_gated_norm_backward(C.byref(ops.hp_norm_args_t(**{**f, **more})),  # noqa: E731
                                                    C.byref(ops.hp_norm_grads_t(**{**grads, **kw})), None)
     assert call() == HP_EINVAL and call(rows=0) == HP_OK
+
+
+# ---- rotary in place -----------------------------------------------------------------------------------------------
+
+def rotary_args(x, out, rows, n_heads, **kw):
+    a = ops.hp_rotary_args_t(**{**dict(dtype=0, n_tensors=1, dim=64, rot=32, n_axes=1, rows=rows, table=A, table_rows=8, positions=B), **kw})
+    a.heads[0], a.x[0], a.out[0] = n_heads, x, out
+    return a
+
+
+@pytest.mark.parametrize("code,x,out,rows,n_heads", [
+    (HP_OK, heads(None, 640), heads(None, 64), 0, 3),         # nothing at all, as empty tensors come: no place, so not in place
+    (HP_OK, heads(None, 640), heads(None, 64), 4, 0), (HP_OK, heads(A, 640), heads(A, 64), 0, 3), (HP_OK, heads(A, 640), heads(A, 64), 4, 0),
+    (HP_EINVAL, heads(A, 640, 64), heads(A, 320, 64), 4, 1), (HP_EINVAL, heads(A, 640, 64), heads(A, 640, 128), 4, 2),
+    (HP_EINVAL, heads(A, 640, 64), heads(A, 640, 128), 1, 2)])
+def test_rotary_in_place_goes_by_the_strides_that_count(code, x, out, rows, n_heads):
+    assert ops._lib().hp_rotary(C.byref(rotary_args(x, out, rows, n_heads)), None) == code
