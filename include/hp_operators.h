@@ -23,9 +23,11 @@
  * type, no more.  Zero rows are in order: nothing is launched.
  *
  * Sums, softmax statistics and angles are held in binary32 or more whatever the
- * element type; results are rounded once, to nearest even.  For equal inputs the
- * results are the same bits on every call: no sum depends on the order in which
- * workgroups finish.
+ * element type; results are rounded once, to nearest even.  Attention in HP_BF16
+ * rounds two values on the way as well, the weights P and the gradients dS of the
+ * scores, which are bfloat16 operands of a matrix product (HP_F32: none).  For equal
+ * inputs the results are the same bits on every call: no sum depends on the order in
+ * which workgroups finish.
  */
 #ifndef HP_OPERATORS_H_
 #define HP_OPERATORS_H_
@@ -213,7 +215,9 @@ int64_t hp_cross_attend_workspace(const hp_attend_args_t *args, int32_t call);
 /* hp_image_ranges - the ranges of a sequence's positions for hp_cross_attend when
  * the states are the image tokens of a token map, packed in its order (what a
  * source buffer of the boundary holds): ranges[2 * (b * seq + p)] and the entry
- * behind it for position p of sample b.  Host memory, no HIP call.
+ * behind it for position p of sample b.  An image has as many states as places in
+ * the sequence; where each place stands for n states, the ranges are n times these.
+ * Host memory, no HIP call.
  *   HP_SEE_SAMPLE:   every image of the sample;
  *   HP_SEE_PREVIOUS: the sample's images that end at or before p;
  *   HP_SEE_LATEST:   the last of these alone.
