@@ -6,6 +6,7 @@ from .binding import (HpError, Plan, hp_backward, hp_backward_accumulate, hp_for
                       hp_forget_tuned_shapes, hp_release_cached_memory, hp_profile_enable, hp_profile_read, hp_set_option, hp_version)
 from .operators import (RotaryScaling, hp_cross_attend, hp_cross_attend_backward, hp_cross_attend_step, hp_cross_attend_workspace,
                         hp_gated_norm, hp_gated_norm_backward, hp_gated_norm_workspace, hp_image_ranges, hp_rotary, hp_rotary_table)
+from .packed import (Packed, hp_pack, hp_packed_attend_step, hp_packed_attend_workspace, hp_packed_linear, hp_unpack)
 from .workloads import Grid, TokenMap
 
 
@@ -38,4 +39,5 @@ def cross_attention(q, k, v, ranges=None, scale=None):
 __all__ = ["rotary", "gated_norm", "cross_attention", "Grid", "TokenMap", "boundary_transform", "Plan", "HpError", "hp_plan_create", "hp_plan_create_host", "hp_plan_create_batched", "hp_plan_create_joined", "hp_plan_tune", "hp_probe_stream", "hp_probe_stream_ex", "hp_release_cached_memory", "hp_forget_tuned_shapes",
            "hp_forward", "hp_forward_static", "hp_zero_image_rows", "hp_text_grads", "hp_backward", "hp_backward_accumulate", "hp_set_option", "hp_get_option", "hp_profile_enable", "hp_profile_read", "hp_version",
            "RotaryScaling", "hp_rotary_table", "hp_rotary", "hp_gated_norm", "hp_gated_norm_backward", "hp_gated_norm_workspace",
-           "hp_cross_attend", "hp_cross_attend_step", "hp_cross_attend_backward", "hp_cross_attend_workspace", "hp_image_ranges"]
+           "hp_cross_attend", "hp_cross_attend_step", "hp_cross_attend_backward", "hp_cross_attend_workspace", "hp_image_ranges",
+           "Packed", "hp_pack", "hp_unpack", "hp_packed_attend_step", "hp_packed_attend_workspace", "hp_packed_linear"]

@@ -13,7 +13,8 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 _ROOT = os.path.dirname(_PKG)
 CSRC = os.path.join(_PKG, "csrc")
 LIB_PATH = os.path.join(_PKG, "libhp.so")
-SOURCES = ["hp_api.hip", "hp_plan.cpp", "hp_attend.hip", "hp_norm.hip", "hp_rotary.hip", "hp_ranges.cpp"]
+SOURCES = ["hp_api.hip", "hp_plan.cpp", "hp_attend.hip", "hp_norm.hip", "hp_rotary.hip", "hp_ranges.cpp",
+           "hp_pack.hip", "hp_packed_attend.hip", "hp_packed_linear.hip"]
 MARSHAL_PATH = os.path.join(_PKG, "hp_marshal.so")
 
 HIPCC_FLAGS = [

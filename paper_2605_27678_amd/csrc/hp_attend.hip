@@ -39,6 +39,7 @@
 #include <type_traits>
 
 #include "hp_device.hpp"
+#include "hp_join.hpp"
 #include "hp_meet.hpp"
 #include "hp_operators.h"
 
@@ -224,8 +225,6 @@ __device__ __forceinline__ void careful_product(Acc (&acc)[DB], const Acc &p, co
 // themselves, from a buffer that begins at the tile's first row, and what lies behind its rows or channels is out of the
 // buffer's bounds and comes as zeros; the caller waits (arrived()) before the barrier behind which the tile is read.
 // Other rows pass through registers at once.
-constexpr uint32_t kOutside = 0x80000000u;
-constexpr int but(int loads) { return (loads & 15) | 0x0f70 | (loads >> 4) << 14; }            // s_waitcnt vmcnt(loads)
 __device__ __forceinline__ void arrived() { __builtin_amdgcn_s_waitcnt(but(0)); }
 // All loads of this wave but those of the last `tiles` tiles, of which it makes EACH a tile.
 template <int EACH> __device__ __forceinline__ void arrived_but(int tiles) {
@@ -675,7 +674,7 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__((kStepWaves<
 // parts are a workgroup's, its waves take every fourth: one wave going through them one behind the other took 45 us of the
 // 54 for one token against 8000 states in 62 parts.  Few are a wave's: 49200 rows and heads of two parts 19 us, with
 // a workgroup each 48.
-constexpr int kMostParts = kWave, kFewParts = 8;
+constexpr int kFewParts = 8;
 template <class T> __global__ __launch_bounds__(kBlock) void attend_join_kernel(Attend p) {
     __shared__ __attribute__((aligned(16))) float half_done[kWaves][HP_ATTEND_MAX_DIM];
     const int lane = (int)threadIdx.x % kWave, wave = (int)threadIdx.x / kWave;
@@ -1207,6 +1206,14 @@ void launch(Kernel what, int dtype, const Attend &p, const dim3 &grid, hipStream
     else launch<float>(what, p, grid, s);
 }
 
+int join(const Attend &p, int dtype, hipStream_t s) {
+    const int64_t items = p.rows * p.heads_q;
+    const uint32_t blocks = (uint32_t)(p.splits <= kFewParts ? (items + kWaves - 1) / kWaves : items);
+    if (dtype == HP_BF16) attend_join_kernel<__bf16><<<blocks, kBlock, 0, s>>>(p);
+    else attend_join_kernel<float><<<blocks, kBlock, 0, s>>>(p);
+    return failed() ? HP_EHIP : HP_OK;
+}
+
 // Forward in either shape: the launch, and the join of the parts.
 int forward(const hp_attend_args_t &a, Kernel what, const dim3 &grid, hipStream_t s) {
     Attend p = params_of(a);
@@ -1217,14 +1224,7 @@ int forward(const hp_attend_args_t &a, Kernel what, const dim3 &grid, hipStream_
     }
     launch(what, a.dtype, p, grid, s);
     if (failed()) return HP_EHIP;
-    if (p.splits > 1) {
-        const int64_t items = p.rows * p.heads_q;
-        const uint32_t blocks = (uint32_t)(p.splits <= kFewParts ? (items + kWaves - 1) / kWaves : items);
-        if (a.dtype == HP_BF16) attend_join_kernel<__bf16><<<blocks, kBlock, 0, s>>>(p);
-        else attend_join_kernel<float><<<blocks, kBlock, 0, s>>>(p);
-        if (failed()) return HP_EHIP;
-    }
-    return HP_OK;
+    return p.splits > 1 ? join(p, a.dtype, s) : HP_OK;
 }
 
 int add_up(const float *part, int splits, int dtype, int64_t rows, int heads, int dim, const hp_heads_t &out, hipStream_t s) {
@@ -1235,6 +1235,13 @@ int add_up(const float *part, int splits, int dtype, int64_t rows, int heads, in
 }
 
 }  // namespace
+
+int hp::join_parts(const Parts &n, int dtype, int64_t rows, int heads_q, int dim, const hp_heads_t &out, float *lse, hipStream_t s) {
+    Attend p{};
+    p.rows = rows, p.heads_q = heads_q, p.dim = dim, p.splits = n.splits, p.out = out, p.lse = lse;
+    p.part = n.products, p.part_lse = n.lse2;
+    return join(p, dtype, s);
+}
 
 extern "C" {
 

@@ -63,6 +63,11 @@ template <int N, class T> __device__ __forceinline__ void put(Vec<T, N> &v, int 
     else v[i] = (T)x;
 }
 
+// Buffers for loads that write LDS themselves, or that bring zeros from beyond the end: an offset that is always outside,
+// and the wait for all of a wave's loads but the last `loads`.
+constexpr uint32_t kOutside = 0x80000000u;
+constexpr int but(int loads) { return (loads & 15) | 0x0f70 | (loads >> 4) << 14; }            // s_waitcnt vmcnt(loads)
+
 __device__ __forceinline__ float wave_sum(float x) {
 #pragma unroll
     for (int d = kWave / 2; d; d /= 2) x += __shfl_xor(x, d);

@@ -10,7 +10,8 @@
 //
 // rotary(), norm(), norm_backward() and attend() do the same for the operators of
 // operators.py, whose checks they repeat: None for whatever is not plainly in
-// order.  In Python they took 11 to 13 us a call.
+// order.  In Python they took 11 to 13 us a call.  pack(), packed_attend() and
+// packed_linear() are those of packed.py.
 #include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -19,6 +20,7 @@
 
 #include "hp.h"
 #include "hp_operators.h"
+#include "hp_packed.h"
 
 namespace {
 
@@ -330,8 +332,102 @@ PyObject *attend(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
     });
 }
 
+// ---- packed states and weights --------------------------------------------------------------------------------------
+
+// A pair (codes, scales) of `rows` rows (negative: any, put there), `heads` heads (0: a matrix's, negative: any, put there)
+// and `dim` channels.
+bool packed_of(PyObject *o, Checks &c, int64_t &rows, int64_t &heads, int64_t dim, hp_packed_t *out) {
+    PyObject *pair[2];
+    if (PyTuple_Check(o)) {                        // a named pair is no plain tuple
+        if (PyTuple_GET_SIZE(o) != 2) return false;
+        pair[0] = PyTuple_GET_ITEM(o, 0), pair[1] = PyTuple_GET_ITEM(o, 1);
+    } else if (entries(o, pair, 2) != 2) {
+        return false;
+    }
+    const int64_t dims = heads == 0 ? 2 : 3, groups = (dim + HP_PACKED_GROUP - 1) / HP_PACKED_GROUP;
+    const at::Tensor *codes = c.take(pair[0], dims, false, false, at::kByte), *scales = c.take(pair[1], dims + 1, false, false, at::kBFloat16);
+    if (!codes || !scales || codes->size(dims - 1) != 16 * groups || scales->size(dims - 1) != groups || scales->size(dims) != 2) return false;
+    if (groups > 1 && scales->stride(dims - 1) != 2) return false;
+    if (rows < 0) rows = codes->size(0);
+    if (heads < 0) heads = codes->size(1);
+    if (codes->size(0) != rows || scales->size(0) != rows || (heads && (codes->size(1) != heads || scales->size(1) != heads))) return false;
+    *out = hp_packed_t{at_of(codes), at_of(scales), codes->stride(0), heads ? codes->stride(1) : 0, scales->stride(0), heads ? scales->stride(1) : 0};
+    return true;
+}
+
+// pack(fn, xs, packed, stream): hp_pack, or hp_unpack with its outputs for xs
+PyObject *pack(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+    return operate(args, n_args, 4, [&](void *fn, void *stream, int *rc) {
+        Checks c;
+        hp_pack_args_t a{};
+        PyObject *xs[HP_PACK_MAX_TENSORS], *packed[HP_PACK_MAX_TENSORS];
+        a.n_tensors = entries(args[1], xs, HP_PACK_MAX_TENSORS);
+        if (a.n_tensors < 1 || entries(args[2], packed, HP_PACK_MAX_TENSORS) != a.n_tensors) return false;
+        for (int i = 0; i < a.n_tensors; ++i) {
+            const at::Tensor *x = c.take(xs[i], -1);
+            if (!x || x->dim() < 2 || x->dim() > 3 || (x->size(x->dim() - 1) > 1 && x->stride(x->dim() - 1) != 1)) return false;
+            const bool matrix = x->dim() == 2;
+            const int64_t dim = x->size(x->dim() - 1);
+            if ((i && (x->size(0) != a.rows || dim != a.dim)) || dim > INT32_MAX || (!matrix && x->size(1) > INT32_MAX)) return false;
+            int64_t rows = x->size(0), heads = matrix ? 0 : x->size(1);
+            if (!matrix && heads == 0) return false;             // no heads: for the way through Python
+            a.rows = rows, a.dim = (int32_t)dim, a.heads[i] = matrix ? 1 : (int32_t)heads;
+            a.x[i] = hp_heads_t{at_of(x), x->stride(0), matrix ? 0 : x->stride(1)};
+            if (!packed_of(packed[i], c, rows, heads, dim, &a.packed[i])) return false;
+        }
+        a.dtype = c.dtype();
+        *rc = without_gil([&] { return ((int (*)(const hp_pack_args_t *, void *))fn)(&a, stream); });
+        return true;
+    });
+}
+
+// packed_attend(fn, q, k, v, ranges, out, lse, scale, workspace, stream)
+PyObject *packed_attend(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+    return operate(args, n_args, 10, [&](void *fn, void *stream, int *rc) {
+        Checks c;
+        hp_packed_attend_args_t a{};
+        const at::Tensor *q = c.take(args[1], 3);
+        if (!q || q->size(1) > INT32_MAX || q->size(2) > INT32_MAX) return false;
+        int64_t keys = -1, heads = -1;
+        if (!packed_of(args[2], c, keys, heads, q->size(2), &a.k) || heads < 1 || heads > INT32_MAX) return false;
+        if (!packed_of(args[3], c, keys, heads, q->size(2), &a.v)) return false;
+        const int64_t pairs[2] = {q->size(0), 2};
+        const at::Tensor *out = c.shaped(args[5], q->sizes());
+        const at::Tensor *ranges = c.shaped(args[4], at::IntArrayRef(pairs, 2), true, true, at::kInt);
+        const at::Tensor *lse = c.shaped(args[6], q->sizes().slice(0, 2), true, true, at::kFloat);
+        if (!c.ok || !scratch_of(args[8], c, &a.workspace, &a.workspace_bytes)) return false;
+        a.dtype = c.dtype(), a.rows = q->size(0), a.keys = keys;
+        a.heads_q = (int32_t)q->size(1), a.heads_k = (int32_t)heads, a.dim = (int32_t)q->size(2);
+        a.scale = (float)(args[7] == Py_None ? std::pow((double)a.dim, -0.5) : PyFloat_AsDouble(args[7]));
+        if (PyErr_Occurred()) return false;
+        a.q = heads_of(q), a.out = heads_of(out);
+        a.ranges = (const int32_t *)at_of(ranges), a.lse = (float *)at_of(lse);
+        *rc = without_gil([&] { return ((int (*)(const hp_packed_attend_args_t *, void *))fn)(&a, stream); });
+        return true;
+    });
+}
+
+// packed_linear(fn, x, w, out, stream)
+PyObject *packed_linear(PyObject *, PyObject *const *args, Py_ssize_t n_args) {
+    return operate(args, n_args, 5, [&](void *fn, void *stream, int *rc) {
+        Checks c;
+        hp_packed_linear_args_t a{};
+        const at::Tensor *x = c.take(args[1], 2);
+        int64_t n_out = -1, heads = 0;
+        if (!x || x->size(1) > INT32_MAX || !packed_of(args[2], c, n_out, heads, x->size(1), &a.w) || n_out > INT32_MAX) return false;
+        const int64_t sizes[2] = {x->size(0), n_out};
+        const at::Tensor *out = c.shaped(args[3], at::IntArrayRef(sizes, 2));
+        if (!out) return false;
+        a.dtype = c.dtype(), a.rows = x->size(0), a.n_in = (int32_t)x->size(1), a.n_out = (int32_t)n_out;
+        a.x = at_of(x), a.x_stride = x->stride(0), a.out = at_of(out), a.out_stride = out->stride(0);
+        *rc = without_gil([&] { return ((int (*)(const hp_packed_linear_args_t *, void *))fn)(&a, stream); });
+        return true;
+    });
+}
+
 #define HP_METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {HP_METHOD(call), HP_METHOD(rotary), HP_METHOD(norm), HP_METHOD(norm_backward), HP_METHOD(attend),
+                         HP_METHOD(pack), HP_METHOD(packed_attend), HP_METHOD(packed_linear),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "hp_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

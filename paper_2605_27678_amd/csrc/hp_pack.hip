@@ -1,0 +1,201 @@
+// Packing rows into groups of 32 values with codes of 4 bits, and back.
+//     low = min, rounded down;  step = (max - low) / 15, rounded up;  code = nearest of low + step * {0 .. 15}, the lower of two
+// A lane takes 8 channels, one word of codes, four lanes a group.  Bound by memory: 2 (or 4) bytes and 0.625 a value.
+#include <cfloat>
+#include <cmath>
+
+#include "hp_packed.hpp"
+
+#pragma clang fp contract(off)
+
+namespace {
+
+using namespace hp;
+
+constexpr int kThreads = 256;
+constexpr int64_t kMostBlocks = 1 << 20;           // of rows; more are taken in turns
+
+struct PackParams {
+    int64_t rows;
+    int32_t dim, words;                            // words of codes a row and head: four a group
+    int32_t heads[HP_PACK_MAX_TENSORS], rows_per_block[HP_PACK_MAX_TENSORS];
+    hp_heads_t x[HP_PACK_MAX_TENSORS];
+    hp_packed_t packed[HP_PACK_MAX_TENSORS];
+};
+
+// A value from another lane of the same four.
+template <int PERM> __device__ __forceinline__ float from_quad(float x) {
+    return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), PERM, 0xf, 0xf, true));
+}
+constexpr int kNext = 0xb1, kOpposite = 0x4e;      // lanes 1 0 3 2 and 2 3 0 1
+__device__ __forceinline__ float quad_min(float x) {
+    x = fminf(x, from_quad<kNext>(x));
+    return fminf(x, from_quad<kOpposite>(x));
+}
+__device__ __forceinline__ float quad_max(float x) {
+    x = fmaxf(x, from_quad<kNext>(x));
+    return fmaxf(x, from_quad<kOpposite>(x));
+}
+
+// The bfloat16 that is next below (or equal), and next above for numbers that are not negative.
+__device__ __forceinline__ float down(float x) {
+    const uint32_t b = __float_as_uint(x);
+    return __uint_as_float((b >> 31 ? b + 0xffffu : b) & 0xffff0000u);
+}
+__device__ __forceinline__ float up(double x) {
+    float f = (float)x;
+    if ((double)f < x) f = __uint_as_float(__float_as_uint(f) + 1);
+    return __uint_as_float((__float_as_uint(f) + 0xffffu) & 0xffff0000u);
+}
+
+// Eight values' codes.  In binary32 u = x - low - code * step is exact where x - low is, and the border is met exactly;
+// where x - low was rounded and u is next to a border, 64 bits decide.
+__device__ __forceinline__ void codes_of(const float (&x)[8], float low, float step, uint32_t (&code)[8]) {
+    const float inv = step > 0.0f ? 1.0f / step : 0.0f, half = 0.5f * step, close = half * (1.0f - 0x1p-16f);
+    float c[8], u[8];
+    bool near = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float t = x[i] - low;
+        c[i] = fminf(rintf(t * inv), 15.0f);
+        u[i] = __builtin_fmaf(-c[i], step, t);
+        near |= fabsf(u[i]) >= close;
+    }
+    if (__any(near)) {
+        bool unsure = false;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float t = x[i] - low;
+            // whichever of x and low is the larger: its test is exact
+            unsure |= fabsf(u[i]) >= close && (t + low != x[i] || x[i] - t != low);
+            if (u[i] > half && c[i] < 15.0f) c[i] += 1.0f;
+            else if (u[i] <= -half && c[i] > 0.0f) c[i] -= 1.0f;
+        }
+        if (__any(unsure)) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const double d = (double)x[i] - (double)low;
+                c[i] = fminf((float)rint(step > 0.0f ? d / (double)step : 0.0), 15.0f);            // x - low may be infinite in binary32
+                const double v = d - (double)c[i] * (double)step;                                  // the product is exact
+                if (v > (double)half && c[i] < 15.0f) c[i] += 1.0f;
+                else if (v <= -(double)half && c[i] > 0.0f) c[i] -= 1.0f;
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) code[i] = (uint32_t)c[i];
+}
+
+template <class T> __global__ __launch_bounds__(kThreads) void pack_kernel(PackParams p) {
+    const int t = (int)blockIdx.z, per_row = p.heads[t] * p.words, rows_per_block = p.rows_per_block[t];
+    const int item = (int)(blockIdx.y * kThreads + threadIdx.x);
+    const int in_block = rows_per_block > 1 ? item / per_row : 0, at_row = item - in_block * per_row;
+    if (in_block >= rows_per_block || at_row >= per_row) return;                 // four lanes of a group alike
+    const int head = at_row / p.words, word = at_row - head * p.words, valid = p.dim - 8 * word;
+    const hp_heads_t &from = p.x[t];
+    const hp_packed_t &to = p.packed[t];
+    for (int64_t row = (int64_t)blockIdx.x * rows_per_block + in_block; row < p.rows; row += (int64_t)gridDim.x * rows_per_block) {
+        const T *src = (const T *)from.data + row * from.row_stride + (int64_t)head * from.head_stride + 8 * word;
+        const Vec<T, 8> v = load<8>(src, valid);
+        float x[8], least = INFINITY, most = -INFINITY;
+        bool fine = true;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x[i] = (float)v[i];
+            if (i >= valid) continue;
+            least = fminf(least, x[i]);
+            most = fmaxf(most, x[i]);
+            fine &= fabsf(x[i]) <= FLT_MAX;
+        }
+        if (!fine) least = -INFINITY;                                            // NaN too, which minima pass over
+        least = quad_min(least), most = quad_max(most);
+        float low = down(least), step = 0.0f;
+        const bool good = low >= -FLT_MAX;
+        if (good) {
+            const double each = ((double)most - (double)low) / 15.0;
+            if (each >= 0x1p-126) step = up(each);
+        } else {
+            low = step = __uint_as_float(0x7fc00000u);
+        }
+        uint32_t code[8] = {}, w = 0;
+        codes_of(x, good ? low : 0.0f, good ? step : 0.0f, code);
+        const bool flat = !good || step == 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w |= (i < valid && !flat ? code[i] : 0u) << (4 * (i / 2) + 16 * (i % 2));
+        ((uint32_t *)((char *)to.codes + row * to.code_row_stride + (int64_t)head * to.code_head_stride))[word] = w;
+        if (word % 4 == 0)
+            ((uint32_t *)((uint16_t *)to.scales + row * to.scale_row_stride + (int64_t)head * to.scale_head_stride))[word / 4] =
+                __float_as_uint(step) >> 16 | (__float_as_uint(low) & 0xffff0000u);
+    }
+}
+
+template <class T> __global__ __launch_bounds__(kThreads) void unpack_kernel(PackParams p) {
+    const int t = (int)blockIdx.z, per_row = p.heads[t] * p.words, rows_per_block = p.rows_per_block[t];
+    const int item = (int)(blockIdx.y * kThreads + threadIdx.x);
+    const int in_block = rows_per_block > 1 ? item / per_row : 0, at_row = item - in_block * per_row;
+    if (in_block >= rows_per_block || at_row >= per_row) return;
+    const int head = at_row / p.words, word = at_row - head * p.words, valid = p.dim - 8 * word;
+    const hp_heads_t &to = p.x[t];
+    const hp_packed_t &from = p.packed[t];
+    for (int64_t row = (int64_t)blockIdx.x * rows_per_block + in_block; row < p.rows; row += (int64_t)gridDim.x * rows_per_block) {
+        const uint32_t w = ((const uint32_t *)((const char *)from.codes + row * from.code_row_stride + (int64_t)head * from.code_head_stride))[word];
+        const uint32_t pair = ((const uint32_t *)((const uint16_t *)from.scales + row * from.scale_row_stride + (int64_t)head * from.scale_head_stride))[word / 4];
+        const float step = step_of(pair), low = low_of(pair);
+        Vec<T, 8> v;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (T)__builtin_fmaf((float)(w >> (4 * (i / 2) + 16 * (i % 2)) & 15u), step, low);
+        store<8>((T *)to.data + row * to.row_stride + (int64_t)head * to.head_stride + 8 * word, v, valid);
+    }
+}
+
+int check(const hp_pack_args_t *a) {
+    if (!a) return HP_EINVAL;
+    if (a->dtype != HP_BF16 && a->dtype != HP_F32) return HP_EINVAL;
+    if (a->n_tensors < 1 || a->n_tensors > HP_PACK_MAX_TENSORS || a->rows < 0) return HP_EINVAL;
+    if (a->dim < 1 || a->dim > HP_PACKED_MAX_DIM) return HP_EINVAL;
+    const int size = a->dtype == HP_BF16 ? 2 : 4;
+    for (int t = 0; t < a->n_tensors; ++t) {
+        if (a->heads[t] < 0 || a->heads[t] > 65536) return HP_EINVAL;
+        const int64_t rows = a->heads[t] > 0 ? a->rows : 0;
+        if (rows > 0 && !a->x[t].data) return HP_EINVAL;
+        if ((uintptr_t)a->x[t].data % size) return HP_EALIGN;
+        if (const int rc = check_packed(a->packed[t], rows, a->heads[t])) return rc;
+    }
+    return HP_OK;
+}
+
+int run(const hp_pack_args_t *a, bool back, hipStream_t stream) {
+    if (const int rc = check(a)) return rc;
+    PackParams p{};
+    p.rows = a->rows, p.dim = a->dim, p.words = 4 * groups_of(a->dim);
+    int64_t blocks = 0, lines = 0;
+    for (int t = 0; t < a->n_tensors; ++t)
+        if ((int64_t)a->heads[t] * p.words > (int64_t)65535 * kThreads) return HP_ELAYOUT;     // blocks of a launch's second axis
+    for (int t = 0; t < a->n_tensors; ++t) {
+        const int64_t per_row = (int64_t)a->heads[t] * p.words;
+        p.heads[t] = a->heads[t], p.x[t] = a->x[t], p.packed[t] = a->packed[t];
+        p.rows_per_block[t] = per_row > 0 && per_row < kThreads ? (int32_t)(kThreads / per_row) : 1;
+        if (per_row == 0) continue;
+        const int64_t b = (a->rows + p.rows_per_block[t] - 1) / p.rows_per_block[t], l = (per_row + kThreads - 1) / kThreads;
+        blocks = b > blocks ? b : blocks, lines = l > lines ? l : lines;
+    }
+    if (blocks == 0) return HP_OK;
+    const dim3 grid((uint32_t)(blocks < kMostBlocks ? blocks : kMostBlocks), (uint32_t)lines, (uint32_t)a->n_tensors);
+    if (a->dtype == HP_BF16) {
+        if (back) unpack_kernel<__bf16><<<grid, kThreads, 0, stream>>>(p);
+        else pack_kernel<__bf16><<<grid, kThreads, 0, stream>>>(p);
+    } else {
+        if (back) unpack_kernel<float><<<grid, kThreads, 0, stream>>>(p);
+        else pack_kernel<float><<<grid, kThreads, 0, stream>>>(p);
+    }
+    return hip_failed(hipGetLastError()) ? HP_EHIP : HP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int hp_pack(const hp_pack_args_t *a, void *stream) { return run(a, false, (hipStream_t)stream); }
+int hp_unpack(const hp_pack_args_t *a, void *stream) { return run(a, true, (hipStream_t)stream); }
+
+}  // extern "C"

@@ -1,0 +1,98 @@
+// What the kernels over packed values share: codes of 4 bits as operands of matrix products.
+//
+// A group's value is low + step * code, so that a sum over its channels is
+//     sum x value = step * sum x code + low * sum x:
+// the matrix units take the codes as they are, which bfloat16 holds exactly, and the step goes over the 4 results that a
+// lane has of 32 channels instead of over the 8 codes that it has unpacked.  Codes become bfloat16 by placing their four
+// bits below the leading one of 16: 0x4180 | code << 3 is 16 + code, two at a time with a shift and an and-or, one
+// instruction a code.  (128 + code would save one shift in eight and cost the sums three more bits to cancel.)  What the
+// 16 adds is taken off again with sum x, which the matrix units make too.
+#pragma once
+
+#include "hp_device.hpp"
+#include "hp_packed.h"
+
+namespace hp {
+
+typedef Vec<__bf16, 8> Frag;
+typedef Vec<float, 4> Quad;
+typedef Vec<uint32_t, 4> Words;
+
+constexpr int kGroup = HP_PACKED_GROUP, kGroupBytes = 16;
+constexpr float kLift = 16.0f;                     // what levels() adds to every code
+
+inline __host__ __device__ int groups_of(int dim) { return (dim + kGroup - 1) / kGroup; }
+
+// The products of 16 x 16 x 32: lane l has, of the left operand, row l % 16, of the right one column l % 16, of both the
+// inner values 8(l / 16) and on, and of the result column l % 16 and rows 4(l / 16) and on.
+__device__ __forceinline__ Quad mma(const Frag &a, const Frag &b, const Quad &c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// A word's eight codes, each lifted by 16: in the order of its channels as hp_pack lays them out.
+__device__ __forceinline__ Frag levels(uint32_t w) {
+    constexpr uint32_t kBits = 0x00780078u, kSixteen = 0x41804180u;
+    union {
+        Words w;
+        Frag f;
+    } u;
+    u.w = Words{(w << 3 & kBits) | kSixteen, (w >> 1 & kBits) | kSixteen, (w >> 5 & kBits) | kSixteen, (w >> 9 & kBits) | kSixteen};
+    return u.f;
+}
+
+__device__ __forceinline__ Frag all_of(float x) {
+    Frag f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = (__bf16)x;
+    return f;
+}
+
+// The two halves of a pair (step, low) as it lies in memory.
+__device__ __forceinline__ float step_of(uint32_t pair) { return __uint_as_float(pair << 16); }
+__device__ __forceinline__ float low_of(uint32_t pair) { return __uint_as_float(pair & 0xffff0000u); }
+
+// Of four lanes l, l + 16, l + 32, l + 48 with four words each: word t of the q-th of them and word q of the t-th change
+// places.
+__device__ __forceinline__ void across_quarters(Words &w) {
+    const auto a = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false), b = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+    const auto c = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false), d = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+    w = Words{c[0], c[1], d[0], d[1]};
+}
+
+// The bfloat16 numbers that stand for a value of type T as an operand: itself, or three that add up to its 24 bits.
+template <class T> constexpr int kTerms = sizeof(T) == 2 ? 1 : 3;
+template <int N> __device__ __forceinline__ void terms(float x, Frag (&f)[N], int i) {
+#pragma unroll
+    for (int t = 0; t < N; ++t) {
+        const __bf16 b = (__bf16)x;
+        f[t][i] = b;
+        x -= (float)b;
+    }
+}
+template <class T> __device__ __forceinline__ void terms(const Vec<T, 8> &x, Frag (&f)[kTerms<T>]) {
+    if constexpr (sizeof(T) == 2) {
+        f[0] = x;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) terms(x[i], f, i);
+    }
+}
+
+constexpr int64_t kMostStride = 1 << 24;           // bytes or elements, of rows: 63 of them stay below kOutside
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void *base) {
+    return __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, 0x7fffffff, 0x00020000);
+}
+
+// What hp_packed_t has to be, for so many rows and heads; strides that no address goes by do not count.
+inline int check_packed(const hp_packed_t &t, int64_t rows, int64_t heads) {
+    if (rows > 0 && heads > 0 && (!t.codes || !t.scales)) return HP_EINVAL;
+    if ((uintptr_t)t.codes % 16 || (uintptr_t)t.scales % 4) return HP_EALIGN;
+    if (rows > 1 && (t.code_row_stride % 16 || t.scale_row_stride % 2)) return HP_EALIGN;
+    if (heads > 1 && (t.code_head_stride % 16 || t.scale_head_stride % 2)) return HP_EALIGN;
+    return HP_OK;
+}
+inline bool short_strides(const hp_packed_t &t, int64_t rows) {
+    return rows <= 1 || (t.code_row_stride >= 0 && t.code_row_stride <= kMostStride && t.scale_row_stride >= 0 && t.scale_row_stride <= kMostStride);
+}
+
+}  // namespace hp

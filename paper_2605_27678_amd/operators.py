@@ -78,8 +78,8 @@ _fast = None            # hp_marshal, or False where it is not used
 _at = {}                # addresses of the calls that go through it
 
 
-def _call(function: str, name: str, *args) -> bool:
-    """The call through hp_marshal.  False if the arguments need a closer look than it takes."""
+def _extension():
+    """hp_marshal, or False."""
     global _fast
     if _fast is None:
         if "torch" not in sys.modules:
@@ -91,7 +91,12 @@ def _call(function: str, name: str, *args) -> bool:
         for f in ("hp_rotary", "hp_gated_norm", "hp_gated_norm_backward", "hp_cross_attend", "hp_cross_attend_step",
                   "hp_cross_attend_backward"):
             _at[f] = C.cast(getattr(L, f), C.c_void_p).value
-    if _fast is False:
+    return _fast
+
+
+def _call(function: str, name: str, *args) -> bool:
+    """The call through hp_marshal.  False if the arguments need a closer look than it takes."""
+    if not _extension():
         return False
     rc = getattr(_fast, function)(_at[name], *args)
     if rc is None:
