@@ -3,10 +3,7 @@
 // A group's value is low + step * code, so that a sum over its channels is
 //     sum x value = step * sum x code + low * sum x:
 // the matrix units take the codes as they are, which bfloat16 holds exactly, and the step goes over the 4 results that a
-// lane has of 32 channels instead of over the 8 codes that it has unpacked.  Codes become bfloat16 by placing their four
-// bits below the leading one of 16: 0x4180 | code << 3 is 16 + code, two at a time with a shift and an and-or, one
-// instruction a code.  (128 + code would save one shift in eight and cost the sums three more bits to cancel.)  What the
-// 16 adds is taken off again with sum x, which the matrix units make too.
+// lane has of 32 channels instead of over the 8 codes that it has unpacked.
 #pragma once
 
 #include "hp_device.hpp"
@@ -19,7 +16,6 @@ typedef Vec<float, 4> Quad;
 typedef Vec<uint32_t, 4> Words;
 
 constexpr int kGroup = HP_PACKED_GROUP, kGroupBytes = 16;
-constexpr float kLift = 16.0f;                     // what levels() adds to every code
 
 inline __host__ __device__ int groups_of(int dim) { return (dim + kGroup - 1) / kGroup; }
 
@@ -29,16 +25,35 @@ __device__ __forceinline__ Quad mma(const Frag &a, const Frag &b, const Quad &c)
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
-// A word's eight codes, each lifted by 16: in the order of its channels as hp_pack lays them out.
-__device__ __forceinline__ Frag levels(uint32_t w) {
-    constexpr uint32_t kBits = 0x00780078u, kSixteen = 0x41804180u;
-    union {
-        Words w;
+// A word's eight codes as an operand of products, kLift more than they are, in the order of their channels.
+//
+// For bfloat16 results a code's four bits go below the leading one of 16: 0x4180 | code << 3 is 16 + code, two at a time with
+// a shift and an and-or, one instruction a code.  (128 + code would save one shift in eight and cost the sums three more bits
+// to cancel.)  What the 16 adds is taken off again with sum x, which the matrix units make too.
+//
+// Binary32 results would feel that the lift cancels (1.8e-6 of their size off instead of 8e-7): there a code less 8 goes
+// through binary32, by the conversion of 4-bit whole numbers, 2.4 instructions a code.
+template <class T> struct Codes;
+template <> struct Codes<__bf16> {
+    static constexpr float kLift = 16.0f;
+    uint32_t sixteen = 0x41804180u;
+    // in a vector register: an and-or takes one constant from a scalar one
+    __device__ __forceinline__ Codes() { asm("" : "+v"(sixteen)); }
+    __device__ __forceinline__ Frag operator()(uint32_t w) const {
+        constexpr uint32_t kBits = 0x00780078u;
+        return __builtin_bit_cast(Frag, Words{(w << 3 & kBits) | sixteen, (w >> 1 & kBits) | sixteen, (w >> 5 & kBits) | sixteen, (w >> 9 & kBits) | sixteen});
+    }
+};
+template <> struct Codes<float> {
+    static constexpr float kLift = -8.0f;
+    __device__ __forceinline__ Frag operator()(uint32_t w) const {
+        const uint32_t twos = w ^ 0x88888888u;
         Frag f;
-    } u;
-    u.w = Words{(w << 3 & kBits) | kSixteen, (w >> 1 & kBits) | kSixteen, (w >> 5 & kBits) | kSixteen, (w >> 9 & kBits) | kSixteen};
-    return u.f;
-}
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = (__bf16)(16.0f * __builtin_amdgcn_cvt_off_f32_i4((int)(twos >> (4 * (i / 2) + 16 * (i % 2)))));
+        return f;
+    }
+};
 
 __device__ __forceinline__ Frag all_of(float x) {
     Frag f;

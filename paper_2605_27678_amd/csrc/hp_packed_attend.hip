@@ -9,9 +9,9 @@
 // each product.  The steps go over a group's 16 x 16 results before they add up.  out^T = V^T P^T has the states as inner
 // values: the transposing LDS load brings a lane 16 states of one channel, in the order in which it has their weights, so
 // that no weight leaves its lane; the weights, times the group's steps, are rounded to bfloat16 (three such numbers in
-// binary32).  What the lift of 16 puts into a product, and 8 more so that codes lie around zero and cancel little, is taken
-// off by a product with -24 throughout, from the very same rounded weights; 8 * sum p step + sum p low come from one more
-// product, whose left rows are the groups' steps and lows.
+// binary32).  What the codes' lift puts into a product, and 8 more so that codes lie around zero and cancel little, is taken
+// off by a product with -24 throughout, from the very same rounded weights (in binary32 they lie there as they are);
+// 8 * sum p step + sum p low come from one more product, whose left rows are the groups' steps and lows.
 #include <climits>
 #include <cmath>
 
@@ -98,8 +98,13 @@ __device__ __forceinline__ float column_sum(float x) {
 
 constexpr float kLag = 8.0f;                       // the maximum is raised when a score passes it by 2^8
 
-template <class T, int GP> __global__ __launch_bounds__(kBlock) void packed_attend_kernel(Params p) {
+// Waves of a SIMD: as many as registers (128, 168 and 256 of them) and LDS (10 KiB a wave for heads of 128) let run.
+template <class T, int GP> constexpr int kResident = sizeof(T) == 2 ? (GP <= 4 ? 4 : 2) : (GP <= 3 ? 3 : 2);
+
+template <class T, int GP> __global__ __launch_bounds__(kBlock, (kResident<T, GP>)) void packed_attend_kernel(Params p) {
     typedef Layout<GP> L;
+    constexpr float kLift = Codes<T>::kLift;
+    constexpr bool kCentred = kLift == -kMiddle;
     constexpr int N = kTerms<T>, kSets = (GP + 3) / 4, kRow = kGroup * GP + 4;
     __shared__ __attribute__((aligned(16))) char lds[kWaves * L::kBytes];
     static_assert(sizeof(lds) >= sizeof(float) * kWaves * kHeads * (kRow + 2), "room for the join");
@@ -115,7 +120,7 @@ template <class T, int GP> __global__ __launch_bounds__(kBlock) void packed_atte
     if (lo >= hi) lo = hi = 0;
 
     // the queries, and the right operand that puts the lows in: for each pair (step, low) of four groups the values
-    // (-16 sum q, sum q), split into three numbers over the quarters
+    // (-lift sum q, sum q), split into three numbers over the quarters
     Frag q[GP][N], sums[kSets] = {};
     const T *q_row = (const T *)p.q.data + row * p.q.row_stride + (int64_t)(head0 + min(col, heads - 1)) * p.q.head_stride;
 #pragma unroll
@@ -151,6 +156,7 @@ template <class T, int GP> __global__ __launch_bounds__(kBlock) void packed_atte
     float top = -INFINITY, sum = 0.0f;
     Quad out[2 * GP] = {}, rest = {};
     const Frag centre = all_of(-kLift - kMiddle);
+    const Codes<T> codes;
     const int n_tiles = (hi - lo + kTile - 1) / kTile;
     const int begin = (int)((int64_t)n_tiles * split / p.splits), end = (int)((int64_t)n_tiles * (split + 1) / p.splits);
     if (begin + wave < end) {
@@ -187,7 +193,7 @@ template <class T, int GP> __global__ __launch_bounds__(kBlock) void packed_atte
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 const int a = (4 * j + t) / GP, g = (4 * j + t) % GP;
-                const Frag c = levels(w[t]);
+                const Frag c = codes(w[t]);
                 Quad d = {};
 #pragma unroll
                 for (int n = 0; n < N; ++n) d = mma(c, q[g][n], d);
@@ -195,7 +201,11 @@ template <class T, int GP> __global__ __launch_bounds__(kBlock) void packed_atte
 #pragma unroll
                 for (int i = 0; i < 4; ++i) s[a][i] += step_of(pairs[i]) * d[i];
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
+        // here, not behind the branch, where all these products' results would have to be kept until then
+#pragma unroll
+        for (int a = 0; a < 4; ++a) asm("" : "+v"(s[a]));
         read();
         if (more) ks.fetch(k_tile, p.k, next, state_head, hi - next, p.groups, lane);
 
@@ -252,6 +262,7 @@ template <class T, int GP> __global__ __launch_bounds__(kBlock) void packed_atte
 #pragma unroll
                 for (int n = 0; n < N; ++n) rest = mma(u.f, weights[b][n], rest);
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
         for (int g = 0; g < GP; ++g) {
@@ -273,14 +284,15 @@ template <class T, int GP> __global__ __launch_bounds__(kBlock) void packed_atte
                 const Pair w = __builtin_amdgcn_ds_read_tr4_b64_v2i32((Lds)(line + 8 * c));
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
-                    const Frag l = levels((uint32_t)w[b]);
+                    const Frag l = codes((uint32_t)w[b]);
 #pragma unroll
                     for (int n = 0; n < N; ++n) {
-                        out[2 * g + c] = mma(centre, weights[b][n], out[2 * g + c]);
+                        if constexpr (!kCentred) out[2 * g + c] = mma(centre, weights[b][n], out[2 * g + c]);
                         out[2 * g + c] = mma(l, weights[b][n], out[2 * g + c]);
                     }
                 }
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
         read();
         if (more) vs.fetch(v_tile, p.v, next, state_head, hi - next, p.groups, lane);

@@ -1,8 +1,9 @@
 // A few rows times a matrix held in 4 bits: out[r][n] = sum_k x[r][k] w[n][k], with a group's value = low + step * code
 //     = sum_g (step_ng sum_k x_rk code_nk + low_ng sum_k x_rk)            (k in group g)
 // The rows of x are the left operand of products of 16 x 16 x 32, a group of 16 rows of w at a time the right one, so that a
-// lane has results of one row of w, whose step and low are its own.  sum x is such a product too, with -16 for every code: it
-// takes off what the codes are lifted by and, times -low / 16, puts the lows in.
+// lane has results of one row of w, whose step and low are its own.  sum x is such a product too, with one number for every
+// code: less their lift.  In bfloat16 it takes the lift off and, times -low / lift, puts the lows in; in binary32 codes are
+// less 8 and not lifted, and it puts low + 8 step in.
 // The waves of a workgroup share out the inner axis, 128 of it at a time, and add up at the end in their order.
 #include <climits>
 #include <cmath>
@@ -76,7 +77,9 @@ template <class T, int NT> __global__ __launch_bounds__(kBlock) void packed_line
         return f;
     };
     Quad acc[NT] = {};
+    constexpr float kLift = Codes<T>::kLift;
     const Frag lift = all_of(-kLift);
+    const Codes<T> codes_of;
     Chunk<T, NT> next;
     if (turn < chunks) next = fetch(turn);
     for (int c = turn; c < chunks; c += p.waves_k) {
@@ -86,8 +89,8 @@ template <class T, int NT> __global__ __launch_bounds__(kBlock) void packed_line
         across_quarters(w);
 #pragma unroll
         for (int j = 0; j < kChunk; ++j) {
-            const Frag l = levels(w[j]);
-            const float step = step_of(f.pairs[j]), low = low_of(f.pairs[j]) * (-1.0f / kLift);
+            const Frag l = codes_of(w[j]);
+            const float step = step_of(f.pairs[j]), low = low_of(f.pairs[j]) * (-1.0f / kLift) + (kLift < 0.0f ? step : 0.0f);
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 Frag a[N];
@@ -95,7 +98,7 @@ template <class T, int NT> __global__ __launch_bounds__(kBlock) void packed_line
                 Quad sum = {};
 #pragma unroll
                 for (int n = 0; n < N; ++n) sum = mma(a[n], lift, sum);
-                Quad d = sum;
+                Quad d = kLift < 0.0f ? Quad{} : sum;
 #pragma unroll
                 for (int n = 0; n < N; ++n) d = mma(a[n], l, d);
 #pragma unroll
