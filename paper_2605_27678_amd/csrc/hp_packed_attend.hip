@@ -6,7 +6,9 @@
 //
 // A wave takes 64 states at a time by itself.  S^T = K Q^T, so that a lane has scores of one head, four states of each 16.
 // Its four words of a 16-byte group change places with those of three other lanes, and it has 8 channels of one state for
-// each product.  The steps go over a group's 16 x 16 results before they add up.  out^T = V^T P^T has the states as inner
+// each product.  The steps go over a group's 16 x 16 results before they add up: each lane reads those of one state, and a
+// multiplication takes them from whichever lane of its row has them.  (Read from LDS by every lane that needs them they were
+// 32 of 56 LDS reads of 16 bytes, and 120 us for 64 requests of 576 to 6404 states.)  out^T = V^T P^T has the states as inner
 // values: the transposing LDS load brings a lane 16 states of one channel, in the order in which it has their weights, so
 // that no weight leaves its lane; the weights, times the group's steps, are rounded to bfloat16 (three such numbers in
 // binary32).  What the codes' lift puts into a product, and 8 more so that codes lie around zero and cancel little, is taken
@@ -14,9 +16,10 @@
 // 8 * sum p step + sum p low come from one more product, whose left rows are the groups' steps and lows.
 #include <climits>
 #include <cmath>
+#include <type_traits>
 
-#include "hp_join.hpp"
 #include "hp_packed.hpp"
+#include "hp_share.hpp"
 
 #pragma clang fp contract(fast)
 
@@ -31,19 +34,25 @@ constexpr float kMiddle = 8.0f;
 
 struct Params {
     int64_t rows, keys;
-    int32_t heads_q, group, groups, dim, splits, head_tiles;
+    int32_t heads_q, group, groups, dim, head_tiles;
+    int32_t units;                                 // of each tile of heads; 0: each row is one
     float scale2;                                  // for exponents of two
     hp_heads_t q, out;
     hp_packed_t k, v;
     const int32_t *ranges;
     float *lse;
-    float *part, *part_lse;                        // [splits][rows * heads_q][dim], [splits][rows * heads_q]
+    // Rows that lie in several units: the unit that has the beginning writes part 1 of its place, the others part 0.
+    // products [heads_k * head_tiles][units][2][part_heads][dim], lse2 the same without dim, rows [rows] first and last unit.
+    float *products, *lse2;
+    int2 *row_units;
+    int32_t part_heads, reserved;
 };
 
 // The 64 states of a wave in LDS: of each tensor codes [64][GP] of 16 bytes, a row's groups turned so that the same group
-// of 8 neighbouring rows lies in different banks, and scales [GP][64] pairs.
+// of 8 neighbouring rows lies in different banks, and scales [64][kPairs] (step, low).
 template <int GP> struct Layout {
-    static constexpr int kCodes = kTile * GP * kGroupBytes, kTensor = kCodes + kTile * GP * 4, kBytes = 2 * kTensor;
+    static constexpr int kPairs = GP == 3 ? 4 : GP;
+    static constexpr int kCodes = kTile * GP * kGroupBytes, kTensor = kCodes + kTile * kPairs * 4, kBytes = 2 * kTensor;
     static __device__ __forceinline__ int slot(int row, int g) {
         if constexpr (GP == 8) return g ^ (row & 7);
         else if constexpr (GP == 4) return g ^ (row >> 1 & 3);
@@ -53,28 +62,36 @@ template <int GP> struct Layout {
     static __device__ __forceinline__ int at(int row, int g) { return (row * GP + slot(row, g)) * kGroupBytes; }
 };
 
-// Brings tiles of one tensor to LDS, 2 GP loads each.
+// Brings tiles of one tensor to LDS.  Load n of a lane is so many rows behind load 0, its group turned the same way: one
+// offset does for all of them (of three groups, which lie across the loads, three).
 template <int GP> struct Loader {
-    uint32_t codes[GP], scales;
+    static constexpr int kPairs = Layout<GP>::kPairs, kLoads = GP + kPairs, kOffsets = GP == 3 ? 3 : 1;
+    uint32_t codes[kOffsets], scales;
     __device__ __forceinline__ void plan(const hp_packed_t &t, int groups, int lane) {
 #pragma unroll
-        for (int n = 0; n < GP; ++n) {
+        for (int n = 0; n < kOffsets; ++n) {
             const int e = n * kWave + lane, row = e / GP, g = Layout<GP>::slot(row, e % GP);     // slot() is its own inverse
             codes[n] = g < groups ? (uint32_t)(row * (int)t.code_row_stride + g * kGroupBytes) : kOutside;
         }
-        scales = (uint32_t)(lane * (int)t.scale_row_stride * 2);
+        const int g = lane % kPairs;
+        scales = g < groups ? (uint32_t)(lane / kPairs * (int)t.scale_row_stride * 2 + 4 * g) : kOutside;
     }
     // left: states from the tile's first on that are seen
-    __device__ __forceinline__ void fetch(char *to, const hp_packed_t &t, int64_t first, int head, int left, int groups, int lane) const {
+    __device__ __forceinline__ void fetch(char *to, const hp_packed_t &t, int64_t first, int head, int left, int lane) const {
         typedef __attribute__((address_space(3))) void *Lds;
         const auto from = buffer_at((const char *)t.codes + first * t.code_row_stride + (int64_t)head * t.code_head_stride);
+        constexpr int kRows = kWave / GP, kPairRows = kWave / kPairs;         // of a load
 #pragma unroll
-        for (int n = 0; n < GP; ++n)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (Lds)(to + n * kWave * 16), 16, (int)((n * kWave + lane) / GP < left ? codes[n] : kOutside), 0, 0, 0);
+        for (int n = 0; n < GP; ++n) {
+            if constexpr (kOffsets == 1)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (Lds)(to + n * kWave * 16), 16, (int)(lane / GP < left - n * kRows ? codes[0] : kOutside), n * kRows * (int)t.code_row_stride, 0, 0);
+            else
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (Lds)(to + n * kWave * 16), 16, (int)((n * kWave + lane) / GP < left ? codes[n % kOffsets] : kOutside), 0, 0, 0);
+        }
         const auto pairs = buffer_at((const uint16_t *)t.scales + first * t.scale_row_stride + (int64_t)head * t.scale_head_stride);
 #pragma unroll
-        for (int g = 0; g < GP; ++g)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(pairs, (Lds)(to + Layout<GP>::kCodes + g * kWave * 4), 4, (int)(lane < left && g < groups ? scales + 4 * g : kOutside), 0, 0, 0);
+        for (int n = 0; n < kPairs; ++n)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(pairs, (Lds)(to + Layout<GP>::kCodes + n * kWave * 4), 4, (int)(lane / kPairs < left - n * kPairRows ? scales : kOutside), n * kPairRows * (int)t.scale_row_stride * 2, 0, 0);
     }
 };
 
@@ -96,10 +113,74 @@ __device__ __forceinline__ float column_sum(float x) {
     return b.x + b.y;
 }
 
+// What a row sees, and the tiles of it: one for rows that see nothing, so that somebody writes their zeros.
+struct Range {
+    int lo, hi;
+    __device__ __forceinline__ int tiles() const { return max(1, (hi - lo + kTile - 1) / kTile); }
+};
+__device__ __forceinline__ Range range_of(const Params &p, int64_t row) {
+    Range r{0, (int)p.keys};
+    if (p.ranges) {
+        r.lo = max(p.ranges[2 * row], 0);
+        r.hi = min(p.ranges[2 * row + 1], (int)p.keys);
+    }
+    if (r.lo >= r.hi) r.lo = r.hi = 0;
+    return r;
+}
+
+// The tiles of a unit: `left` of them, the first of which is the skip-th of `row` and the at-th of all.
+struct Share {
+    int64_t row;
+    int skip, left, at, total, units;
+};
+// All rows' tiles lie one behind the other, and the units take equal shares, whatever the rows' lengths: each wave adds up
+// the lengths for itself, a few rows a lane.
+constexpr int kRowsALane = 8, kMostShared = kRowsALane * kWave;
+__device__ __forceinline__ Share share_of(const Params &p, int unit, int lane) {
+    if (!p.units) return Share{unit, 0, range_of(p, unit).tiles(), 0, 0, 0};
+    const int rows = (int)p.rows, each = (rows + kWave - 1) / kWave, mine = lane * each;
+    int own = 0;
+    for (int i = 0; i < each; ++i)
+        if (mine + i < rows) own += range_of(p, mine + i).tiles();
+    int upto = own;
+#pragma unroll
+    for (int d = 1; d < kWave; d *= 2) {
+        const int before = __shfl_up(upto, d);
+        if (lane >= d) upto += before;
+    }
+    Share s;
+    s.total = __builtin_amdgcn_readlane(upto, kWave - 1);
+    s.units = min(p.units, (s.total + kWaves - 1) / kWaves);       // none with less than a tile for each wave
+    s.at = unit < s.units ? first_of(s.total, unit, s.units) : 0;
+    s.left = unit < s.units ? first_of(s.total, unit + 1, s.units) - s.at : 0;
+    // the lane whose rows have that tile, then the row
+    const int at_lane = __builtin_ctzll(__ballot(upto > s.at));
+    int before = __builtin_amdgcn_readlane(upto - own, at_lane), row = at_lane * each;
+    for (;; ++row) {
+        const int n = range_of(p, row).tiles();
+        if (before + n > s.at) break;
+        before += n;
+    }
+    s.row = row, s.skip = s.at - before;
+    return s;
+}
+
+// x of lane I of this lane's row of 16.
+template <int I> __device__ __forceinline__ float of_lane(float x) {
+    return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), 0x150 + I, 0xf, 0xf, true));
+}
+// f(0) to f(N - 1), as constants.
+template <int N, class F> __device__ __forceinline__ void each(const F &f) {
+    if constexpr (N > 0) {
+        each<N - 1>(f);
+        f(std::integral_constant<int, N - 1>{});
+    }
+}
+
 constexpr float kLag = 8.0f;                       // the maximum is raised when a score passes it by 2^8
 
 // Waves of a SIMD: as many as registers (128, 168 and 256 of them) and LDS (10 KiB a wave for heads of 128) let run.
-template <class T, int GP> constexpr int kResident = sizeof(T) == 2 ? (GP <= 4 ? 4 : 2) : (GP <= 3 ? 3 : 2);
+template <class T, int GP> constexpr int kResident = sizeof(T) == 2 ? (GP <= 4 ? 4 : 2) : (GP <= 2 ? 3 : 2);
 
 template <class T, int GP> __global__ __launch_bounds__(kBlock, (kResident<T, GP>)) void packed_attend_kernel(Params p) {
     typedef Layout<GP> L;
@@ -109,15 +190,40 @@ template <class T, int GP> __global__ __launch_bounds__(kBlock, (kResident<T, GP
     __shared__ __attribute__((aligned(16))) char lds[kWaves * L::kBytes];
     static_assert(sizeof(lds) >= sizeof(float) * kWaves * kHeads * (kRow + 2), "room for the join");
     const int tid = (int)threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), col = lane % 16, quarter = lane / 16;
-    const int64_t row = blockIdx.x;
-    const int state_head = (int)blockIdx.y / p.head_tiles, first_head = ((int)blockIdx.y % p.head_tiles) * kHeads, split = (int)blockIdx.z;
+    const int unit = (int)blockIdx.x, state_head = (int)blockIdx.y / p.head_tiles, first_head = ((int)blockIdx.y % p.head_tiles) * kHeads;
     const int heads = min(p.group - first_head, kHeads), head0 = state_head * p.group + first_head;
-    int lo = 0, hi = (int)p.keys;
-    if (p.ranges) {
-        lo = max(p.ranges[2 * row], 0);
-        hi = min(p.ranges[2 * row + 1], (int)p.keys);
+    char *const k_tile = lds + wave * L::kBytes, *const v_tile = k_tile + L::kTensor;
+    const uint32_t *const k_scales = (const uint32_t *)(k_tile + L::kCodes), *const v_scales = (const uint32_t *)(v_tile + L::kCodes);
+    Loader<GP> ks, vs;
+    ks.plan(p.k, p.groups, lane);
+    vs.plan(p.v, p.groups, lane);
+    // a wave's tiles are its own: no barriers, only its own loads to wait for and its own reads to finish
+    const auto settle = [] {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    };
+    const auto read = [&] {
+        __builtin_amdgcn_s_waitcnt(0xc07f);        // lgkmcnt(0)
+        settle();
+    };
+    // of a quarter's states 16 a + 4 quarter + i, a and i < 4, lane 4 a + i has the steps and brings the transposed codes
+    const int own = 16 * (col / 4) + 4 * quarter + col % 4;
+    const Frag centre = all_of(-kLift - kMiddle);
+    const Codes<T> codes;
+
+    Share share = share_of(p, unit, lane);
+  for (; share.left > 0; ++share.row, share.skip = 0) {
+    const int64_t row = share.row;
+    const Range see = range_of(p, row);
+    const int lo = see.lo, hi = see.hi, n_tiles = see.tiles();
+    const int begin = share.skip, end = min(n_tiles, begin + share.left);
+    share.left -= end - begin;
+    const bool whole = begin == 0 && end == n_tiles;
+    if (p.units && begin == 0 && blockIdx.y == 0 && tid == 0) {
+        const int first = share.at;                // its place among all tiles
+        p.row_units[row] = make_int2(unit, whole ? unit : unit_of(share.total, first + n_tiles - 1, share.units));
     }
-    if (lo >= hi) lo = hi = 0;
+    share.at += end - begin;
 
     // the queries, and the right operand that puts the lows in: for each pair (step, low) of four groups the values
     // (-lift sum q, sum q), split into three numbers over the quarters
@@ -138,76 +244,51 @@ template <class T, int GP> __global__ __launch_bounds__(kBlock, (kResident<T, GP
         sums[g / 4][2 * (g % 4) + 1] = (__bf16)part;
     }
 
-    char *const k_tile = lds + wave * L::kBytes, *const v_tile = k_tile + L::kTensor;
-    const uint32_t *const k_scales = (const uint32_t *)(k_tile + L::kCodes), *const v_scales = (const uint32_t *)(v_tile + L::kCodes);
-    Loader<GP> ks, vs;
-    ks.plan(p.k, p.groups, lane);
-    vs.plan(p.v, p.groups, lane);
-    // a wave's tiles are its own: no barriers, only its own loads to wait for and its own reads to finish
-    const auto settle = [] {
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-    };
-    const auto read = [&] {
-        __builtin_amdgcn_s_waitcnt(0xc07f);        // lgkmcnt(0)
-        settle();
-    };
-
     float top = -INFINITY, sum = 0.0f;
     Quad out[2 * GP] = {}, rest = {};
-    const Frag centre = all_of(-kLift - kMiddle);
-    const Codes<T> codes;
-    const int n_tiles = (hi - lo + kTile - 1) / kTile;
-    const int begin = (int)((int64_t)n_tiles * split / p.splits), end = (int)((int64_t)n_tiles * (split + 1) / p.splits);
     if (begin + wave < end) {
         const int key0 = lo + (begin + wave) * kTile;
-        ks.fetch(k_tile, p.k, key0, state_head, hi - key0, p.groups, lane);
-        vs.fetch(v_tile, p.v, key0, state_head, hi - key0, p.groups, lane);
+        ks.fetch(k_tile, p.k, key0, state_head, hi - key0, lane);
+        vs.fetch(v_tile, p.v, key0, state_head, hi - key0, lane);
     }
     for (int tile = begin + wave; tile < end; tile += kWaves) {
         const int key0 = lo + tile * kTile, next = key0 + kWaves * kTile;
         const bool more = tile + kWaves < end;
-        __builtin_amdgcn_s_waitcnt(but(2 * GP));   // all but V's
+        __builtin_amdgcn_s_waitcnt(but(Loader<GP>::kLoads));   // all but V's
         settle();
         Quad s[4];
+        const Vec<uint32_t, L::kPairs> k_pairs = *(const Vec<uint32_t, L::kPairs> *)(k_scales + L::kPairs * own);
 #pragma unroll
         for (int a = 0; a < 4; ++a) {
             s[a] = Quad{};
+            const Vec<uint32_t, L::kPairs> pairs = *(const Vec<uint32_t, L::kPairs> *)(k_scales + L::kPairs * (16 * a + col));
 #pragma unroll
             for (int h = 0; h < kSets; ++h) {
-                union {
-                    Words w;
-                    Frag f;
-                } u;
+                Words w = {};
 #pragma unroll
-                for (int j = 0; j < 4; ++j) u.w[j] = 4 * h + j < GP ? k_scales[(4 * h + j) * kTile + 16 * a + col] : 0u;
-                s[a] = mma(u.f, sums[h], s[a]);
+                for (int j = 0; j < 4 && 4 * h + j < L::kPairs; ++j) w[j] = pairs[4 * h + j];
+                s[a] = mma(__builtin_bit_cast(Frag, w), sums[h], s[a]);
             }
         }
-#pragma unroll
-        for (int j = 0; j < GP; ++j) {
+        each<GP>([&](auto j) {
             // pieces 4j .. 4j + 3 of this column's four states of GP groups, one a quarter
             const int mine = 4 * j + quarter;
             Words w = *(const Words *)(k_tile + L::at(16 * (mine / GP) + col, mine % GP));
             across_quarters(w);
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const int a = (4 * j + t) / GP, g = (4 * j + t) % GP;
-                const Frag c = codes(w[t]);
+            each<4>([&](auto t) {
+                constexpr int a = (4 * j + t) / GP, g = (4 * j + t) % GP;
+                const Frag c = codes(w[t.value]);
                 Quad d = {};
 #pragma unroll
                 for (int n = 0; n < N; ++n) d = mma(c, q[g][n], d);
-                const Words pairs = *(const Words *)(k_scales + g * kTile + 16 * a + 4 * quarter);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) s[a][i] += step_of(pairs[i]) * d[i];
-            }
-            __builtin_amdgcn_sched_barrier(0);
-        }
+                each<4>([&](auto i) { s[a][i.value] += of_lane<4 * a + i>(step_of(k_pairs[g])) * d[i.value]; });
+            });
+        });
         // here, not behind the branch, where all these products' results would have to be kept until then
 #pragma unroll
         for (int a = 0; a < 4; ++a) asm("" : "+v"(s[a]));
         read();
-        if (more) ks.fetch(k_tile, p.k, next, state_head, hi - next, p.groups, lane);
+        if (more) ks.fetch(k_tile, p.k, next, state_head, hi - next, lane);
 
         if (key0 + kTile > hi)
 #pragma unroll
@@ -238,47 +319,41 @@ template <class T, int GP> __global__ __launch_bounds__(kBlock, (kResident<T, GP
                 sum += s[a][i];
             }
 
-        if (more) __builtin_amdgcn_s_waitcnt(but(2 * GP));
+        if (more) __builtin_amdgcn_s_waitcnt(but(Loader<GP>::kLoads));
         else __builtin_amdgcn_s_waitcnt(but(0));
         settle();
         // 8 sum p step + sum p low: row 2g of the left operand has group g's steps, row 2g + 1 its lows
         {
-            const uint32_t *line = v_scales + min(col / 2, GP - 1) * kTile + 4 * quarter;
-            const uint32_t half = col % 2 ? 0x07060302u : 0x05040100u;
-            Frag weights[2][N];
+            typedef short Four __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) Four *Lds;
+            // 16 lanes bring four states' pairs, 8 bytes a lane; beyond a state's pairs rows of the product are not read
+            const uint32_t *line = v_scales + L::kPairs * (4 * quarter + col / 4) + 2 * (col % 4 % (L::kPairs / 2));
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
-                const Words even = *(const Words *)(line + 32 * b), odd = *(const Words *)(line + 32 * b + 16);
-                union {
-                    Words w;
-                    Frag f;
-                } u;
+                const Four even = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(line + L::kPairs * 32 * b)), odd = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(line + L::kPairs * (32 * b + 16)));
+                const Frag pairs = __builtin_bit_cast(Frag, __builtin_shufflevector(even, odd, 0, 1, 2, 3, 4, 5, 6, 7));
+                Frag weights[N];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    u.w[i] = __builtin_amdgcn_perm(odd[i], even[i], half);
-                    terms(s[2 * b][i], weights[b], 2 * i);
-                    terms(s[2 * b + 1][i], weights[b], 2 * i + 1);
+                    terms(s[2 * b][i], weights, i);
+                    terms(s[2 * b + 1][i], weights, 4 + i);
                 }
 #pragma unroll
-                for (int n = 0; n < N; ++n) rest = mma(u.f, weights[b][n], rest);
+                for (int n = 0; n < N; ++n) rest = mma(pairs, weights[n], rest);
             }
-            __builtin_amdgcn_sched_barrier(0);
         }
-#pragma unroll
-        for (int g = 0; g < GP; ++g) {
+        const Vec<uint32_t, L::kPairs> v_pairs = *(const Vec<uint32_t, L::kPairs> *)(v_scales + L::kPairs * own);
+        each<GP>([&](auto g) {
             Frag weights[2][N];
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const Words even = *(const Words *)(v_scales + g * kTile + 32 * b + 4 * quarter), odd = *(const Words *)(v_scales + g * kTile + 32 * b + 16 + 4 * quarter);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    terms(s[2 * b][i] * step_of(even[i]), weights[b], 2 * i);
-                    terms(s[2 * b + 1][i] * step_of(odd[i]), weights[b], 2 * i + 1);
-                }
-            }
+            each<8>([&](auto e) {
+                constexpr int b = e / 4, i = e % 4;
+                const float step = step_of(v_pairs[g.value]);
+                terms(of_lane<8 * b + i>(step) * s[2 * b][i], weights[b], 2 * i);
+                terms(of_lane<8 * b + 4 + i>(step) * s[2 * b + 1][i], weights[b], 2 * i + 1);
+            });
             typedef int Pair __attribute__((ext_vector_type(2)));
             typedef __attribute__((address_space(3))) Pair *Lds;
-            const char *line = v_tile + L::at(16 * (col / 4) + 4 * quarter + col % 4, g);      // the 16 lanes of a quarter: its states
+            const char *line = v_tile + L::at(own, g);
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 const Pair w = __builtin_amdgcn_ds_read_tr4_b64_v2i32((Lds)(line + 8 * c));
@@ -292,10 +367,9 @@ template <class T, int GP> __global__ __launch_bounds__(kBlock, (kResident<T, GP
                     }
                 }
             }
-            __builtin_amdgcn_sched_barrier(0);
-        }
+        });
         read();
-        if (more) vs.fetch(v_tile, p.v, next, state_head, hi - next, p.groups, lane);
+        if (more) vs.fetch(v_tile, p.v, next, state_head, hi - next, lane);
     }
     sum = column_sum(sum);
 
@@ -325,14 +399,14 @@ template <class T, int GP> __global__ __launch_bounds__(kBlock, (kResident<T, GP
                 join[(wave * kHeads + col) * kRow + kGroup * g + 16 * c + 8 * (quarter / 2) + 2 * i + quarter % 2] = (out[2 * g + c][i] + more) * share;
     }
     __syncthreads();
-    const int64_t n = p.rows * p.heads_q, out_row = row * p.heads_q + head0;
+    const int64_t part = ((int64_t)blockIdx.y * p.units + unit) * 2 + (begin == 0);
     for (int e = tid; e < heads * 8 * GP; e += kBlock) {
         const int m = e / (8 * GP), d = 4 * (e % (8 * GP));
         if (d >= p.dim) continue;
         Quad v = {};
         for (int w = 0; w < kWaves; ++w) v += *(const Quad *)(join + (w * kHeads + m) * kRow + d);
-        if (p.splits > 1) {
-            store<4>(p.part + (split * n + out_row + m) * p.dim + d, v, p.dim - d);
+        if (!whole) {
+            store<4>(p.products + (part * p.part_heads + m) * p.dim + d, v, p.dim - d);
         } else {
             Vec<T, 4> o;
 #pragma unroll
@@ -341,9 +415,53 @@ template <class T, int GP> __global__ __launch_bounds__(kBlock, (kResident<T, GP
         }
     }
     if (wave == 0 && quarter == 0 && col < heads) {
-        if (p.splits > 1) p.part_lse[split * n + out_row + col] = lse2;
-        else if (p.lse) p.lse[out_row + col] = lse2 * kLn2;
+        if (!whole) p.lse2[part * p.part_heads + col] = lse2;
+        else if (p.lse) p.lse[row * p.heads_q + head0 + col] = lse2 * kLn2;
     }
+    __syncthreads();                               // the next row's tiles come where this was
+  }
+}
+
+// Joins the parts of rows that lie in several units: a workgroup for a row and head, whose waves take every fourth part.
+template <class T> __global__ __launch_bounds__(kBlock) void packed_join_kernel(Params p) {
+    __shared__ __attribute__((aligned(16))) float shared[kWaves][HP_ATTEND_MAX_DIM];
+    const int lane = (int)threadIdx.x % kWave, wave = (int)threadIdx.x / kWave;
+    const int64_t row = blockIdx.x;
+    const int2 units = p.row_units[row];
+    if (units.x == units.y) return;                // written as it was made
+    const int head = (int)blockIdx.y, state_head = head / p.group, in_group = head - state_head * p.group;
+    const int64_t line = (int64_t)(state_head * p.head_tiles + in_group / kHeads) * p.units;
+    const auto part = [&](int u) { return ((line + u) * 2 + (u == units.x)) * p.part_heads + in_group % kHeads; };
+    float top = -INFINITY;
+    for (int u = units.x + lane; u <= units.y; u += kWave) top = fmaxf(top, p.lse2[part(u)]);
+#pragma unroll
+    for (int d = kWave / 2; d; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
+    // nothing seen in a part: no weight; NaN stays
+    const auto weight = [&](int u) {
+        const float t = p.lse2[part(u)];
+        return t == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(t - top);
+    };
+    float sum = 0.0f;
+    for (int u = units.x + lane; u <= units.y; u += kWave) sum += weight(u);
+    sum = wave_sum(sum);
+    Quad acc = {};
+    const int d = 4 * lane;
+#pragma unroll 4
+    for (int u = units.x + wave; u <= units.y; u += kWaves) {
+        const float w = weight(u);
+        const Quad v = load<4>(p.products + part(u) * p.dim + d, p.dim - d);
+        if (w != 0.0f) acc += w * v;
+    }
+    *(Quad *)&shared[wave][d] = acc;
+    __syncthreads();
+    if (wave) return;
+    for (int w = 1; w < kWaves; ++w) acc += *(const Quad *)&shared[w][d];
+    const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+    Vec<T, 4> o;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) o[t] = (T)(acc[t] * inv);
+    store<4>((T *)p.out.data + row * p.out.row_stride + (int64_t)head * p.out.head_stride + d, o, p.dim - d);
+    if (p.lse && lane == 0) p.lse[row * p.heads_q + head] = sum == 0.0f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
 // ---- host ------------------------------------------------------------------------------------------------------
@@ -352,14 +470,17 @@ int64_t align16(int64_t n) { return (n + 15) / 16 * 16; }
 
 int head_tiles_of(const hp_packed_attend_args_t &a) { return (a.heads_q / a.heads_k + kHeads - 1) / kHeads; }
 
-// Parts of each row's range.
-int32_t splits_of(const hp_packed_attend_args_t &a) {
-    const int64_t each = a.rows * a.heads_k * head_tiles_of(a);
-    if (each == 0) return 1;
-    const int64_t want = (each <= kComputeUnits / 2 ? 2 * kComputeUnits : 8 * kComputeUnits) / each;
-    const int64_t most = a.keys / (kWaves * kTile) < kMostParts ? a.keys / (kWaves * kTile) : kMostParts;
-    const int64_t n = want < most ? want : most;
-    return (int32_t)(n < 1 ? 1 : n);
+// Units of each tile of heads: as many as run at once, or, of few heads' rows each, four times as many workgroups.  0: the
+// rows are enough by themselves, or too many to be added up.
+int32_t units_of(const hp_packed_attend_args_t &a) {
+    const int64_t columns = (int64_t)a.heads_k * head_tiles_of(a), tiles = a.keys / kTile + 1;
+    if (a.rows > kMostShared || a.rows * tiles > INT_MAX) return 0;
+    const int64_t groups = groups_of(a.dim), resident = a.dtype == HP_BF16 ? (groups <= 4 ? 4 : 2) : (groups <= 2 ? 3 : 2);
+    const int64_t slots = kComputeUnits * resident;
+    int64_t units = slots / columns;
+    if (units < 4) units = (4 * slots + columns - 1) / columns;
+    const int64_t most = (a.rows * tiles + kWaves - 1) / kWaves;
+    return (int32_t)(units < most ? units : most);
 }
 
 int check_sizes(const hp_packed_attend_args_t *a) {
@@ -373,9 +494,11 @@ int check_sizes(const hp_packed_attend_args_t *a) {
     return HP_OK;
 }
 
+int part_heads_of(const hp_packed_attend_args_t &a) { return a.heads_q / a.heads_k < kHeads ? a.heads_q / a.heads_k : kHeads; }
+
 int64_t workspace_of(const hp_packed_attend_args_t &a) {
-    const int64_t splits = splits_of(a), outs = a.rows * a.heads_q;
-    return splits > 1 ? align16(4 * splits * outs) + 4 * splits * outs * a.dim : 0;
+    const int64_t units = a.rows > 0 ? units_of(a) : 0, parts = 2 * units * a.heads_k * head_tiles_of(a) * part_heads_of(a);
+    return units > 0 ? align16(4 * parts * a.dim) + align16(4 * parts) + align16(8 * a.rows) : 0;
 }
 
 int check(const hp_packed_attend_args_t *a) {
@@ -419,19 +542,23 @@ int hp_packed_attend_step(const hp_packed_attend_args_t *a, void *stream) {
     Params p{};
     p.rows = a->rows, p.keys = a->keys;
     p.heads_q = a->heads_q, p.group = a->heads_q / a->heads_k, p.groups = groups_of(a->dim), p.dim = a->dim;
-    p.splits = splits_of(*a), p.head_tiles = head_tiles_of(*a);
+    p.units = units_of(*a), p.head_tiles = head_tiles_of(*a), p.part_heads = part_heads_of(*a);
     p.scale2 = a->scale * kLog2e;
     p.q = a->q, p.out = a->out, p.k = a->k, p.v = a->v, p.ranges = a->ranges, p.lse = a->lse;
-    if (p.splits > 1) {
-        p.part_lse = (float *)a->workspace;
-        p.part = (float *)((char *)a->workspace + align16(4 * p.splits * p.rows * p.heads_q));
-    }
-    const dim3 grid((uint32_t)p.rows, (uint32_t)(a->heads_k * p.head_tiles), (uint32_t)p.splits);
+    const int64_t parts = (int64_t)2 * p.units * a->heads_k * p.head_tiles * p.part_heads;
+    char *ws = (char *)a->workspace;
+    p.products = (float *)ws;
+    p.lse2 = (float *)(ws + align16(4 * parts * p.dim));
+    p.row_units = (int2 *)(ws + align16(4 * parts * p.dim) + align16(4 * parts));
+    const dim3 grid((uint32_t)(p.units ? p.units : p.rows), (uint32_t)(a->heads_k * p.head_tiles));
     if (a->dtype == HP_BF16) launch<__bf16>(p, grid, s);
     else launch<float>(p, grid, s);
     if (hip_failed(hipGetLastError())) return HP_EHIP;
-    if (p.splits == 1) return HP_OK;
-    return join_parts(Parts{p.part, p.part_lse, p.splits}, a->dtype, p.rows, p.heads_q, p.dim, p.out, p.lse, s);
+    if (p.units <= 1) return HP_OK;                // no row has parts
+    const dim3 joins((uint32_t)p.rows, (uint32_t)p.heads_q);
+    if (a->dtype == HP_BF16) packed_join_kernel<__bf16><<<joins, kBlock, 0, s>>>(p);
+    else packed_join_kernel<float><<<joins, kBlock, 0, s>>>(p);
+    return hip_failed(hipGetLastError()) ? HP_EHIP : HP_OK;
 }
 
 }  // extern "C"
