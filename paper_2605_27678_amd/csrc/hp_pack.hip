@@ -42,48 +42,50 @@ __device__ __forceinline__ float down(float x) {
     const uint32_t b = __float_as_uint(x);
     return __uint_as_float((b >> 31 ? b + 0xffffu : b) & 0xffff0000u);
 }
+__device__ __forceinline__ float up(float x) { return __uint_as_float((__float_as_uint(x) + 0xffffu) & 0xffff0000u); }
 __device__ __forceinline__ float up(double x) {
     float f = (float)x;
     if ((double)f < x) f = __uint_as_float(__float_as_uint(f) + 1);
-    return __uint_as_float((__float_as_uint(f) + 0xffffu) & 0xffff0000u);
+    return up(f);
 }
 
-// Eight values' codes.  In binary32 u = x - low - code * step is exact where x - low is, and the border is met exactly;
-// where x - low was rounded and u is next to a border, 64 bits decide.
-__device__ __forceinline__ void codes_of(const float (&x)[8], float low, float step, uint32_t (&code)[8]) {
-    const float inv = step > 0.0f ? 1.0f / step : 0.0f, half = 0.5f * step, close = half * (1.0f - 0x1p-16f);
-    float c[8], u[8];
-    bool near = false;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float t = x[i] - low;
-        c[i] = fminf(rintf(t * inv), 15.0f);
-        u[i] = __builtin_fmaf(-c[i], step, t);
-        near |= fabsf(u[i]) >= close;
-    }
-    if (__any(near)) {
-        bool unsure = false;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float t = x[i] - low;
-            // whichever of x and low is the larger: its test is exact
-            unsure |= fabsf(u[i]) >= close && (t + low != x[i] || x[i] - t != low);
-            if (u[i] > half && c[i] < 15.0f) c[i] += 1.0f;
-            else if (u[i] <= -half && c[i] > 0.0f) c[i] -= 1.0f;
-        }
-        if (__any(unsure)) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const double d = (double)x[i] - (double)low;
-                c[i] = fminf((float)rint(step > 0.0f ? d / (double)step : 0.0), 15.0f);            // x - low may be infinite in binary32
-                const double v = d - (double)c[i] * (double)step;                                  // the product is exact
-                if (v > (double)half && c[i] < 15.0f) c[i] += 1.0f;
-                else if (v <= -(double)half && c[i] > 0.0f) c[i] -= 1.0f;
-            }
-        }
-    }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) code[i] = (uint32_t)c[i];
+struct Scale {
+    float step, low;
+    bool plain;                                    // the borders low + (k + 1/2) step are exact in binary32
+};
+
+// Where step and low are not too far apart, low + 15 step and the borders between the levels are sums of two numbers of 13
+// bits and 8 that binary32 holds exactly, and comparing with them decides as the definition does; elsewhere (a low value
+// that is less than 2^-12 of a step but not zero, or more than 2^14 steps) 64 bits do.
+__device__ __forceinline__ Scale scale_of(float least, float most) {
+    Scale s;
+    s.low = down(least);
+    const float d = most - s.low, about = d * (1.0f / 15.0f);
+    float step = up(about);
+    const float lower = __uint_as_float(__float_as_uint(step) - 0x10000u), higher = __uint_as_float(__float_as_uint(step) + 0x10000u);
+    s.step = __builtin_fmaf(15.0f, lower, s.low) >= most ? lower : __builtin_fmaf(15.0f, step, s.low) >= most ? step : higher;
+    const float size = fabsf(s.low);
+    s.plain = d >= 0x1p-100f && d <= 0x1p100f && (size == 0.0f || (size >= 0x1p-12f * s.step && size <= 0x1p14f * s.step));
+    if (d == 0.0f) s.step = 0.0f, s.plain = true;
+    return s;
+}
+__device__ __forceinline__ float careful_step(float low, float most) {
+    const double each = ((double)most - (double)low) / 15.0;
+    return each >= 0x1p-126 ? up(each) : 0.0f;
+}
+
+// A code is the level below a value, found roughly, and one more if the value lies beyond the border behind that level.
+__device__ __forceinline__ uint32_t code_of(float x, const Scale &s, float inv, float from, float border) {
+    const float below = floorf(__builtin_fmaf(x, inv, from));
+    return (uint32_t)(int)below + (x > __builtin_fmaf(below, s.step, border) ? 1u : 0u);
+}
+__device__ __forceinline__ uint32_t careful_code(float x, float low, float step) {
+    const double d = (double)x - (double)low, half = 0.5 * (double)step;
+    double c = fmin(rint(d / (double)step), 15.0);
+    const double v = d - c * (double)step;          // the product is exact
+    if (v > half && c < 15.0) c += 1.0;
+    else if (v <= -half && c > 0.0) c -= 1.0;
+    return (uint32_t)c;
 }
 
 template <class T> __global__ __launch_bounds__(kThreads) void pack_kernel(PackParams p) {
@@ -97,31 +99,33 @@ template <class T> __global__ __launch_bounds__(kThreads) void pack_kernel(PackP
     for (int64_t row = (int64_t)blockIdx.x * rows_per_block + in_block; row < p.rows; row += (int64_t)gridDim.x * rows_per_block) {
         const T *src = (const T *)from.data + row * from.row_stride + (int64_t)head * from.head_stride + 8 * word;
         const Vec<T, 8> v = load<8>(src, valid);
-        float x[8], least = INFINITY, most = -INFINITY;
-        bool fine = true;
+        float x[8], least = INFINITY, most = -INFINITY, none = 0.0f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             x[i] = (float)v[i];
-            if (i >= valid) continue;
-            least = fminf(least, x[i]);
-            most = fmaxf(most, x[i]);
-            fine &= fabsf(x[i]) <= FLT_MAX;
+            none = __builtin_fmaf(x[i], 0.0f, none);                             // NaN if any is infinite or NaN
+            least = fminf(least, valid > 7 || i < valid ? x[i] : INFINITY);
+            most = fmaxf(most, valid > 7 || i < valid ? x[i] : -INFINITY);
         }
-        if (!fine) least = -INFINITY;                                            // NaN too, which minima pass over
+        if (!(none == 0.0f)) least = -INFINITY;
         least = quad_min(least), most = quad_max(most);
-        float low = down(least), step = 0.0f;
-        const bool good = low >= -FLT_MAX;
-        if (good) {
-            const double each = ((double)most - (double)low) / 15.0;
-            if (each >= 0x1p-126) step = up(each);
-        } else {
-            low = step = __uint_as_float(0x7fc00000u);
-        }
-        uint32_t code[8] = {}, w = 0;
-        codes_of(x, good ? low : 0.0f, good ? step : 0.0f, code);
-        const bool flat = !good || step == 0.0f;
+        Scale s = scale_of(least, most);
+        if (valid < 8)                                                           // channels that are not there: code 0
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w |= (i < valid && !flat ? code[i] : 0u) << (4 * (i / 2) + 16 * (i % 2));
+            for (int i = 0; i < 8; ++i) x[i] = i < valid ? x[i] : s.low;
+        const bool good = s.low >= -FLT_MAX;
+        uint32_t w = 0;
+        if (__all(s.plain || !good)) {
+            const float inv = s.step > 0.0f ? __builtin_amdgcn_rcpf(s.step) : 0.0f, from = -s.low * inv, border = __builtin_fmaf(0.5f, s.step, s.low);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w |= code_of(x[i], s, inv, from, border) << (4 * (i / 2) + 16 * (i % 2));
+        } else {
+            if (good) s.step = careful_step(s.low, most);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w |= (s.step > 0.0f ? careful_code(x[i], s.low, s.step) : 0u) << (4 * (i / 2) + 16 * (i % 2));
+        }
+        if (!good) s.low = s.step = __uint_as_float(0x7fc00000u), w = 0;
+        const float low = s.low, step = s.step;
         ((uint32_t *)((char *)to.codes + row * to.code_row_stride + (int64_t)head * to.code_head_stride))[word] = w;
         if (word % 4 == 0)
             ((uint32_t *)((uint16_t *)to.scales + row * to.scale_row_stride + (int64_t)head * to.scale_head_stride))[word / 4] =

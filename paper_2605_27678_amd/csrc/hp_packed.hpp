@@ -93,9 +93,28 @@ template <class T> __device__ __forceinline__ void terms(const Vec<T, 8> &x, Fra
     }
 }
 
+// What a wave brings to LDS is its own: no barriers, only its own loads to wait for, and its own reads to finish before the
+// next loads write there.
+__device__ __forceinline__ void settle() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+__device__ __forceinline__ void reads_done() {
+    __builtin_amdgcn_s_waitcnt(0xc07f);            // lgkmcnt(0)
+    settle();
+}
+
 constexpr int64_t kMostStride = 1 << 24;           // bytes or elements, of rows: 63 of them stay below kOutside
+// Loads of a wave that write LDS: 16 or 4 bytes a lane from `offset` (the lane's) and `more` (the wave's) bytes behind
+// `base`, one lane's behind the other from `to`; zeros for lanes with kOutside.
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_at(const void *base) {
     return __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, 0x7fffffff, 0x00020000);
+}
+__device__ __forceinline__ void pieces_to_lds(const void *base, char *to, uint32_t offset, int more) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer_at(base), (__attribute__((address_space(3))) void *)to, 16, (int)offset, more, 0, 0);
+}
+__device__ __forceinline__ void words_to_lds(const void *base, char *to, uint32_t offset, int more) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(buffer_at(base), (__attribute__((address_space(3))) void *)to, 4, (int)offset, more, 0, 0);
 }
 
 // What hp_packed_t has to be, for so many rows and heads; strides that no address goes by do not count.

@@ -78,20 +78,16 @@ template <int GP> struct Loader {
     }
     // left: states from the tile's first on that are seen
     __device__ __forceinline__ void fetch(char *to, const hp_packed_t &t, int64_t first, int head, int left, int lane) const {
-        typedef __attribute__((address_space(3))) void *Lds;
-        const auto from = buffer_at((const char *)t.codes + first * t.code_row_stride + (int64_t)head * t.code_head_stride);
+        const char *const codes_at = (const char *)t.codes + first * t.code_row_stride + (int64_t)head * t.code_head_stride;
+        const uint16_t *const pairs_at = (const uint16_t *)t.scales + first * t.scale_row_stride + (int64_t)head * t.scale_head_stride;
         constexpr int kRows = kWave / GP, kPairRows = kWave / kPairs;         // of a load
 #pragma unroll
-        for (int n = 0; n < GP; ++n) {
-            if constexpr (kOffsets == 1)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (Lds)(to + n * kWave * 16), 16, (int)(lane / GP < left - n * kRows ? codes[0] : kOutside), n * kRows * (int)t.code_row_stride, 0, 0);
-            else
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (Lds)(to + n * kWave * 16), 16, (int)((n * kWave + lane) / GP < left ? codes[n % kOffsets] : kOutside), 0, 0, 0);
-        }
-        const auto pairs = buffer_at((const uint16_t *)t.scales + first * t.scale_row_stride + (int64_t)head * t.scale_head_stride);
+        for (int n = 0; n < GP; ++n)
+            if constexpr (kOffsets == 1) pieces_to_lds(codes_at, to + n * kWave * 16, lane / GP < left - n * kRows ? codes[0] : kOutside, n * kRows * (int)t.code_row_stride);
+            else pieces_to_lds(codes_at, to + n * kWave * 16, (n * kWave + lane) / GP < left ? codes[n % kOffsets] : kOutside, 0);
 #pragma unroll
         for (int n = 0; n < kPairs; ++n)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(pairs, (Lds)(to + Layout<GP>::kCodes + n * kWave * 4), 4, (int)(lane / kPairs < left - n * kPairRows ? scales : kOutside), n * kPairRows * (int)t.scale_row_stride * 2, 0, 0);
+            words_to_lds(pairs_at, to + Layout<GP>::kCodes + n * kWave * 4, lane / kPairs < left - n * kPairRows ? scales : kOutside, n * kPairRows * (int)t.scale_row_stride * 2);
     }
 };
 
@@ -197,15 +193,6 @@ template <class T, int GP> __global__ __launch_bounds__(kBlock, (kResident<T, GP
     Loader<GP> ks, vs;
     ks.plan(p.k, p.groups, lane);
     vs.plan(p.v, p.groups, lane);
-    // a wave's tiles are its own: no barriers, only its own loads to wait for and its own reads to finish
-    const auto settle = [] {
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-    };
-    const auto read = [&] {
-        __builtin_amdgcn_s_waitcnt(0xc07f);        // lgkmcnt(0)
-        settle();
-    };
     // of a quarter's states 16 a + 4 quarter + i, a and i < 4, lane 4 a + i has the steps and brings the transposed codes
     const int own = 16 * (col / 4) + 4 * quarter + col % 4;
     const Frag centre = all_of(-kLift - kMiddle);
@@ -287,7 +274,7 @@ template <class T, int GP> __global__ __launch_bounds__(kBlock, (kResident<T, GP
         // here, not behind the branch, where all these products' results would have to be kept until then
 #pragma unroll
         for (int a = 0; a < 4; ++a) asm("" : "+v"(s[a]));
-        read();
+        reads_done();
         if (more) ks.fetch(k_tile, p.k, next, state_head, hi - next, lane);
 
         if (key0 + kTile > hi)
@@ -368,7 +355,7 @@ template <class T, int GP> __global__ __launch_bounds__(kBlock, (kResident<T, GP
                 }
             }
         });
-        read();
+        reads_done();
         if (more) vs.fetch(v_tile, p.v, next, state_head, hi - next, lane);
     }
     sum = column_sum(sum);
