@@ -20,8 +20,7 @@ namespace {
 using namespace hp;
 
 constexpr int kOuts = 16;                          // rows of w of a tile
-constexpr int kChunk = 4, kChannels = kChunk * kGroup;                   // groups and channels at a time
-constexpr int kMostWaves = 8;
+constexpr int kWaves = 8, kBlock = kWaves * kWave;
 
 struct Params {
     int64_t rows;
@@ -33,107 +32,115 @@ struct Params {
     int64_t out_stride;
 };
 
-// What a wave has in LDS of a chunk: R rows of x, 16 MT rows of w's codes and as many of its pairs (step, low).  The 16-byte
-// pieces of a row are turned, so that the same piece of neighbouring rows lies in different banks.
-template <class T, int R, int MT> struct Stage {
-    static constexpr int kPieces = kChannels * (int)sizeof(T) / 16, kRowBytes = 16 * kPieces;         // of a row of x
-    static constexpr int kX = R * kRowBytes, kCodes = MT * kOuts * kChunk * kGroupBytes, kPairs = MT * kOuts * kChunk * 4, kBytes = kX + kCodes + kPairs;
-    static constexpr int kXLoads = R * kPieces / kWave, kLoads = kXLoads + 2 * MT;
+// How a launch is cut.  A wave has in LDS, of a chunk of CH groups, R rows of x (4, or tiles of 16) and 16 MT rows of w's
+// codes and pairs (step, low), DEPTH chunks in turn.  The 16-byte pieces of a row are turned, so that the same piece of
+// neighbouring rows lies in different banks.  EXACT: rows of x are whole aligned pieces, which loads bring to LDS by themselves.
+template <class T, int R_, int CH_, int MT_, int DEPTH_, bool EXACT_> struct Cut {
+    typedef T type;
+    static constexpr int R = R_, CH = CH_, MT = MT_, DEPTH = DEPTH_, N = kTerms<T>, NT = (R + 15) / 16;
+    static constexpr bool EXACT = EXACT_;
+    static constexpr int kPiece = 16 / (int)sizeof(T), kPieces = CH * kGroup / kPiece, kRowBytes = 16 * kPieces;      // of x
+    static constexpr int kXLoads = R * kPieces / kWave, kWLoads = (MT * CH + 3) / 4;                                  // kWLoads: of codes, and of pairs
+    static constexpr int kCodes = R * kRowBytes, kPairs = kCodes + kWLoads * kWave * 16, kBytes = kPairs + kWLoads * kWave * 4;
+    static constexpr int kLoads = (EXACT ? kXLoads : 0) + 2 * kWLoads, kLds = kWaves * DEPTH * kBytes;
     // binary32 operands are two pieces, which stay neighbours
-    static __device__ __forceinline__ int x_slot(int row, int piece) { return sizeof(T) == 2 ? piece ^ (row & 15) : piece ^ (2 * row & 30); }
-    static __device__ __forceinline__ int code_slot(int row, int piece) { return piece ^ (row >> 1 & 3); }
+    static __device__ __forceinline__ int x_slot(int row, int piece) { return sizeof(T) == 2 ? piece ^ (row & (kPieces - 1)) : piece ^ (2 * row & (kPieces - 2)); }
+    static __device__ __forceinline__ int code_slot(int row, int piece) { return CH == 4 ? piece ^ (row >> 1 & 3) : piece ^ (row >> 2 & 1); }
+    // loads of x whose pieces are turned alike are so many rows and loads apart
+    static constexpr int kRowsALoad = kWave / kPieces, kPeriod = sizeof(T) == 2 ? kPieces : kPieces / 2;
+    static constexpr int kKinds = kPeriod / kRowsALoad < kXLoads ? kPeriod / kRowsALoad : kXLoads;
+    static_assert(kLds <= 160 * 1024 && kLds >= kWaves * MT * NT * kWave * 16, "fits, and has room for the sums");
+    static_assert((DEPTH - 1) * kLoads < 64, "what a wave can wait for");
 };
 
-// R: rows of x (4, or tiles of 16), MT: tiles of w of a wave, DEPTH: chunks in LDS, EXACT: rows of x are whole aligned pieces
-// that loads bring to LDS by themselves.
-template <class T, int R, int MT, int DEPTH, bool EXACT> __global__ __launch_bounds__(kMostWaves * kWave) void packed_linear_kernel(Params p) {
-    typedef Stage<T, R, MT> S;
-    constexpr int N = kTerms<T>, NT = (R + 15) / 16;
+template <class C> __global__ __launch_bounds__(kBlock) void packed_linear_kernel(Params p) {
+    typedef typename C::type T;
+    constexpr int R = C::R, CH = C::CH, MT = C::MT, DEPTH = C::DEPTH, N = C::N, NT = C::NT;
     constexpr float kLift = Codes<T>::kLift;
     extern __shared__ __attribute__((aligned(16))) char shared[];
     const int tid = (int)threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), col = lane % 16, quarter = lane / 16;
-    const int turn = wave & (p.waves_k - 1), tiles = (int)blockDim.x / kWave / p.waves_k;
+    const int turn = wave & (p.waves_k - 1), tiles = kWaves / p.waves_k;
     const int n0 = ((int)blockIdx.x * tiles + wave / p.waves_k) * kOuts * MT;
     const int64_t r0 = (int64_t)blockIdx.y * R;
-    const int rows = (int)min(p.rows - r0, (int64_t)R), all = n0 < p.n_out ? (p.groups + kChunk - 1) / kChunk : 0;
-    const int chunks = (all - turn + p.waves_k - 1) / p.waves_k;
-    char *const mine = shared + wave * (DEPTH * S::kBytes);
+    const int rows = (int)min(p.rows - r0, (int64_t)R);
+    // whole chunks of this wave, and one that is not whole behind the last
+    const int all = n0 < p.n_out ? p.n_in / (CH * kGroup) : 0, chunks = (all - turn + p.waves_k - 1) / p.waves_k;
+    char *const mine = shared + wave * (DEPTH * C::kBytes);
 
     const T *const x0 = (const T *)p.x + r0 * p.x_stride;
     const char *const codes = (const char *)p.w.codes + n0 * p.w.code_row_stride;
     const uint16_t *const pairs = (const uint16_t *)p.w.scales + n0 * p.w.scale_row_stride;
-    // what a lane brings: of x a piece of every kWave / kPieces rows, of the codes piece and of the pairs pair lane % 4 of row lane / 4
-    constexpr int kRowsALoad = kWave / S::kPieces, kKinds = 16 / kRowsALoad < S::kXLoads ? 16 / kRowsALoad : S::kXLoads;
-    int x_piece[kKinds];
-    uint32_t x_at[kKinds];
+    // what a lane brings
+    int x_piece[C::kKinds], x_row[C::kKinds];
+    uint32_t x_at[C::kKinds], code_at[C::kWLoads], pair_at[C::kWLoads];
 #pragma unroll
-    for (int n = 0; n < kKinds; ++n) {
-        const int row = n * kRowsALoad + lane / S::kPieces;
-        x_piece[n] = S::x_slot(row, lane % S::kPieces);
-        x_at[n] = (uint32_t)(row * (int)p.x_stride * (int)sizeof(T) + 16 * x_piece[n]);
+    for (int n = 0; n < C::kKinds; ++n) {
+        x_row[n] = n * C::kRowsALoad + lane / C::kPieces;
+        x_piece[n] = C::x_slot(x_row[n], lane % C::kPieces);
+        x_at[n] = (uint32_t)(x_row[n] * (int)p.x_stride * (int)sizeof(T) + 16 * x_piece[n]);
     }
-    const int w_row = lane / 4, code_piece = S::code_slot(w_row, lane % 4);
-    const uint32_t code_at = (uint32_t)(w_row * (int)p.w.code_row_stride + kGroupBytes * code_piece), pair_at = (uint32_t)(w_row * (int)p.w.scale_row_stride * 2 + 4 * (lane % 4));
-
-    // Chunk i of this wave; beyond its last one, and of rows and groups that are not there, zeros, which are not read.
-    const auto fetch = [&](int i) {
-        char *to = mine + i % DEPTH * S::kBytes;
-        const int c = i < chunks ? turn + i * p.waves_k : all, g0 = c * kChunk;
+    const int w_row = lane / CH, code_piece = C::code_slot(w_row, lane % CH);
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            const bool there = i < chunks && n0 + kOuts * m + w_row < p.n_out;
-            pieces_to_lds(codes, to + S::kX + m * kWave * 16, there && g0 + code_piece < p.groups ? code_at + g0 * kGroupBytes : kOutside, kOuts * m * (int)p.w.code_row_stride);
-            words_to_lds(pairs, to + S::kX + S::kCodes + m * kWave * 4, there && g0 + lane % 4 < p.groups ? pair_at + 4 * g0 : kOutside, 2 * kOuts * m * (int)p.w.scale_row_stride);
-        }
+    for (int n = 0; n < C::kWLoads; ++n) {
+        const int row = n * (kWave / CH) + w_row;
+        const bool there = row < kOuts * MT && n0 + row < p.n_out;
+        code_at[n] = there ? (uint32_t)(row * (int)p.w.code_row_stride + kGroupBytes * code_piece) : kOutside;
+        pair_at[n] = there ? (uint32_t)(row * (int)p.w.scale_row_stride * 2 + 4 * (lane % CH)) : kOutside;
+    }
+    const auto fetch_w = [&](char *to, int g0, bool whole) {
 #pragma unroll
-        for (int n = 0; n < S::kXLoads; ++n) {
-            const int row = n * kRowsALoad + lane / S::kPieces, piece = x_piece[n % kKinds], k = c * kChannels + piece * (16 / (int)sizeof(T));
-            if constexpr (EXACT) {
-                pieces_to_lds(x0, to + n * kWave * 16, i < chunks && row < rows && k < p.n_in ? x_at[n % kKinds] + c * S::kRowBytes : kOutside, n / kKinds * 16 * (int)p.x_stride * (int)sizeof(T));
-            } else {
-                *(Vec<T, 16 / sizeof(T)> *)(to + (n * kWave + lane) * 16) = load<16 / sizeof(T)>(x0 + row * p.x_stride + k, i < chunks && row < rows ? p.n_in - k : 0);
-            }
+        for (int n = 0; n < C::kWLoads; ++n) {
+            pieces_to_lds(codes, to + C::kCodes + n * kWave * 16, whole || g0 + code_piece < p.groups ? code_at[n] : kOutside, g0 * kGroupBytes);
+            words_to_lds(pairs, to + C::kPairs + n * kWave * 4, whole || g0 + lane % CH < p.groups ? pair_at[n] : kOutside, g0 * 4);
         }
     };
+    const auto fetch_x = [&](char *to, int g0, bool whole) {
+#pragma unroll
+        for (int n = 0; n < C::kXLoads; ++n) {
+            const int kind = n % C::kKinds, behind = n / C::kKinds * C::kPeriod;
+            const bool there = x_row[kind] + behind < rows && (whole || g0 * kGroup + x_piece[kind] * C::kPiece < p.n_in);
+            pieces_to_lds(x0, to + n * kWave * 16, there ? x_at[kind] : kOutside, (behind * (int)p.x_stride + g0 * kGroup) * (int)sizeof(T));
+        }
+    };
+    // rows that are no whole pieces pass through registers
+    typedef Vec<T, C::kPiece> Piece;
+    const auto from_row = [&](int n) { return x0 + min(x_row[n % C::kKinds] + n / C::kKinds * C::kPeriod, rows - 1) * p.x_stride + x_piece[n % C::kKinds] * C::kPiece; };
+
     Quad acc[MT][NT] = {};
     const Frag ones = all_of(1.0f);
     const Codes<T> codes_of;
     const auto add = [&](const char *from) {
-        Words w[MT], pairs[MT];
+        Words low[MT] = {};
+        Frag sums[NT] = {};
 #pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            w[m] = *(const Words *)(from + S::kX + (m * kOuts + col) * kChunk * kGroupBytes + kGroupBytes * S::code_slot(col, quarter));
-            pairs[m] = *(const Words *)(from + S::kX + S::kCodes + (m * kOuts + col) * kChunk * 4);
-            across_quarters(w[m]);
-        }
-        Frag sums[NT];
-#pragma unroll
-        for (int j = 0; j < kChunk; ++j) {
+        for (int j = 0; j < CH; ++j) {
             Frag a[NT][N];
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 const int row = 16 * t + (R < 16 ? col % R : col);
                 Vec<T, 8> x;
                 if constexpr (sizeof(T) == 2) {
-                    x = *(const Vec<T, 8> *)(from + row * S::kRowBytes + 16 * S::x_slot(row, 4 * j + quarter));
+                    x = *(const Vec<T, 8> *)(from + row * C::kRowBytes + 16 * C::x_slot(row, 4 * j + quarter));
                 } else {
-                    const Quad lower = *(const Quad *)(from + row * S::kRowBytes + 16 * S::x_slot(row, 8 * j + 2 * quarter));
-                    const Quad upper = *(const Quad *)(from + row * S::kRowBytes + 16 * S::x_slot(row, 8 * j + 2 * quarter + 1));
+                    const Quad lower = *(const Quad *)(from + row * C::kRowBytes + 16 * C::x_slot(row, 8 * j + 2 * quarter));
+                    const Quad upper = *(const Quad *)(from + row * C::kRowBytes + 16 * C::x_slot(row, 8 * j + 2 * quarter + 1));
                     x = __builtin_shufflevector(lower, upper, 0, 1, 2, 3, 4, 5, 6, 7);
                 }
                 terms<T>(x, a[t]);
                 Quad sum = {};                     // of this lane's row of x, in all four numbers
 #pragma unroll
                 for (int n = 0; n < N; ++n) sum = mma(ones, a[t][n], sum);
-                const float first = (float)(__bf16)sum[0], second = (float)(__bf16)(sum[0] - first);
-                const float part = quarter == 0 ? first : quarter == 1 ? second : N > 1 && quarter == 2 ? sum[0] - first - second : 0.0f;
+                const float second = sum[0] - (float)(__bf16)sum[0];
+                const float part = quarter == 0 ? sum[0] : quarter == 1 ? second : N > 1 && quarter == 2 ? second - (float)(__bf16)second : 0.0f;
                 sums[t][2 * j] = (__bf16)(-kLift * part);
                 sums[t][2 * j + 1] = (__bf16)part;
             }
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
-                const Frag l = codes_of(w[m][j]);
-                const float step = step_of(pairs[m][j]);
+                const int row = kOuts * m + col;
+                const Frag l = codes_of(*(const uint32_t *)(from + C::kCodes + (row * CH + C::code_slot(row, j)) * kGroupBytes + 4 * quarter));
+                low[m][j] = *(const uint32_t *)(from + C::kPairs + (row * CH + j) * 4);
+                const float step = step_of(low[m][j]);
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
                     Quad d = {};
@@ -147,19 +154,56 @@ template <class T, int R, int MT, int DEPTH, bool EXACT> __global__ __launch_bou
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int t = 0; t < NT; ++t) acc[m][t] = mma(sums[t], __builtin_bit_cast(Frag, pairs[m]), acc[m][t]);
+            for (int t = 0; t < NT; ++t) acc[m][t] = mma(sums[t], __builtin_bit_cast(Frag, low[m]), acc[m][t]);
     };
-    for (int i = 0; i < DEPTH - 1; ++i) fetch(i);
+
+    const auto group_of = [&](int i) { return (turn + i * p.waves_k) * CH; };
+    const auto stage = [&](int i) { return mine + i % DEPTH * C::kBytes; };
+    for (int i = 0; i < DEPTH - 1 && i < chunks; ++i) {
+        fetch_w(stage(i), group_of(i), true);
+        if constexpr (C::EXACT) fetch_x(stage(i), group_of(i), true);
+    }
+    Piece held[C::EXACT ? 1 : C::kXLoads];
+    if (!C::EXACT && chunks > 0)
+#pragma unroll
+        for (int n = 0; n < C::kXLoads; ++n) held[C::EXACT ? 0 : n] = *(const typename VecOf<T, C::kPiece>::mem *)(from_row(n) + group_of(0) * kGroup);
     for (int i = 0; i < chunks; ++i) {
-        fetch(i + DEPTH - 1);
-        if constexpr (EXACT) __builtin_amdgcn_s_waitcnt(but((DEPTH - 1) * S::kLoads));
-        else __builtin_amdgcn_s_waitcnt(but(0));
+        const bool more = i + DEPTH - 1 < chunks;
+        if (more) fetch_w(stage(i + DEPTH - 1), group_of(i + DEPTH - 1), true);
+        if constexpr (C::EXACT) {
+            if (more) {
+                fetch_x(stage(i + DEPTH - 1), group_of(i + DEPTH - 1), true);
+                __builtin_amdgcn_s_waitcnt(but((DEPTH - 1) * C::kLoads));
+            } else {
+                __builtin_amdgcn_s_waitcnt(but(0));
+            }
+        } else {
+#pragma unroll
+            for (int n = 0; n < C::kXLoads; ++n) *(Piece *)(stage(i) + (n * kWave + lane) * 16) = held[n];
+            // the pieces came behind w's chunk i
+            __builtin_amdgcn_s_waitcnt(but(0));
+#pragma unroll
+            for (int n = 0; n < C::kXLoads; ++n) held[n] = *(const typename VecOf<T, C::kPiece>::mem *)(from_row(n) + group_of(i + 1 < chunks ? i + 1 : i) * kGroup);
+        }
         settle();
-        add(mine + i % DEPTH * S::kBytes);
+        add(stage(i));
+        reads_done();
+    }
+    if (n0 < p.n_out && p.n_in % (CH * kGroup) && all % p.waves_k == turn) {
+        const int g0 = all * CH;
+        fetch_w(mine, g0, false);
+        if constexpr (C::EXACT) {
+            fetch_x(mine, g0, false);
+        } else {
+#pragma unroll
+            for (int n = 0; n < C::kXLoads; ++n) *(Piece *)(mine + (n * kWave + lane) * 16) = load<C::kPiece>(from_row(n) + g0 * kGroup, p.n_in - g0 * kGroup - x_piece[n % C::kKinds] * C::kPiece);
+        }
+        __builtin_amdgcn_s_waitcnt(but(0));
+        settle();
+        add(mine);
         reads_done();
     }
     if (p.waves_k > 1) {
-        __builtin_amdgcn_s_waitcnt(but(0));        // zeros still on their way would come into what follows
         __syncthreads();
         Quad *const parts = (Quad *)shared;        // [wave][MT][NT][lane]
         if (turn)
@@ -202,58 +246,51 @@ int check(const hp_packed_linear_args_t *a) {
     return short_strides(a->w, a->n_out) ? HP_OK : HP_ELAYOUT;
 }
 
-template <class T, int R, int MT, int DEPTH, int WAVES, bool EXACT> void launch(Params &p, hipStream_t s) {
-    constexpr int kLds = WAVES * DEPTH * Stage<T, R, MT>::kBytes;
-    static_assert(kLds <= 160 * 1024 && kLds >= WAVES * MT * ((R + 15) / 16) * kWave * 16, "fits, and has room for the sums");
-    static_assert((DEPTH - 1) * Stage<T, R, MT>::kLoads < 64, "what a wave can wait for");
-    const int64_t tiles = (p.n_out + kOuts * MT - 1) / (kOuts * MT), chunks = (p.groups + kChunk - 1) / kChunk;
+template <class C> void launch(Params &p, hipStream_t s) {
+    const int64_t tiles = (p.n_out + kOuts * C::MT - 1) / (kOuts * C::MT), chunks = (p.groups + C::CH - 1) / C::CH;
     p.waves_k = 1;
-    while (p.waves_k < WAVES && 2 * p.waves_k <= chunks) p.waves_k *= 2;
-    const int64_t each = WAVES / p.waves_k;
-    packed_linear_kernel<T, R, MT, DEPTH, EXACT><<<dim3((uint32_t)((tiles + each - 1) / each), (uint32_t)((p.rows + R - 1) / R)), WAVES * kWave, kLds, s>>>(p);
+    while (p.waves_k < kWaves && 2 * p.waves_k <= chunks) p.waves_k *= 2;
+    const int64_t each = kWaves / p.waves_k;
+    packed_linear_kernel<C><<<dim3((uint32_t)((tiles + each - 1) / each), (uint32_t)((p.rows + C::R - 1) / C::R)), kBlock, C::kLds, s>>>(p);
 }
 
-template <class T> void launch(Params &p, hipStream_t s) {
-    constexpr int kSize = sizeof(T);
-    const bool exact = (uintptr_t)p.x % 16 == 0 && (p.rows <= 1 || (p.x_stride % (16 / kSize) == 0 && p.x_stride >= 0 && p.x_stride <= kMostStride / 2)) && p.n_in % (16 / kSize) == 0;
+template <class T> void choose(Params &p, hipStream_t s) {
+    constexpr int kPiece = 16 / sizeof(T);
+    const bool exact = (uintptr_t)p.x % 16 == 0 && p.n_in % kPiece == 0 && (p.rows <= 1 || (p.x_stride % kPiece == 0 && p.x_stride >= 0 && p.x_stride <= kMostStride / 4));
     const int per = (p.n_out + kOuts * kComputeUnits - 1) / (kOuts * kComputeUnits);       // tiles of a workgroup a compute unit
     if (!exact) {
-        if (p.rows <= 4) launch<T, 4, 1, 2, 8, false>(p, s);
-        else if (p.rows <= 16 && per < 2) launch<T, 16, 1, 2, 4, false>(p, s);
-        else if (p.rows <= 16) launch<T, 16, 2, 2, 4, false>(p, s);
-        else launch<T, 32, 2, 2, 4, false>(p, s);
+        if (p.rows <= 4 && per < 2) launch<Cut<T, 4, 4, 1, 4, false>>(p, s);
+        else if (p.rows <= 4) launch<Cut<T, 4, 4, 2, 4, false>>(p, s);
+        else if (p.rows <= 16 && per < 2) launch<Cut<T, 16, 2, 1, 3, false>>(p, s);
+        else if (p.rows <= 16) launch<Cut<T, 16, 2, 2, 3, false>>(p, s);
+        else launch<Cut<T, 32, 2, 2, 2, false>>(p, s);
         return;
     }
     if (p.rows <= 4) {
-        if (per >= 4) {
-            if constexpr (kSize == 2) launch<T, 4, 4, 3, 8, true>(p, s);
-            else launch<T, 4, 4, 2, 8, true>(p, s);
-        }
-        else if (per == 3) launch<T, 4, 3, 3, 8, true>(p, s);
-        else if (per == 2) launch<T, 4, 2, 4, 8, true>(p, s);
-        else launch<T, 4, 1, 4, 8, true>(p, s);
-        return;
-    }
-    if constexpr (kSize == 2) {
+        if (per >= 4) launch<Cut<T, 4, 4, 4, sizeof(T) == 2 ? 3 : 2, true>>(p, s);
+        else if (per == 3) launch<Cut<T, 4, 4, 3, 3, true>>(p, s);
+        else if (per == 2) launch<Cut<T, 4, 4, 2, 4, true>>(p, s);
+        else launch<Cut<T, 4, 4, 1, 4, true>>(p, s);
+    } else if constexpr (sizeof(T) == 2) {
         if (p.rows <= 16) {
-            if (per >= 4) launch<T, 16, 4, 2, 8, true>(p, s);
-            else if (per == 3) launch<T, 16, 3, 2, 8, true>(p, s);
-            else if (per == 2) launch<T, 16, 2, 3, 8, true>(p, s);
-            else launch<T, 16, 1, 3, 8, true>(p, s);
+            if (per >= 4) launch<Cut<T, 16, 4, 4, 2, true>>(p, s);
+            else if (per == 3) launch<Cut<T, 16, 4, 3, 2, true>>(p, s);
+            else if (per == 2) launch<Cut<T, 16, 4, 2, 3, true>>(p, s);
+            else launch<Cut<T, 16, 4, 1, 3, true>>(p, s);
         } else if (p.rows <= 32) {
-            if (per >= 2) launch<T, 32, 2, 3, 4, true>(p, s);
-            else launch<T, 32, 1, 3, 4, true>(p, s);
+            if (per >= 2) launch<Cut<T, 32, 2, 2, 3, true>>(p, s);
+            else launch<Cut<T, 32, 2, 1, 3, true>>(p, s);
         } else {
-            if (per >= 2) launch<T, 64, 2, 2, 4, true>(p, s);
-            else launch<T, 64, 1, 2, 4, true>(p, s);
+            if (per >= 2) launch<Cut<T, 64, 2, 2, 2, true>>(p, s);
+            else launch<Cut<T, 64, 2, 1, 2, true>>(p, s);
         }
     } else {
         if (p.rows <= 16) {
-            if (per >= 2) launch<T, 16, 2, 3, 4, true>(p, s);
-            else launch<T, 16, 1, 3, 4, true>(p, s);
+            if (per >= 2) launch<Cut<T, 16, 2, 2, 3, true>>(p, s);
+            else launch<Cut<T, 16, 2, 1, 3, true>>(p, s);
         } else {
-            if (per >= 2) launch<T, 32, 2, 2, 4, true>(p, s);
-            else launch<T, 32, 1, 2, 4, true>(p, s);
+            if (per >= 2) launch<Cut<T, 32, 2, 2, 2, true>>(p, s);
+            else launch<Cut<T, 32, 2, 1, 2, true>>(p, s);
         }
     }
 }
@@ -269,8 +306,8 @@ int hp_packed_linear(const hp_packed_linear_args_t *a, void *stream) {
     p.rows = a->rows, p.n_in = a->n_in, p.n_out = a->n_out, p.groups = groups_of(a->n_in);
     p.x = a->x, p.x_stride = a->x_stride, p.w = a->w, p.out = a->out, p.out_stride = a->out_stride;
     const hipStream_t s = (hipStream_t)stream;
-    if (a->dtype == HP_BF16) launch<__bf16>(p, s);
-    else launch<float>(p, s);
+    if (a->dtype == HP_BF16) choose<__bf16>(p, s);
+    else choose<float>(p, s);
     return hip_failed(hipGetLastError()) ? HP_EHIP : HP_OK;
 }
 
