@@ -28,7 +28,6 @@ namespace {
 using namespace hp;
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-constexpr int kWaves = 4, kBlock = kWaves * kWave;
 constexpr int kTile = 64, kHeads = 16;             // states of a wave's tile, heads of a workgroup
 constexpr float kMiddle = 8.0f;
 
@@ -95,17 +94,18 @@ __device__ __forceinline__ float2 across_halves(float x) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return make_float2(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
-__device__ __forceinline__ float2 across_rows(float x) {
-    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+// Of quarters 0 and 1 (and 2 and 3): the first has both its own x and the second's, the second both their y.
+__device__ __forceinline__ float2 across_rows(float x, float y) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false, false);
     return make_float2(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 // Over the four lanes of a column.
 __device__ __forceinline__ float column_max(float x) {
-    const float2 a = across_halves(x), b = across_rows(fmaxf(a.x, a.y));
+    const float2 a = across_halves(x), b = across_rows(fmaxf(a.x, a.y), fmaxf(a.x, a.y));
     return fmaxf(b.x, b.y);
 }
 __device__ __forceinline__ float column_sum(float x) {
-    const float2 a = across_halves(x), b = across_rows(a.x + a.y);
+    const float2 a = across_halves(x), b = across_rows(a.x + a.y, a.x + a.y);
     return b.x + b.y;
 }
 
@@ -124,39 +124,55 @@ __device__ __forceinline__ Range range_of(const Params &p, int64_t row) {
     return r;
 }
 
-// The tiles of a unit: `left` of them, the first of which is the skip-th of `row` and the at-th of all.
+// All rows' tiles lie one behind the other, and the units take equal shares, whatever the rows' lengths: each wave adds up
+// the lengths for itself, a few rows a lane.  The tiles of a unit: `left` of them, the first of which is the skip-th of `row`
+// and the at-th of all.
+constexpr int kRowsALane = 8, kMostShared = kRowsALane * kWave;
 struct Share {
     int64_t row;
     int skip, left, at, total, units;
+    Range held;                                    // of row `lane`, where there are no more rows than lanes
+    bool few;
+    __device__ __forceinline__ Range now(const Params &p) const {
+        if (!few) return range_of(p, row);
+        return Range{__builtin_amdgcn_readlane(held.lo, (int)row), __builtin_amdgcn_readlane(held.hi, (int)row)};
+    }
 };
-// All rows' tiles lie one behind the other, and the units take equal shares, whatever the rows' lengths: each wave adds up
-// the lengths for itself, a few rows a lane.
-constexpr int kRowsALane = 8, kMostShared = kRowsALane * kWave;
-__device__ __forceinline__ Share share_of(const Params &p, int unit, int lane) {
-    if (!p.units) return Share{unit, 0, range_of(p, unit).tiles(), 0, 0, 0};
+__device__ __forceinline__ Share share_of(const Params &p, int unit, int lane, int waves) {
+    Share s{unit, 0, 0, 0, 0, 0, Range{}, false};
+    if (!p.units) {
+        s.left = range_of(p, unit).tiles();
+        return s;
+    }
     const int rows = (int)p.rows, each = (rows + kWave - 1) / kWave, mine = lane * each;
+    s.few = each == 1;
     int own = 0;
-    for (int i = 0; i < each; ++i)
-        if (mine + i < rows) own += range_of(p, mine + i).tiles();
+    if (s.few) {
+        s.held = range_of(p, min(lane, rows - 1));
+        own = lane < rows ? s.held.tiles() : 0;
+    } else {
+        for (int i = 0; i < each; ++i)
+            if (mine + i < rows) own += range_of(p, mine + i).tiles();
+    }
     int upto = own;
 #pragma unroll
     for (int d = 1; d < kWave; d *= 2) {
         const int before = __shfl_up(upto, d);
         if (lane >= d) upto += before;
     }
-    Share s;
     s.total = __builtin_amdgcn_readlane(upto, kWave - 1);
-    s.units = min(p.units, (s.total + kWaves - 1) / kWaves);       // none with less than a tile for each wave
+    s.units = min(p.units, (s.total + waves - 1) / waves);         // none with less than a tile for each wave
     s.at = unit < s.units ? first_of(s.total, unit, s.units) : 0;
     s.left = unit < s.units ? first_of(s.total, unit + 1, s.units) - s.at : 0;
     // the lane whose rows have that tile, then the row
     const int at_lane = __builtin_ctzll(__ballot(upto > s.at));
     int before = __builtin_amdgcn_readlane(upto - own, at_lane), row = at_lane * each;
-    for (;; ++row) {
-        const int n = range_of(p, row).tiles();
-        if (before + n > s.at) break;
-        before += n;
-    }
+    if (!s.few)
+        for (;; ++row) {
+            const int n = range_of(p, row).tiles();
+            if (before + n > s.at) break;
+            before += n;
+        }
     s.row = row, s.skip = s.at - before;
     return s;
 }
@@ -175,16 +191,19 @@ template <int N, class F> __device__ __forceinline__ void each(const F &f) {
 
 constexpr float kLag = 8.0f;                       // the maximum is raised when a score passes it by 2^8
 
-// Waves of a SIMD: as many as registers (128, 168 and 256 of them) and LDS (10 KiB a wave for heads of 128) let run.
-template <class T, int GP> constexpr int kResident = sizeof(T) == 2 ? (GP <= 4 ? 4 : 2) : (GP <= 2 ? 3 : 2);
+// Waves of a workgroup, and workgroups of a compute unit: as registers and LDS let run (of 160 KiB, which two workgroups of 80
+// or four of 40 do not share: 1024 of these took two turns, 64 requests 88 us instead of 77).
+template <int GP> constexpr int kWaves = GP == 8 ? 7 : 4;
+template <class T, int GP> constexpr int kResident = sizeof(T) == 2 ? (GP <= 3 ? 4 : GP == 4 ? 3 : 1) : (GP <= 2 ? 3 : GP <= 4 ? 2 : 1);
+template <class T, int GP> constexpr int kWavesASimd = (kWaves<GP> * kResident<T, GP> + 3) / 4;
 
-template <class T, int GP> __global__ __launch_bounds__(kBlock, (kResident<T, GP>)) void packed_attend_kernel(Params p) {
+template <class T, int GP> __global__ __launch_bounds__((kWaves<GP> * kWave), (kWavesASimd<T, GP>)) void packed_attend_kernel(Params p) {
     typedef Layout<GP> L;
     constexpr float kLift = Codes<T>::kLift;
     constexpr bool kCentred = kLift == -kMiddle;
-    constexpr int N = kTerms<T>, kSets = (GP + 3) / 4, kRow = kGroup * GP + 4;
+    constexpr int N = kTerms<T>, kSets = (GP + 3) / 4, kWaves = ::kWaves<GP>;
     __shared__ __attribute__((aligned(16))) char lds[kWaves * L::kBytes];
-    static_assert(sizeof(lds) >= sizeof(float) * kWaves * kHeads * (kRow + 2), "room for the join");
+    static_assert(sizeof(lds) >= 16 * kWaves * 2 * GP * kWave + 8 * kWaves * kHeads, "room for the join");
     const int tid = (int)threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), col = lane % 16, quarter = lane / 16;
     const int unit = (int)blockIdx.x, state_head = (int)blockIdx.y / p.head_tiles, first_head = ((int)blockIdx.y % p.head_tiles) * kHeads;
     const int heads = min(p.group - first_head, kHeads), head0 = state_head * p.group + first_head;
@@ -198,10 +217,10 @@ template <class T, int GP> __global__ __launch_bounds__(kBlock, (kResident<T, GP
     const Frag centre = all_of(-kLift - kMiddle);
     const Codes<T> codes;
 
-    Share share = share_of(p, unit, lane);
+    Share share = share_of(p, unit, lane, kWaves);
   for (; share.left > 0; ++share.row, share.skip = 0) {
     const int64_t row = share.row;
-    const Range see = range_of(p, row);
+    const Range see = share.now(p);
     const int lo = see.lo, hi = see.hi, n_tiles = see.tiles();
     const int begin = share.skip, end = min(n_tiles, begin + share.left);
     share.left -= end - begin;
@@ -216,14 +235,42 @@ template <class T, int GP> __global__ __launch_bounds__(kBlock, (kResident<T, GP
     // (-lift sum q, sum q), split into three numbers over the quarters
     Frag q[GP][N], sums[kSets] = {};
     const T *q_row = (const T *)p.q.data + row * p.q.row_stride + (int64_t)(head0 + min(col, heads - 1)) * p.q.head_stride;
+    Vec<T, 8> x[GP];
+    int dim = p.dim;
+    asm volatile("" : "+s"(dim));                  // or the places of all channels would be kept over the rows
+    if (dim % 8 == 0) {                            // pieces are there or not
+#pragma unroll
+        for (int g = 0; g < GP; ++g) {
+            const int d = kGroup * g + 8 * quarter;
+            x[g] = *(const typename VecOf<T, 8>::mem *)(q_row + (d < dim ? d : 0));
+            if (d >= dim) x[g] = Vec<T, 8>{};
+        }
+    } else {
+#pragma unroll
+        for (int g = 0; g < GP; ++g) {
+            const int d = kGroup * g + 8 * quarter;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const T one = q_row[min(d + i, dim - 1)];
+                x[g][i] = d + i < dim ? one : (T)0.0f;
+            }
+            __builtin_amdgcn_sched_barrier(0);     // no more of them at a time than registers hold
+        }
+    }
+    // the first tiles are under way while the queries are made operands
+    __builtin_amdgcn_sched_barrier(0);
+    if (begin + wave < end) {
+        const int key0 = lo + (begin + wave) * kTile;
+        ks.fetch(k_tile, p.k, key0, state_head, hi - key0, lane);
+        vs.fetch(v_tile, p.v, key0, state_head, hi - key0, lane);
+    }
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int g = 0; g < GP; ++g) {
-        const int d = kGroup * g + 8 * quarter;
-        const Vec<T, 8> x = load<8>(q_row + d, p.dim - d);
-        terms<T>(x, q[g]);
+        terms<T>(x[g], q[g]);
         float sum = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum += (float)x[i];
+        for (int i = 0; i < 8; ++i) sum += (float)x[g][i];
         sum = column_sum(sum);
         const __bf16 a = (__bf16)sum, b = (__bf16)(sum - (float)a), c = (__bf16)(sum - (float)a - (float)b);
         const float part = quarter == 0 ? (float)a : quarter == 1 ? (float)b : quarter == 2 ? (float)c : 0.0f;
@@ -233,11 +280,6 @@ template <class T, int GP> __global__ __launch_bounds__(kBlock, (kResident<T, GP
 
     float top = -INFINITY, sum = 0.0f;
     Quad out[2 * GP] = {}, rest = {};
-    if (begin + wave < end) {
-        const int key0 = lo + (begin + wave) * kTile;
-        ks.fetch(k_tile, p.k, key0, state_head, hi - key0, lane);
-        vs.fetch(v_tile, p.v, key0, state_head, hi - key0, lane);
-    }
     for (int tile = begin + wave; tile < end; tile += kWaves) {
         const int key0 = lo + tile * kTile, next = key0 + kWaves * kTile;
         const bool more = tile + kWaves < end;
@@ -257,18 +299,13 @@ template <class T, int GP> __global__ __launch_bounds__(kBlock, (kResident<T, GP
                 s[a] = mma(__builtin_bit_cast(Frag, w), sums[h], s[a]);
             }
         }
-        each<GP>([&](auto j) {
-            // pieces 4j .. 4j + 3 of this column's four states of GP groups, one a quarter
-            const int mine = 4 * j + quarter;
-            Words w = *(const Words *)(k_tile + L::at(16 * (mine / GP) + col, mine % GP));
-            across_quarters(w);
-            each<4>([&](auto t) {
-                constexpr int a = (4 * j + t) / GP, g = (4 * j + t) % GP;
-                const Frag c = codes(w[t.value]);
+        each<GP>([&](auto g) {
+            each<4>([&](auto a) {
+                const Frag c = codes(*(const uint32_t *)(k_tile + L::at(16 * a + col, g) + 4 * quarter));
                 Quad d = {};
 #pragma unroll
                 for (int n = 0; n < N; ++n) d = mma(c, q[g][n], d);
-                each<4>([&](auto i) { s[a][i.value] += of_lane<4 * a + i>(step_of(k_pairs[g])) * d[i.value]; });
+                each<4>([&](auto i) { s[a][i.value] += of_lane<4 * a + i>(step_of(k_pairs[g.value])) * d[i.value]; });
             });
         });
         // here, not behind the branch, where all these products' results would have to be kept until then
@@ -360,8 +397,9 @@ template <class T, int GP> __global__ __launch_bounds__(kBlock, (kResident<T, GP
     }
     sum = column_sum(sum);
 
-    // join the waves in the tiles' place: statistics, then the products of each
-    float *const join = (float *)lds, *const tops = join + kWaves * kHeads * kRow, *const totals = tops + kWaves * kHeads;
+    // join the waves in the tiles' place: statistics, then the products, of which each wave adds up every kWaves-th tile
+    Quad *const join = (Quad *)lds;                // [wave][2 GP][lane]
+    float *const tops = (float *)(join + kWaves * 2 * GP * kWave), *const totals = tops + kWaves * kHeads;
     __syncthreads();
     if (quarter == 0) {
         tops[wave * kHeads + col] = top;
@@ -369,36 +407,41 @@ template <class T, int GP> __global__ __launch_bounds__(kBlock, (kResident<T, GP
     }
     __syncthreads();
     float most = -INFINITY, total = 0.0f;
+#pragma unroll
     for (int w = 0; w < kWaves; ++w) most = fmaxf(most, tops[w * kHeads + col]);
     // a wave without a maximum has seen nothing, or NaN alone
     const auto weight = [&](float t) { return t == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(t - most); };
+#pragma unroll
     for (int w = 0; w < kWaves; ++w) total += totals[w * kHeads + col] * weight(tops[w * kHeads + col]);
-    const float share = total == 0.0f ? 0.0f : weight(top) / total;
+    const float part_of_all = total == 0.0f ? 0.0f : weight(top) / total;
     const float lse2 = total == 0.0f ? -INFINITY : most + __builtin_amdgcn_logf(total);
 #pragma unroll
     for (int g = 0; g < GP; ++g) {
         const int from = 16 * (g / 2) + col;
         const float more = kMiddle * __shfl(rest[2 * (g % 2)], from) + __shfl(rest[2 * (g % 2) + 1], from);
 #pragma unroll
-        for (int c = 0; c < 2; ++c)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)            // rows of the transposed load are a word's bits in order
-                join[(wave * kHeads + col) * kRow + kGroup * g + 16 * c + 8 * (quarter / 2) + 2 * i + quarter % 2] = (out[2 * g + c][i] + more) * share;
+        for (int c = 0; c < 2; ++c) {
+            // rows of the transposed load are a word's bits in order: even channels in one quarter, odd ones in the next
+            const Quad v = (out[2 * g + c] + more) * part_of_all;
+            const float2 a = across_rows(v[0], v[2]), b = across_rows(v[1], v[3]);
+            join[(wave * 2 * GP + 2 * g + c) * kWave + lane] = Quad{a.x, a.y, b.x, b.y};
+        }
     }
     __syncthreads();
     const int64_t part = ((int64_t)blockIdx.y * p.units + unit) * 2 + (begin == 0);
-    for (int e = tid; e < heads * 8 * GP; e += kBlock) {
-        const int m = e / (8 * GP), d = 4 * (e % (8 * GP));
-        if (d >= p.dim) continue;
+    for (int t = wave; t < 2 * GP; t += kWaves) {
+        const int d = 16 * t + 4 * quarter;
         Quad v = {};
-        for (int w = 0; w < kWaves; ++w) v += *(const Quad *)(join + (w * kHeads + m) * kRow + d);
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) v += join[(w * 2 * GP + t) * kWave + lane];
+        if (col >= heads || d >= p.dim) continue;
         if (!whole) {
-            store<4>(p.products + (part * p.part_heads + m) * p.dim + d, v, p.dim - d);
+            store<4>(p.products + (part * p.part_heads + col) * p.dim + d, v, p.dim - d);
         } else {
             Vec<T, 4> o;
 #pragma unroll
-            for (int t = 0; t < 4; ++t) o[t] = (T)v[t];
-            store<4>((T *)p.out.data + row * p.out.row_stride + (int64_t)(head0 + m) * p.out.head_stride + d, o, p.dim - d);
+            for (int i = 0; i < 4; ++i) o[i] = (T)v[i];
+            store<4>((T *)p.out.data + row * p.out.row_stride + (int64_t)(head0 + col) * p.out.head_stride + d, o, p.dim - d);
         }
     }
     if (wave == 0 && quarter == 0 && col < heads) {
@@ -409,40 +452,45 @@ template <class T, int GP> __global__ __launch_bounds__(kBlock, (kResident<T, GP
   }
 }
 
-// Joins the parts of rows that lie in several units: a workgroup for a row and head, whose waves take every fourth part.
-template <class T> __global__ __launch_bounds__(kBlock) void packed_join_kernel(Params p) {
-    __shared__ __attribute__((aligned(16))) float shared[kWaves][HP_ATTEND_MAX_DIM];
-    const int lane = (int)threadIdx.x % kWave, wave = (int)threadIdx.x / kWave;
+// Joins the parts of rows that lie in several units.  A row and head has `waves` waves, which take every waves-th part; a
+// workgroup is one row and head of four or sixteen waves, or four heads of one.
+constexpr int kMostJoin = 16;
+template <class T> __global__ __launch_bounds__(kMostJoin * kWave) void packed_join_kernel(Params p, int waves) {
+    __shared__ __attribute__((aligned(16))) float shared[kMostJoin][HP_ATTEND_MAX_DIM];
+    const int lane = (int)threadIdx.x % kWave, index = __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave), wave = index % waves;
     const int64_t row = blockIdx.x;
     const int2 units = p.row_units[row];
     if (units.x == units.y) return;                // written as it was made
-    const int head = (int)blockIdx.y, state_head = head / p.group, in_group = head - state_head * p.group;
+    const int head = (int)(blockIdx.y * (blockDim.x / kWave / waves)) + index / waves, state_head = head / p.group, in_group = head - state_head * p.group;
+    if (head >= p.heads_q) return;                 // whole waves, and only where each works by itself
     const int64_t line = (int64_t)(state_head * p.head_tiles + in_group / kHeads) * p.units;
     const auto part = [&](int u) { return ((line + u) * 2 + (u == units.x)) * p.part_heads + in_group % kHeads; };
-    float top = -INFINITY;
-    for (int u = units.x + lane; u <= units.y; u += kWave) top = fmaxf(top, p.lse2[part(u)]);
+    // of the first 64 parts each lane keeps one's logarithm
+    const int first = units.x + lane;
+    const float own = first <= units.y ? p.lse2[part(first)] : -INFINITY;
+    float top = own;
+    for (int u = first + kWave; u <= units.y; u += kWave) top = fmaxf(top, p.lse2[part(u)]);
 #pragma unroll
     for (int d = kWave / 2; d; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
     // nothing seen in a part: no weight; NaN stays
-    const auto weight = [&](int u) {
-        const float t = p.lse2[part(u)];
-        return t == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(t - top);
-    };
-    float sum = 0.0f;
-    for (int u = units.x + lane; u <= units.y; u += kWave) sum += weight(u);
+    const auto weight = [&](float t) { return t == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(t - top); };
+    const float mine = weight(own);
+    float sum = mine;
+    for (int u = first + kWave; u <= units.y; u += kWave) sum += weight(p.lse2[part(u)]);
     sum = wave_sum(sum);
     Quad acc = {};
     const int d = 4 * lane;
-#pragma unroll 4
-    for (int u = units.x + wave; u <= units.y; u += kWaves) {
-        const float w = weight(u);
+    for (int u = units.x + wave; u <= units.y; u += waves) {
         const Quad v = load<4>(p.products + part(u) * p.dim + d, p.dim - d);
+        const float w = u - units.x < kWave ? __shfl(mine, u - units.x) : weight(p.lse2[part(u)]);
         if (w != 0.0f) acc += w * v;
     }
-    *(Quad *)&shared[wave][d] = acc;
-    __syncthreads();
-    if (wave) return;
-    for (int w = 1; w < kWaves; ++w) acc += *(const Quad *)&shared[w][d];
+    if (waves > 1) {
+        *(Quad *)&shared[wave][d] = acc;
+        __syncthreads();
+        if (wave) return;
+        for (int w = 1; w < waves; ++w) acc += *(const Quad *)&shared[w][d];
+    }
     const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
     Vec<T, 4> o;
 #pragma unroll
@@ -457,16 +505,19 @@ int64_t align16(int64_t n) { return (n + 15) / 16 * 16; }
 
 int head_tiles_of(const hp_packed_attend_args_t &a) { return (a.heads_q / a.heads_k + kHeads - 1) / kHeads; }
 
+int waves_of(int groups) { return groups <= 4 ? kWaves<4> : kWaves<8>; }
+template <class T> int resident_of(int groups) { return groups <= 2 ? kResident<T, 2> : groups <= 3 ? kResident<T, 3> : groups <= 4 ? kResident<T, 4> : kResident<T, 8>; }
+
 // Units of each tile of heads: as many as run at once, or, of few heads' rows each, four times as many workgroups.  0: the
 // rows are enough by themselves, or too many to be added up.
 int32_t units_of(const hp_packed_attend_args_t &a) {
     const int64_t columns = (int64_t)a.heads_k * head_tiles_of(a), tiles = a.keys / kTile + 1;
     if (a.rows > kMostShared || a.rows * tiles > INT_MAX) return 0;
-    const int64_t groups = groups_of(a.dim), resident = a.dtype == HP_BF16 ? (groups <= 4 ? 4 : 2) : (groups <= 2 ? 3 : 2);
-    const int64_t slots = kComputeUnits * resident;
+    const int groups = groups_of(a.dim), waves = waves_of(groups);
+    const int64_t slots = kComputeUnits * (a.dtype == HP_BF16 ? resident_of<__bf16>(groups) : resident_of<float>(groups));
     int64_t units = slots / columns;
     if (units < 4) units = (4 * slots + columns - 1) / columns;
-    const int64_t most = (a.rows * tiles + kWaves - 1) / kWaves;
+    const int64_t most = (a.rows * tiles + waves - 1) / waves;
     return (int32_t)(units < most ? units : most);
 }
 
@@ -506,11 +557,21 @@ int check(const hp_packed_attend_args_t *a) {
     return HP_OK;
 }
 
+template <class T, int GP> void launch(const Params &p, const dim3 &grid, hipStream_t s) {
+    packed_attend_kernel<T, GP><<<grid, kWaves<GP> * kWave, 0, s>>>(p);
+}
 template <class T> void launch(const Params &p, const dim3 &grid, hipStream_t s) {
-    if (p.groups <= 2) packed_attend_kernel<T, 2><<<grid, kBlock, 0, s>>>(p);
-    else if (p.groups == 3) packed_attend_kernel<T, 3><<<grid, kBlock, 0, s>>>(p);
-    else if (p.groups == 4) packed_attend_kernel<T, 4><<<grid, kBlock, 0, s>>>(p);
-    else packed_attend_kernel<T, 8><<<grid, kBlock, 0, s>>>(p);
+    if (p.groups <= 2) launch<T, 2>(p, grid, s);
+    else if (p.groups == 3) launch<T, 3>(p, grid, s);
+    else if (p.groups == 4) launch<T, 4>(p, grid, s);
+    else launch<T, 8>(p, grid, s);
+}
+
+template <class T> void join(const Params &p, hipStream_t s) {
+    const int64_t items = p.rows * p.heads_q;
+    // few rows and heads have many parts each, many few
+    const int waves = items <= kComputeUnits ? kMostJoin : items <= 4 * kComputeUnits ? 4 : 1, each = waves == 1 ? 4 : 1;
+    packed_join_kernel<T><<<dim3((uint32_t)p.rows, (uint32_t)((p.heads_q + each - 1) / each)), waves * each * kWave, 0, s>>>(p, waves);
 }
 
 }  // namespace
@@ -542,9 +603,8 @@ int hp_packed_attend_step(const hp_packed_attend_args_t *a, void *stream) {
     else launch<float>(p, grid, s);
     if (hip_failed(hipGetLastError())) return HP_EHIP;
     if (p.units <= 1) return HP_OK;                // no row has parts
-    const dim3 joins((uint32_t)p.rows, (uint32_t)p.heads_q);
-    if (a->dtype == HP_BF16) packed_join_kernel<__bf16><<<joins, kBlock, 0, s>>>(p);
-    else packed_join_kernel<float><<<joins, kBlock, 0, s>>>(p);
+    if (a->dtype == HP_BF16) join<__bf16>(p, s);
+    else join<float>(p, s);
     return hip_failed(hipGetLastError()) ? HP_EHIP : HP_OK;
 }
 
