@@ -34,7 +34,7 @@ constexpr float kMiddle = 8.0f;
 struct Params {
     int64_t rows, keys;
     int32_t heads_q, group, groups, dim, head_tiles;
-    int32_t units;                                 // of each tile of heads; 0: each row is one
+    int32_t units, least;                          // of each tile of heads (0: each row is one), and the tiles that a unit has at least
     float scale2;                                  // for exponents of two
     hp_heads_t q, out;
     hp_packed_t k, v;
@@ -138,7 +138,7 @@ struct Share {
         return Range{__builtin_amdgcn_readlane(held.lo, (int)row), __builtin_amdgcn_readlane(held.hi, (int)row)};
     }
 };
-__device__ __forceinline__ Share share_of(const Params &p, int unit, int lane, int waves) {
+__device__ __forceinline__ Share share_of(const Params &p, int unit, int lane) {
     Share s{unit, 0, 0, 0, 0, 0, Range{}, false};
     if (!p.units) {
         s.left = range_of(p, unit).tiles();
@@ -161,7 +161,7 @@ __device__ __forceinline__ Share share_of(const Params &p, int unit, int lane, i
         if (lane >= d) upto += before;
     }
     s.total = __builtin_amdgcn_readlane(upto, kWave - 1);
-    s.units = min(p.units, (s.total + waves - 1) / waves);         // none with less than a tile for each wave
+    s.units = min(p.units, (s.total + p.least - 1) / p.least);
     s.at = unit < s.units ? first_of(s.total, unit, s.units) : 0;
     s.left = unit < s.units ? first_of(s.total, unit + 1, s.units) - s.at : 0;
     // the lane whose rows have that tile, then the row
@@ -195,13 +195,15 @@ constexpr float kLag = 8.0f;                       // the maximum is raised when
 // or four of 40 do not share: 1024 of these took two turns, 64 requests 88 us instead of 77).
 template <int GP> constexpr int kWaves = GP == 8 ? 7 : 4;
 template <class T, int GP> constexpr int kResident = sizeof(T) == 2 ? (GP <= 3 ? 4 : GP == 4 ? 3 : 1) : (GP <= 2 ? 3 : GP <= 4 ? 2 : 1);
-template <class T, int GP> constexpr int kWavesASimd = (kWaves<GP> * kResident<T, GP> + 3) / 4;
+// Few rows: a workgroup a compute unit, with more waves, so that short ranges are not cut.
+template <int GP> constexpr int kFewWaves = GP == 8 ? 7 : 8;
+template <class T, int GP, int WAVES> constexpr int kWavesASimd = WAVES == kWaves<GP> ? (WAVES * kResident<T, GP> + 3) / 4 : (WAVES + 3) / 4;
 
-template <class T, int GP> __global__ __launch_bounds__((kWaves<GP> * kWave), (kWavesASimd<T, GP>)) void packed_attend_kernel(Params p) {
+template <class T, int GP, int WAVES> __global__ __launch_bounds__((WAVES * kWave), (kWavesASimd<T, GP, WAVES>)) void packed_attend_kernel(Params p) {
     typedef Layout<GP> L;
     constexpr float kLift = Codes<T>::kLift;
     constexpr bool kCentred = kLift == -kMiddle;
-    constexpr int N = kTerms<T>, kSets = (GP + 3) / 4, kWaves = ::kWaves<GP>;
+    constexpr int N = kTerms<T>, kSets = (GP + 3) / 4, kWaves = WAVES;
     __shared__ __attribute__((aligned(16))) char lds[kWaves * L::kBytes];
     static_assert(sizeof(lds) >= 16 * kWaves * 2 * GP * kWave + 8 * kWaves * kHeads, "room for the join");
     const int tid = (int)threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), col = lane % 16, quarter = lane / 16;
@@ -217,7 +219,7 @@ template <class T, int GP> __global__ __launch_bounds__((kWaves<GP> * kWave), (k
     const Frag centre = all_of(-kLift - kMiddle);
     const Codes<T> codes;
 
-    Share share = share_of(p, unit, lane, kWaves);
+    Share share = share_of(p, unit, lane);
   for (; share.left > 0; ++share.row, share.skip = 0) {
     const int64_t row = share.row;
     const Range see = share.now(p);
@@ -505,20 +507,28 @@ int64_t align16(int64_t n) { return (n + 15) / 16 * 16; }
 
 int head_tiles_of(const hp_packed_attend_args_t &a) { return (a.heads_q / a.heads_k + kHeads - 1) / kHeads; }
 
-int waves_of(int groups) { return groups <= 4 ? kWaves<4> : kWaves<8>; }
 template <class T> int resident_of(int groups) { return groups <= 2 ? kResident<T, 2> : groups <= 3 ? kResident<T, 3> : groups <= 4 ? kResident<T, 4> : kResident<T, 8>; }
 
-// Units of each tile of heads: as many as run at once, or, of few heads' rows each, four times as many workgroups.  0: the
-// rows are enough by themselves, or too many to be added up.
-int32_t units_of(const hp_packed_attend_args_t &a) {
+// Units of each tile of heads, how many tiles each has at least, and whether its workgroup has more waves.
+struct Cut {
+    int32_t units, least;
+    bool few;
+};
+Cut cut_of(const hp_packed_attend_args_t &a) {
     const int64_t columns = (int64_t)a.heads_k * head_tiles_of(a), tiles = a.keys / kTile + 1;
-    if (a.rows > kMostShared || a.rows * tiles > INT_MAX) return 0;
-    const int groups = groups_of(a.dim), waves = waves_of(groups);
+    // 0: the rows are enough by themselves, or too many to be added up
+    if (a.rows > kMostShared || a.rows * tiles > INT_MAX) return Cut{0, 1, false};
+    const int groups = groups_of(a.dim), waves = groups <= 2 ? kWaves<2> : groups <= 3 ? kWaves<3> : groups <= 4 ? kWaves<4> : kWaves<8>;
+    const int few = groups <= 4 ? kFewWaves<4> : kFewWaves<8>;
+    // two tiles a wave of larger workgroups, if these are no more than compute units: joining parts is a launch more
+    const int64_t units = (a.rows * tiles + 2 * few - 1) / (2 * few);
+    if (units * columns <= kComputeUnits) return Cut{(int32_t)units, 2 * few, true};
     const int64_t slots = kComputeUnits * (a.dtype == HP_BF16 ? resident_of<__bf16>(groups) : resident_of<float>(groups));
-    int64_t units = slots / columns;
-    if (units < 4) units = (4 * slots + columns - 1) / columns;
+    // as many as run at once, or, of few rows each, four times as many workgroups
+    int64_t n = slots / columns;
+    if (n < 4) n = (4 * slots + columns - 1) / columns;
     const int64_t most = (a.rows * tiles + waves - 1) / waves;
-    return (int32_t)(units < most ? units : most);
+    return Cut{(int32_t)(n < most ? n : most), waves, false};
 }
 
 int check_sizes(const hp_packed_attend_args_t *a) {
@@ -535,7 +545,7 @@ int check_sizes(const hp_packed_attend_args_t *a) {
 int part_heads_of(const hp_packed_attend_args_t &a) { return a.heads_q / a.heads_k < kHeads ? a.heads_q / a.heads_k : kHeads; }
 
 int64_t workspace_of(const hp_packed_attend_args_t &a) {
-    const int64_t units = a.rows > 0 ? units_of(a) : 0, parts = 2 * units * a.heads_k * head_tiles_of(a) * part_heads_of(a);
+    const int64_t units = a.rows > 0 ? cut_of(a).units : 0, parts = 2 * units * a.heads_k * head_tiles_of(a) * part_heads_of(a);
     return units > 0 ? align16(4 * parts * a.dim) + align16(4 * parts) + align16(8 * a.rows) : 0;
 }
 
@@ -557,14 +567,15 @@ int check(const hp_packed_attend_args_t *a) {
     return HP_OK;
 }
 
-template <class T, int GP> void launch(const Params &p, const dim3 &grid, hipStream_t s) {
-    packed_attend_kernel<T, GP><<<grid, kWaves<GP> * kWave, 0, s>>>(p);
+template <class T, int GP> void launch(bool few, const Params &p, const dim3 &grid, hipStream_t s) {
+    if (few) packed_attend_kernel<T, GP, kFewWaves<GP>><<<grid, kFewWaves<GP> * kWave, 0, s>>>(p);
+    else packed_attend_kernel<T, GP, kWaves<GP>><<<grid, kWaves<GP> * kWave, 0, s>>>(p);
 }
-template <class T> void launch(const Params &p, const dim3 &grid, hipStream_t s) {
-    if (p.groups <= 2) launch<T, 2>(p, grid, s);
-    else if (p.groups == 3) launch<T, 3>(p, grid, s);
-    else if (p.groups == 4) launch<T, 4>(p, grid, s);
-    else launch<T, 8>(p, grid, s);
+template <class T> void launch(bool few, const Params &p, const dim3 &grid, hipStream_t s) {
+    if (p.groups <= 2) launch<T, 2>(few, p, grid, s);
+    else if (p.groups == 3) launch<T, 3>(few, p, grid, s);
+    else if (p.groups == 4) launch<T, 4>(few, p, grid, s);
+    else launch<T, 8>(few, p, grid, s);
 }
 
 template <class T> void join(const Params &p, hipStream_t s) {
@@ -590,7 +601,8 @@ int hp_packed_attend_step(const hp_packed_attend_args_t *a, void *stream) {
     Params p{};
     p.rows = a->rows, p.keys = a->keys;
     p.heads_q = a->heads_q, p.group = a->heads_q / a->heads_k, p.groups = groups_of(a->dim), p.dim = a->dim;
-    p.units = units_of(*a), p.head_tiles = head_tiles_of(*a), p.part_heads = part_heads_of(*a);
+    const Cut cut = cut_of(*a);
+    p.units = cut.units, p.least = cut.least, p.head_tiles = head_tiles_of(*a), p.part_heads = part_heads_of(*a);
     p.scale2 = a->scale * kLog2e;
     p.q = a->q, p.out = a->out, p.k = a->k, p.v = a->v, p.ranges = a->ranges, p.lse = a->lse;
     const int64_t parts = (int64_t)2 * p.units * a->heads_k * p.head_tiles * p.part_heads;
@@ -599,8 +611,8 @@ int hp_packed_attend_step(const hp_packed_attend_args_t *a, void *stream) {
     p.lse2 = (float *)(ws + align16(4 * parts * p.dim));
     p.row_units = (int2 *)(ws + align16(4 * parts * p.dim) + align16(4 * parts));
     const dim3 grid((uint32_t)(p.units ? p.units : p.rows), (uint32_t)(a->heads_k * p.head_tiles));
-    if (a->dtype == HP_BF16) launch<__bf16>(p, grid, s);
-    else launch<float>(p, grid, s);
+    if (a->dtype == HP_BF16) launch<__bf16>(cut.few, p, grid, s);
+    else launch<float>(cut.few, p, grid, s);
     if (hip_failed(hipGetLastError())) return HP_EHIP;
     if (p.units <= 1) return HP_OK;                // no row has parts
     if (a->dtype == HP_BF16) join<__bf16>(p, s);
