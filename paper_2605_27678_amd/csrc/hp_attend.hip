@@ -39,7 +39,6 @@
 #include <type_traits>
 
 #include "hp_device.hpp"
-#include "hp_join.hpp"
 #include "hp_meet.hpp"
 #include "hp_operators.h"
 
@@ -674,7 +673,7 @@ template <class T, int DP, bool EXACT> __global__ __launch_bounds__((kStepWaves<
 // parts are a workgroup's, its waves take every fourth: one wave going through them one behind the other took 45 us of the
 // 54 for one token against 8000 states in 62 parts.  Few are a wave's: 49200 rows and heads of two parts 19 us, with
 // a workgroup each 48.
-constexpr int kFewParts = 8;
+constexpr int kMostParts = kWave, kFewParts = 8;
 template <class T> __global__ __launch_bounds__(kBlock) void attend_join_kernel(Attend p) {
     __shared__ __attribute__((aligned(16))) float half_done[kWaves][HP_ATTEND_MAX_DIM];
     const int lane = (int)threadIdx.x % kWave, wave = (int)threadIdx.x / kWave;
@@ -1206,14 +1205,6 @@ void launch(Kernel what, int dtype, const Attend &p, const dim3 &grid, hipStream
     else launch<float>(what, p, grid, s);
 }
 
-int join(const Attend &p, int dtype, hipStream_t s) {
-    const int64_t items = p.rows * p.heads_q;
-    const uint32_t blocks = (uint32_t)(p.splits <= kFewParts ? (items + kWaves - 1) / kWaves : items);
-    if (dtype == HP_BF16) attend_join_kernel<__bf16><<<blocks, kBlock, 0, s>>>(p);
-    else attend_join_kernel<float><<<blocks, kBlock, 0, s>>>(p);
-    return failed() ? HP_EHIP : HP_OK;
-}
-
 // Forward in either shape: the launch, and the join of the parts.
 int forward(const hp_attend_args_t &a, Kernel what, const dim3 &grid, hipStream_t s) {
     Attend p = params_of(a);
@@ -1224,7 +1215,14 @@ int forward(const hp_attend_args_t &a, Kernel what, const dim3 &grid, hipStream_
     }
     launch(what, a.dtype, p, grid, s);
     if (failed()) return HP_EHIP;
-    return p.splits > 1 ? join(p, a.dtype, s) : HP_OK;
+    if (p.splits > 1) {
+        const int64_t items = p.rows * p.heads_q;
+        const uint32_t blocks = (uint32_t)(p.splits <= kFewParts ? (items + kWaves - 1) / kWaves : items);
+        if (a.dtype == HP_BF16) attend_join_kernel<__bf16><<<blocks, kBlock, 0, s>>>(p);
+        else attend_join_kernel<float><<<blocks, kBlock, 0, s>>>(p);
+        if (failed()) return HP_EHIP;
+    }
+    return HP_OK;
 }
 
 int add_up(const float *part, int splits, int dtype, int64_t rows, int heads, int dim, const hp_heads_t &out, hipStream_t s) {
@@ -1235,13 +1233,6 @@ int add_up(const float *part, int splits, int dtype, int64_t rows, int heads, in
 }
 
 }  // namespace
-
-int hp::join_parts(const Parts &n, int dtype, int64_t rows, int heads_q, int dim, const hp_heads_t &out, float *lse, hipStream_t s) {
-    Attend p{};
-    p.rows = rows, p.heads_q = heads_q, p.dim = dim, p.splits = n.splits, p.out = out, p.lse = lse;
-    p.part = n.products, p.part_lse = n.lse2;
-    return join(p, dtype, s);
-}
 
 extern "C" {
 

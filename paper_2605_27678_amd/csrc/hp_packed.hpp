@@ -66,14 +66,6 @@ __device__ __forceinline__ Frag all_of(float x) {
 __device__ __forceinline__ float step_of(uint32_t pair) { return __uint_as_float(pair << 16); }
 __device__ __forceinline__ float low_of(uint32_t pair) { return __uint_as_float(pair & 0xffff0000u); }
 
-// Of four lanes l, l + 16, l + 32, l + 48 with four words each: word t of the q-th of them and word q of the t-th change
-// places.
-__device__ __forceinline__ void across_quarters(Words &w) {
-    const auto a = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false), b = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
-    const auto c = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false), d = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
-    w = Words{c[0], c[1], d[0], d[1]};
-}
-
 // The bfloat16 numbers that stand for a value of type T as an operand: itself, or three that add up to its 24 bits.
 template <class T> constexpr int kTerms = sizeof(T) == 2 ? 1 : 3;
 template <int N> __device__ __forceinline__ void terms(float x, Frag (&f)[N], int i) {
@@ -125,8 +117,14 @@ inline int check_packed(const hp_packed_t &t, int64_t rows, int64_t heads) {
     if (heads > 1 && (t.code_head_stride % 16 || t.scale_head_stride % 2)) return HP_EALIGN;
     return HP_OK;
 }
+// Row strides that offsets of 32 bits hold for a tile's rows; a single row has none.
 inline bool short_strides(const hp_packed_t &t, int64_t rows) {
     return rows <= 1 || (t.code_row_stride >= 0 && t.code_row_stride <= kMostStride && t.scale_row_stride >= 0 && t.scale_row_stride <= kMostStride);
+}
+
+inline hp_packed_t without_unused(hp_packed_t t, int64_t rows) {
+    if (rows <= 1) t.code_row_stride = t.scale_row_stride = 0;
+    return t;
 }
 
 }  // namespace hp

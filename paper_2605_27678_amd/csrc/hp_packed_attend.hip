@@ -5,8 +5,7 @@
 // in one pass with a running maximum m and sum.  The codes go into the matrix units as they are (hp_packed.hpp).
 //
 // A wave takes 64 states at a time by itself.  S^T = K Q^T, so that a lane has scores of one head, four states of each 16.
-// Its four words of a 16-byte group change places with those of three other lanes, and it has 8 channels of one state for
-// each product.  The steps go over a group's 16 x 16 results before they add up: each lane reads those of one state, and a
+// A word of codes is a lane's 8 channels of one state, an operand as it is.  The steps go over a group's 16 x 16 results before they add up: each lane reads those of one state, and a
 // multiplication takes them from whichever lane of its row has them.  (Read from LDS by every lane that needs them they were
 // 32 of 56 LDS reads of 16 bytes, and 120 us for 64 requests of 576 to 6404 states.)  out^T = V^T P^T has the states as inner
 // values: the transposing LDS load brings a lane 16 states of one channel, in the order in which it has their weights, so
@@ -44,7 +43,7 @@ struct Params {
     // products [heads_k * head_tiles][units][2][part_heads][dim], lse2 the same without dim, rows [rows] first and last unit.
     float *products, *lse2;
     int2 *row_units;
-    int32_t part_heads, reserved;
+    int32_t part_heads;
 };
 
 // The 64 states of a wave in LDS: of each tensor codes [64][GP] of 16 bytes, a row's groups turned so that the same group
@@ -220,238 +219,238 @@ template <class T, int GP, int WAVES> __global__ __launch_bounds__((WAVES * kWav
     const Codes<T> codes;
 
     Share share = share_of(p, unit, lane);
-  for (; share.left > 0; ++share.row, share.skip = 0) {
-    const int64_t row = share.row;
-    const Range see = share.now(p);
-    const int lo = see.lo, hi = see.hi, n_tiles = see.tiles();
-    const int begin = share.skip, end = min(n_tiles, begin + share.left);
-    share.left -= end - begin;
-    const bool whole = begin == 0 && end == n_tiles;
-    if (p.units && begin == 0 && blockIdx.y == 0 && tid == 0) {
-        const int first = share.at;                // its place among all tiles
-        p.row_units[row] = make_int2(unit, whole ? unit : unit_of(share.total, first + n_tiles - 1, share.units));
-    }
-    share.at += end - begin;
-
-    // the queries, and the right operand that puts the lows in: for each pair (step, low) of four groups the values
-    // (-lift sum q, sum q), split into three numbers over the quarters
-    Frag q[GP][N], sums[kSets] = {};
-    const T *q_row = (const T *)p.q.data + row * p.q.row_stride + (int64_t)(head0 + min(col, heads - 1)) * p.q.head_stride;
-    Vec<T, 8> x[GP];
-    int dim = p.dim;
-    asm volatile("" : "+s"(dim));                  // or the places of all channels would be kept over the rows
-    if (dim % 8 == 0) {                            // pieces are there or not
-#pragma unroll
-        for (int g = 0; g < GP; ++g) {
-            const int d = kGroup * g + 8 * quarter;
-            x[g] = *(const typename VecOf<T, 8>::mem *)(q_row + (d < dim ? d : 0));
-            if (d >= dim) x[g] = Vec<T, 8>{};
+    for (; share.left > 0; ++share.row, share.skip = 0) {
+        const int64_t row = share.row;
+        const Range see = share.now(p);
+        const int lo = see.lo, hi = see.hi, n_tiles = see.tiles();
+        const int begin = share.skip, end = min(n_tiles, begin + share.left);
+        share.left -= end - begin;
+        const bool whole = begin == 0 && end == n_tiles;
+        if (p.units && begin == 0 && blockIdx.y == 0 && tid == 0) {
+            const int first = share.at;                // its place among all tiles
+            p.row_units[row] = make_int2(unit, whole ? unit : unit_of(share.total, first + n_tiles - 1, share.units));
         }
-    } else {
-#pragma unroll
-        for (int g = 0; g < GP; ++g) {
-            const int d = kGroup * g + 8 * quarter;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const T one = q_row[min(d + i, dim - 1)];
-                x[g][i] = d + i < dim ? one : (T)0.0f;
+        share.at += end - begin;
+
+        // the queries, and the right operand that puts the lows in: for each pair (step, low) of four groups the values
+        // (-lift sum q, sum q), split into three numbers over the quarters
+        Frag q[GP][N], sums[kSets] = {};
+        const T *q_row = (const T *)p.q.data + row * p.q.row_stride + (int64_t)(head0 + min(col, heads - 1)) * p.q.head_stride;
+        Vec<T, 8> x[GP];
+        int dim = p.dim;
+        asm volatile("" : "+s"(dim));                  // or the places of all channels would be kept over the rows
+        if (dim % 8 == 0) {                            // pieces are there or not
+    #pragma unroll
+            for (int g = 0; g < GP; ++g) {
+                const int d = kGroup * g + 8 * quarter;
+                x[g] = *(const typename VecOf<T, 8>::mem *)(q_row + (d < dim ? d : 0));
+                if (d >= dim) x[g] = Vec<T, 8>{};
             }
-            __builtin_amdgcn_sched_barrier(0);     // no more of them at a time than registers hold
-        }
-    }
-    // the first tiles are under way while the queries are made operands
-    __builtin_amdgcn_sched_barrier(0);
-    if (begin + wave < end) {
-        const int key0 = lo + (begin + wave) * kTile;
-        ks.fetch(k_tile, p.k, key0, state_head, hi - key0, lane);
-        vs.fetch(v_tile, p.v, key0, state_head, hi - key0, lane);
-    }
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int g = 0; g < GP; ++g) {
-        terms<T>(x[g], q[g]);
-        float sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum += (float)x[g][i];
-        sum = column_sum(sum);
-        const __bf16 a = (__bf16)sum, b = (__bf16)(sum - (float)a), c = (__bf16)(sum - (float)a - (float)b);
-        const float part = quarter == 0 ? (float)a : quarter == 1 ? (float)b : quarter == 2 ? (float)c : 0.0f;
-        sums[g / 4][2 * (g % 4)] = (__bf16)(-kLift * part);
-        sums[g / 4][2 * (g % 4) + 1] = (__bf16)part;
-    }
-
-    float top = -INFINITY, sum = 0.0f;
-    Quad out[2 * GP] = {}, rest = {};
-    for (int tile = begin + wave; tile < end; tile += kWaves) {
-        const int key0 = lo + tile * kTile, next = key0 + kWaves * kTile;
-        const bool more = tile + kWaves < end;
-        __builtin_amdgcn_s_waitcnt(but(Loader<GP>::kLoads));   // all but V's
-        settle();
-        Quad s[4];
-        const Vec<uint32_t, L::kPairs> k_pairs = *(const Vec<uint32_t, L::kPairs> *)(k_scales + L::kPairs * own);
-#pragma unroll
-        for (int a = 0; a < 4; ++a) {
-            s[a] = Quad{};
-            const Vec<uint32_t, L::kPairs> pairs = *(const Vec<uint32_t, L::kPairs> *)(k_scales + L::kPairs * (16 * a + col));
-#pragma unroll
-            for (int h = 0; h < kSets; ++h) {
-                Words w = {};
-#pragma unroll
-                for (int j = 0; j < 4 && 4 * h + j < L::kPairs; ++j) w[j] = pairs[4 * h + j];
-                s[a] = mma(__builtin_bit_cast(Frag, w), sums[h], s[a]);
-            }
-        }
-        each<GP>([&](auto g) {
-            each<4>([&](auto a) {
-                const Frag c = codes(*(const uint32_t *)(k_tile + L::at(16 * a + col, g) + 4 * quarter));
-                Quad d = {};
-#pragma unroll
-                for (int n = 0; n < N; ++n) d = mma(c, q[g][n], d);
-                each<4>([&](auto i) { s[a][i.value] += of_lane<4 * a + i>(step_of(k_pairs[g.value])) * d[i.value]; });
-            });
-        });
-        // here, not behind the branch, where all these products' results would have to be kept until then
-#pragma unroll
-        for (int a = 0; a < 4; ++a) asm("" : "+v"(s[a]));
-        reads_done();
-        if (more) ks.fetch(k_tile, p.k, next, state_head, hi - next, lane);
-
-        if (key0 + kTile > hi)
-#pragma unroll
-            for (int a = 0; a < 4; ++a)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) s[a][i] = key0 + 16 * a + 4 * quarter + i < hi ? s[a][i] : -INFINITY;
-        float most = s[0][0];
-#pragma unroll
-        for (int a = 0; a < 4; ++a)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) most = fmaxf(most, s[a][i]);
-        most = column_max(most) * p.scale2;
-        const bool grows = most > top + kLag;
-        if (__any(grows)) {
-            const float keep = grows ? __builtin_amdgcn_exp2f(top - most) : 1.0f;
-            top = grows ? most : top;
-            sum *= keep;
-            rest *= keep;
-#pragma unroll
-            for (int c = 0; c < 2 * GP; ++c) out[c] *= keep;
-        }
-        const float base = top == -INFINITY ? 0.0f : top;
-#pragma unroll
-        for (int a = 0; a < 4; ++a)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                s[a][i] = __builtin_amdgcn_exp2f(s[a][i] * p.scale2 - base);
-                sum += s[a][i];
-            }
-
-        if (more) __builtin_amdgcn_s_waitcnt(but(Loader<GP>::kLoads));
-        else __builtin_amdgcn_s_waitcnt(but(0));
-        settle();
-        // 8 sum p step + sum p low: row 2g of the left operand has group g's steps, row 2g + 1 its lows
-        {
-            typedef short Four __attribute__((ext_vector_type(4)));
-            typedef __attribute__((address_space(3))) Four *Lds;
-            // 16 lanes bring four states' pairs, 8 bytes a lane; beyond a state's pairs rows of the product are not read
-            const uint32_t *line = v_scales + L::kPairs * (4 * quarter + col / 4) + 2 * (col % 4 % (L::kPairs / 2));
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const Four even = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(line + L::kPairs * 32 * b)), odd = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(line + L::kPairs * (32 * b + 16)));
-                const Frag pairs = __builtin_bit_cast(Frag, __builtin_shufflevector(even, odd, 0, 1, 2, 3, 4, 5, 6, 7));
-                Frag weights[N];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    terms(s[2 * b][i], weights, i);
-                    terms(s[2 * b + 1][i], weights, 4 + i);
+        } else {
+    #pragma unroll
+            for (int g = 0; g < GP; ++g) {
+                const int d = kGroup * g + 8 * quarter;
+    #pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const T one = q_row[min(d + i, dim - 1)];
+                    x[g][i] = d + i < dim ? one : (T)0.0f;
                 }
-#pragma unroll
-                for (int n = 0; n < N; ++n) rest = mma(pairs, weights[n], rest);
+                __builtin_amdgcn_sched_barrier(0);     // no more of them at a time than registers hold
             }
         }
-        const Vec<uint32_t, L::kPairs> v_pairs = *(const Vec<uint32_t, L::kPairs> *)(v_scales + L::kPairs * own);
-        each<GP>([&](auto g) {
-            Frag weights[2][N];
-            each<8>([&](auto e) {
-                constexpr int b = e / 4, i = e % 4;
-                const float step = step_of(v_pairs[g.value]);
-                terms(of_lane<8 * b + i>(step) * s[2 * b][i], weights[b], 2 * i);
-                terms(of_lane<8 * b + 4 + i>(step) * s[2 * b + 1][i], weights[b], 2 * i + 1);
+        // the first tiles are under way while the queries are made operands
+        __builtin_amdgcn_sched_barrier(0);
+        if (begin + wave < end) {
+            const int key0 = lo + (begin + wave) * kTile;
+            ks.fetch(k_tile, p.k, key0, state_head, hi - key0, lane);
+            vs.fetch(v_tile, p.v, key0, state_head, hi - key0, lane);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    #pragma unroll
+        for (int g = 0; g < GP; ++g) {
+            terms<T>(x[g], q[g]);
+            float sum = 0.0f;
+    #pragma unroll
+            for (int i = 0; i < 8; ++i) sum += (float)x[g][i];
+            sum = column_sum(sum);
+            const __bf16 a = (__bf16)sum, b = (__bf16)(sum - (float)a), c = (__bf16)(sum - (float)a - (float)b);
+            const float part = quarter == 0 ? (float)a : quarter == 1 ? (float)b : quarter == 2 ? (float)c : 0.0f;
+            sums[g / 4][2 * (g % 4)] = (__bf16)(-kLift * part);
+            sums[g / 4][2 * (g % 4) + 1] = (__bf16)part;
+        }
+
+        float top = -INFINITY, sum = 0.0f;
+        Quad out[2 * GP] = {}, rest = {};
+        for (int tile = begin + wave; tile < end; tile += kWaves) {
+            const int key0 = lo + tile * kTile, next = key0 + kWaves * kTile;
+            const bool more = tile + kWaves < end;
+            __builtin_amdgcn_s_waitcnt(but(Loader<GP>::kLoads));   // all but V's
+            settle();
+            Quad s[4];
+            const Vec<uint32_t, L::kPairs> k_pairs = *(const Vec<uint32_t, L::kPairs> *)(k_scales + L::kPairs * own);
+    #pragma unroll
+            for (int a = 0; a < 4; ++a) {
+                s[a] = Quad{};
+                const Vec<uint32_t, L::kPairs> pairs = *(const Vec<uint32_t, L::kPairs> *)(k_scales + L::kPairs * (16 * a + col));
+    #pragma unroll
+                for (int h = 0; h < kSets; ++h) {
+                    Words w = {};
+    #pragma unroll
+                    for (int j = 0; j < 4 && 4 * h + j < L::kPairs; ++j) w[j] = pairs[4 * h + j];
+                    s[a] = mma(__builtin_bit_cast(Frag, w), sums[h], s[a]);
+                }
+            }
+            each<GP>([&](auto g) {
+                each<4>([&](auto a) {
+                    const Frag c = codes(*(const uint32_t *)(k_tile + L::at(16 * a + col, g) + 4 * quarter));
+                    Quad d = {};
+    #pragma unroll
+                    for (int n = 0; n < N; ++n) d = mma(c, q[g][n], d);
+                    each<4>([&](auto i) { s[a][i.value] += of_lane<4 * a + i>(step_of(k_pairs[g.value])) * d[i.value]; });
+                });
             });
-            typedef int Pair __attribute__((ext_vector_type(2)));
-            typedef __attribute__((address_space(3))) Pair *Lds;
-            const char *line = v_tile + L::at(own, g);
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const Pair w = __builtin_amdgcn_ds_read_tr4_b64_v2i32((Lds)(line + 8 * c));
-#pragma unroll
+            // here, not behind the branch, where all these products' results would have to be kept until then
+    #pragma unroll
+            for (int a = 0; a < 4; ++a) asm("" : "+v"(s[a]));
+            reads_done();
+            if (more) ks.fetch(k_tile, p.k, next, state_head, hi - next, lane);
+
+            if (key0 + kTile > hi)
+    #pragma unroll
+                for (int a = 0; a < 4; ++a)
+    #pragma unroll
+                    for (int i = 0; i < 4; ++i) s[a][i] = key0 + 16 * a + 4 * quarter + i < hi ? s[a][i] : -INFINITY;
+            float most = s[0][0];
+    #pragma unroll
+            for (int a = 0; a < 4; ++a)
+    #pragma unroll
+                for (int i = 0; i < 4; ++i) most = fmaxf(most, s[a][i]);
+            most = column_max(most) * p.scale2;
+            const bool grows = most > top + kLag;
+            if (__any(grows)) {
+                const float keep = grows ? __builtin_amdgcn_exp2f(top - most) : 1.0f;
+                top = grows ? most : top;
+                sum *= keep;
+                rest *= keep;
+    #pragma unroll
+                for (int c = 0; c < 2 * GP; ++c) out[c] *= keep;
+            }
+            const float base = top == -INFINITY ? 0.0f : top;
+    #pragma unroll
+            for (int a = 0; a < 4; ++a)
+    #pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    s[a][i] = __builtin_amdgcn_exp2f(s[a][i] * p.scale2 - base);
+                    sum += s[a][i];
+                }
+
+            if (more) __builtin_amdgcn_s_waitcnt(but(Loader<GP>::kLoads));
+            else __builtin_amdgcn_s_waitcnt(but(0));
+            settle();
+            // 8 sum p step + sum p low: row 2g of the left operand has group g's steps, row 2g + 1 its lows
+            {
+                typedef short Four __attribute__((ext_vector_type(4)));
+                typedef __attribute__((address_space(3))) Four *Lds;
+                // 16 lanes bring four states' pairs, 8 bytes a lane; beyond a state's pairs rows of the product are not read
+                const uint32_t *line = v_scales + L::kPairs * (4 * quarter + col / 4) + 2 * (col % 4 % (L::kPairs / 2));
+    #pragma unroll
                 for (int b = 0; b < 2; ++b) {
-                    const Frag l = codes((uint32_t)w[b]);
-#pragma unroll
-                    for (int n = 0; n < N; ++n) {
-                        if constexpr (!kCentred) out[2 * g + c] = mma(centre, weights[b][n], out[2 * g + c]);
-                        out[2 * g + c] = mma(l, weights[b][n], out[2 * g + c]);
+                    const Four even = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(line + L::kPairs * 32 * b)), odd = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(line + L::kPairs * (32 * b + 16)));
+                    const Frag pairs = __builtin_bit_cast(Frag, __builtin_shufflevector(even, odd, 0, 1, 2, 3, 4, 5, 6, 7));
+                    Frag weights[N];
+    #pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        terms(s[2 * b][i], weights, i);
+                        terms(s[2 * b + 1][i], weights, 4 + i);
+                    }
+    #pragma unroll
+                    for (int n = 0; n < N; ++n) rest = mma(pairs, weights[n], rest);
+                }
+            }
+            const Vec<uint32_t, L::kPairs> v_pairs = *(const Vec<uint32_t, L::kPairs> *)(v_scales + L::kPairs * own);
+            each<GP>([&](auto g) {
+                Frag weights[2][N];
+                each<8>([&](auto e) {
+                    constexpr int b = e / 4, i = e % 4;
+                    const float step = step_of(v_pairs[g.value]);
+                    terms(of_lane<8 * b + i>(step) * s[2 * b][i], weights[b], 2 * i);
+                    terms(of_lane<8 * b + 4 + i>(step) * s[2 * b + 1][i], weights[b], 2 * i + 1);
+                });
+                typedef int Pair __attribute__((ext_vector_type(2)));
+                typedef __attribute__((address_space(3))) Pair *Lds;
+                const char *line = v_tile + L::at(own, g);
+    #pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const Pair w = __builtin_amdgcn_ds_read_tr4_b64_v2i32((Lds)(line + 8 * c));
+    #pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        const Frag l = codes((uint32_t)w[b]);
+    #pragma unroll
+                        for (int n = 0; n < N; ++n) {
+                            if constexpr (!kCentred) out[2 * g + c] = mma(centre, weights[b][n], out[2 * g + c]);
+                            out[2 * g + c] = mma(l, weights[b][n], out[2 * g + c]);
+                        }
                     }
                 }
-            }
-        });
-        reads_done();
-        if (more) vs.fetch(v_tile, p.v, next, state_head, hi - next, lane);
-    }
-    sum = column_sum(sum);
+            });
+            reads_done();
+            if (more) vs.fetch(v_tile, p.v, next, state_head, hi - next, lane);
+        }
+        sum = column_sum(sum);
 
-    // join the waves in the tiles' place: statistics, then the products, of which each wave adds up every kWaves-th tile
-    Quad *const join = (Quad *)lds;                // [wave][2 GP][lane]
-    float *const tops = (float *)(join + kWaves * 2 * GP * kWave), *const totals = tops + kWaves * kHeads;
-    __syncthreads();
-    if (quarter == 0) {
-        tops[wave * kHeads + col] = top;
-        totals[wave * kHeads + col] = sum;
-    }
-    __syncthreads();
-    float most = -INFINITY, total = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) most = fmaxf(most, tops[w * kHeads + col]);
-    // a wave without a maximum has seen nothing, or NaN alone
-    const auto weight = [&](float t) { return t == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(t - most); };
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) total += totals[w * kHeads + col] * weight(tops[w * kHeads + col]);
-    const float part_of_all = total == 0.0f ? 0.0f : weight(top) / total;
-    const float lse2 = total == 0.0f ? -INFINITY : most + __builtin_amdgcn_logf(total);
-#pragma unroll
-    for (int g = 0; g < GP; ++g) {
-        const int from = 16 * (g / 2) + col;
-        const float more = kMiddle * __shfl(rest[2 * (g % 2)], from) + __shfl(rest[2 * (g % 2) + 1], from);
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            // rows of the transposed load are a word's bits in order: even channels in one quarter, odd ones in the next
-            const Quad v = (out[2 * g + c] + more) * part_of_all;
-            const float2 a = across_rows(v[0], v[2]), b = across_rows(v[1], v[3]);
-            join[(wave * 2 * GP + 2 * g + c) * kWave + lane] = Quad{a.x, a.y, b.x, b.y};
+        // join the waves in the tiles' place: statistics, then the products, of which each wave adds up every kWaves-th tile
+        Quad *const join = (Quad *)lds;                // [wave][2 GP][lane]
+        float *const tops = (float *)(join + kWaves * 2 * GP * kWave), *const totals = tops + kWaves * kHeads;
+        __syncthreads();
+        if (quarter == 0) {
+            tops[wave * kHeads + col] = top;
+            totals[wave * kHeads + col] = sum;
         }
-    }
-    __syncthreads();
-    const int64_t part = ((int64_t)blockIdx.y * p.units + unit) * 2 + (begin == 0);
-    for (int t = wave; t < 2 * GP; t += kWaves) {
-        const int d = 16 * t + 4 * quarter;
-        Quad v = {};
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) v += join[(w * 2 * GP + t) * kWave + lane];
-        if (col >= heads || d >= p.dim) continue;
-        if (!whole) {
-            store<4>(p.products + (part * p.part_heads + col) * p.dim + d, v, p.dim - d);
-        } else {
-            Vec<T, 4> o;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] = (T)v[i];
-            store<4>((T *)p.out.data + row * p.out.row_stride + (int64_t)(head0 + col) * p.out.head_stride + d, o, p.dim - d);
+        __syncthreads();
+        float most = -INFINITY, total = 0.0f;
+    #pragma unroll
+        for (int w = 0; w < kWaves; ++w) most = fmaxf(most, tops[w * kHeads + col]);
+        // a wave without a maximum has seen nothing, or NaN alone
+        const auto weight = [&](float t) { return t == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(t - most); };
+    #pragma unroll
+        for (int w = 0; w < kWaves; ++w) total += totals[w * kHeads + col] * weight(tops[w * kHeads + col]);
+        const float part_of_all = total == 0.0f ? 0.0f : weight(top) / total;
+        const float lse2 = total == 0.0f ? -INFINITY : most + __builtin_amdgcn_logf(total);
+    #pragma unroll
+        for (int g = 0; g < GP; ++g) {
+            const int from = 16 * (g / 2) + col;
+            const float more = kMiddle * __shfl(rest[2 * (g % 2)], from) + __shfl(rest[2 * (g % 2) + 1], from);
+    #pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                // rows of the transposed load are a word's bits in order: even channels in one quarter, odd ones in the next
+                const Quad v = (out[2 * g + c] + more) * part_of_all;
+                const float2 a = across_rows(v[0], v[2]), b = across_rows(v[1], v[3]);
+                join[(wave * 2 * GP + 2 * g + c) * kWave + lane] = Quad{a.x, a.y, b.x, b.y};
+            }
         }
+        __syncthreads();
+        const int64_t part = ((int64_t)blockIdx.y * p.units + unit) * 2 + (begin == 0);
+        for (int t = wave; t < 2 * GP; t += kWaves) {
+            const int d = 16 * t + 4 * quarter;
+            Quad v = {};
+    #pragma unroll
+            for (int w = 0; w < kWaves; ++w) v += join[(w * 2 * GP + t) * kWave + lane];
+            if (col >= heads || d >= p.dim) continue;
+            if (!whole) {
+                store<4>(p.products + (part * p.part_heads + col) * p.dim + d, v, p.dim - d);
+            } else {
+                Vec<T, 4> o;
+    #pragma unroll
+                for (int i = 0; i < 4; ++i) o[i] = (T)v[i];
+                store<4>((T *)p.out.data + row * p.out.row_stride + (int64_t)(head0 + col) * p.out.head_stride + d, o, p.dim - d);
+            }
+        }
+        if (wave == 0 && quarter == 0 && col < heads) {
+            if (!whole) p.lse2[part * p.part_heads + col] = lse2;
+            else if (p.lse) p.lse[row * p.heads_q + head0 + col] = lse2 * kLn2;
+        }
+        __syncthreads();                               // the next row's tiles come where this was
     }
-    if (wave == 0 && quarter == 0 && col < heads) {
-        if (!whole) p.lse2[part * p.part_heads + col] = lse2;
-        else if (p.lse) p.lse[row * p.heads_q + head0 + col] = lse2 * kLn2;
-    }
-    __syncthreads();                               // the next row's tiles come where this was
-  }
 }
 
 // Joins the parts of rows that lie in several units.  A row and head has `waves` waves, which take every waves-th part; a
@@ -537,8 +536,8 @@ int check_sizes(const hp_packed_attend_args_t *a) {
     if (a->dim < 1 || a->dim > HP_ATTEND_MAX_DIM || a->heads_k < 1 || a->heads_q < 1) return HP_EINVAL;
     if (a->heads_q % a->heads_k || a->heads_q > 16384) return HP_ELAYOUT;
     if (a->rows < 0 || a->keys < 0) return HP_EINVAL;
-    // 256 lanes a row, and in the join one wave or workgroup a row and head, of launches below 2^32
-    if (a->rows > 1 << 23 || a->rows * a->heads_q > (1 << 24) - 1 || a->keys > INT_MAX - 1024) return HP_ELAYOUT;
+    // up to 448 lanes a row, of launches below 2^32; states are counted in 32 bits, with tiles to spare
+    if (a->rows > 1 << 23 || a->rows > ((1 << 30) - 1024) / (a->heads_q / a->heads_k) || a->keys > INT_MAX - 1024) return HP_ELAYOUT;
     return HP_OK;
 }
 
@@ -604,7 +603,7 @@ int hp_packed_attend_step(const hp_packed_attend_args_t *a, void *stream) {
     const Cut cut = cut_of(*a);
     p.units = cut.units, p.least = cut.least, p.head_tiles = head_tiles_of(*a), p.part_heads = part_heads_of(*a);
     p.scale2 = a->scale * kLog2e;
-    p.q = a->q, p.out = a->out, p.k = a->k, p.v = a->v, p.ranges = a->ranges, p.lse = a->lse;
+    p.q = a->q, p.out = a->out, p.k = without_unused(a->k, a->keys), p.v = without_unused(a->v, a->keys), p.ranges = a->ranges, p.lse = a->lse;
     const int64_t parts = (int64_t)2 * p.units * a->heads_k * p.head_tiles * p.part_heads;
     char *ws = (char *)a->workspace;
     p.products = (float *)ws;

@@ -7,10 +7,7 @@
 // The waves of a workgroup share out the inner axis, 128 of it at a time, and add up at the end in their order.  Each brings its
 // own pieces of x and w to LDS, ahead of their use and without barriers: the operands' rows lie in neighbouring lanes, and
 // loads straight into registers took the caches 64 cycles each, one a lane, where runs of 64 and 256 bytes take 16
-// (12288 x 12288 by 16 rows: 36 us, with AAA).
-#include <climits>
-#include <cmath>
-
+// (12288 x 12288 by 16 rows: 36 us, this way 30).
 #include "hp_packed.hpp"
 
 #pragma clang fp contract(fast)
@@ -246,52 +243,48 @@ int check(const hp_packed_linear_args_t *a) {
     return short_strides(a->w, a->n_out) ? HP_OK : HP_ELAYOUT;
 }
 
-template <class C> void launch(Params &p, hipStream_t s) {
+// Workgroups of a launch, along w's rows and x's; p.waves_k is set for them.
+template <class C> dim3 blocks_of(Params &p) {
     const int64_t tiles = (p.n_out + kOuts * C::MT - 1) / (kOuts * C::MT), chunks = (p.groups + C::CH - 1) / C::CH;
     p.waves_k = 1;
     while (p.waves_k < kWaves && 2 * p.waves_k <= chunks) p.waves_k *= 2;
     const int64_t each = kWaves / p.waves_k;
-    packed_linear_kernel<C><<<dim3((uint32_t)((tiles + each - 1) / each), (uint32_t)((p.rows + C::R - 1) / C::R)), kBlock, C::kLds, s>>>(p);
+    return dim3((uint32_t)((tiles + each - 1) / each), (uint32_t)((p.rows + C::R - 1) / C::R));
 }
 
+// The first of these cuts, the smallest, of which the compute units take all workgroups at once; otherwise the last.  A
+// larger tile reads x and waits for the join less often, a second turn costs as much as the first (us, each cut by itself):
+//   4096 x 4096 by 16 rows in tiles of 16 / 32 rows of w   6.0 / 7.8      12288 x 12288: 16 / 32 / 48 / 64   42 / 40 / 29 / 35
+//   8192 x 2048 by 64 rows in tiles of 16 x 32 / 32 x 32 / 64 x 32 (rows of x times rows of w)   11.8 / 16.1 / 23.4
+//   8192 x 8192 by 64 rows, the same                                                             44.9 / 35.2 / 28.6
+// Up to four rows in bfloat16 are the exception: their workgroups are small enough that several share a compute unit, and
+// tiles of 16 were the fastest throughout (12288 x 12288 by one row 24.4, of 48 26.2; 28672 x 4096 22.6 and 28.8).
+template <class C, class... More> void launch(Params &p, hipStream_t s) {
+    const dim3 blocks = blocks_of<C>(p);
+    if constexpr (sizeof...(More) > 0)
+        if ((int64_t)blocks.x * blocks.y > kComputeUnits) return launch<More...>(p, s);
+    packed_linear_kernel<C><<<blocks, kBlock, C::kLds, s>>>(p);
+}
+
+// Rows of x that are no whole aligned pieces of 16 bytes pass through registers and wait for themselves (12288 x 12288 by 16
+// rows: 49 us).  Up to 4 rows take 1/4 of the LDS that 16 do (4096 x 4096 by one row 5.7 us, as 16 rows 5.9; 12288 x 12288 24 and
+// 33).  Binary32 has three products for one and twice x's bytes: 64 rows do not fit.
 template <class T> void choose(Params &p, hipStream_t s) {
     constexpr int kPiece = 16 / sizeof(T);
-    const bool exact = (uintptr_t)p.x % 16 == 0 && p.n_in % kPiece == 0 && (p.rows <= 1 || (p.x_stride % kPiece == 0 && p.x_stride >= 0 && p.x_stride <= kMostStride / 4));
-    const int per = (p.n_out + kOuts * kComputeUnits - 1) / (kOuts * kComputeUnits);       // tiles of a workgroup a compute unit
+    const bool exact = (uintptr_t)p.x % 16 == 0 && p.n_in % kPiece == 0 && p.x_stride % kPiece == 0 && p.x_stride >= 0 && p.x_stride <= kMostStride / 4;
     if (!exact) {
-        if (p.rows <= 4 && per < 2) launch<Cut<T, 4, 4, 1, 4, false>>(p, s);
-        else if (p.rows <= 4) launch<Cut<T, 4, 4, 2, 4, false>>(p, s);
-        else if (p.rows <= 16 && per < 2) launch<Cut<T, 16, 2, 1, 3, false>>(p, s);
-        else if (p.rows <= 16) launch<Cut<T, 16, 2, 2, 3, false>>(p, s);
+        if (p.rows <= 4) launch<Cut<T, 4, 4, 1, 4, false>, Cut<T, 4, 4, 2, 4, false>>(p, s);
+        else if (p.rows <= 16) launch<Cut<T, 16, 2, 1, 3, false>, Cut<T, 16, 2, 2, 3, false>>(p, s);
         else launch<Cut<T, 32, 2, 2, 2, false>>(p, s);
-        return;
-    }
-    if (p.rows <= 4) {
-        if (per >= 4) launch<Cut<T, 4, 4, 4, sizeof(T) == 2 ? 3 : 2, true>>(p, s);
-        else if (per == 3) launch<Cut<T, 4, 4, 3, 3, true>>(p, s);
-        else if (per == 2) launch<Cut<T, 4, 4, 2, 4, true>>(p, s);
-        else launch<Cut<T, 4, 4, 1, 4, true>>(p, s);
     } else if constexpr (sizeof(T) == 2) {
-        if (p.rows <= 16) {
-            if (per >= 4) launch<Cut<T, 16, 4, 4, 2, true>>(p, s);
-            else if (per == 3) launch<Cut<T, 16, 4, 3, 2, true>>(p, s);
-            else if (per == 2) launch<Cut<T, 16, 4, 2, 3, true>>(p, s);
-            else launch<Cut<T, 16, 4, 1, 3, true>>(p, s);
-        } else if (p.rows <= 32) {
-            if (per >= 2) launch<Cut<T, 32, 2, 2, 3, true>>(p, s);
-            else launch<Cut<T, 32, 2, 1, 3, true>>(p, s);
-        } else {
-            if (per >= 2) launch<Cut<T, 64, 2, 2, 2, true>>(p, s);
-            else launch<Cut<T, 64, 2, 1, 2, true>>(p, s);
-        }
+        if (p.rows <= 4) launch<Cut<T, 4, 4, 1, 4, true>>(p, s);
+        else if (p.rows <= 16) launch<Cut<T, 16, 2, 1, 3, true>, Cut<T, 16, 4, 2, 3, true>, Cut<T, 16, 4, 3, 2, true>, Cut<T, 16, 4, 4, 2, true>>(p, s);
+        else if (p.rows <= 32) launch<Cut<T, 16, 4, 2, 3, true>, Cut<T, 32, 2, 2, 3, true>, Cut<T, 32, 2, 4, 2, true>>(p, s);
+        else launch<Cut<T, 16, 4, 2, 3, true>, Cut<T, 32, 2, 2, 3, true>, Cut<T, 64, 2, 2, 2, true>>(p, s);
     } else {
-        if (p.rows <= 16) {
-            if (per >= 2) launch<Cut<T, 16, 2, 2, 3, true>>(p, s);
-            else launch<Cut<T, 16, 2, 1, 3, true>>(p, s);
-        } else {
-            if (per >= 2) launch<Cut<T, 32, 2, 2, 2, true>>(p, s);
-            else launch<Cut<T, 32, 2, 1, 2, true>>(p, s);
-        }
+        if (p.rows <= 4) launch<Cut<T, 4, 4, 1, 4, true>, Cut<T, 4, 4, 2, 4, true>, Cut<T, 4, 4, 3, 3, true>, Cut<T, 4, 4, 4, 2, true>>(p, s);
+        else if (p.rows <= 16) launch<Cut<T, 16, 2, 1, 3, true>, Cut<T, 16, 2, 2, 3, true>, Cut<T, 16, 2, 3, 3, true>, Cut<T, 16, 2, 4, 2, true>>(p, s);
+        else launch<Cut<T, 16, 2, 2, 3, true>, Cut<T, 32, 2, 2, 2, true>>(p, s);
     }
 }
 
@@ -304,7 +297,7 @@ int hp_packed_linear(const hp_packed_linear_args_t *a, void *stream) {
     if (a->rows == 0 || a->n_out == 0) return HP_OK;
     Params p{};
     p.rows = a->rows, p.n_in = a->n_in, p.n_out = a->n_out, p.groups = groups_of(a->n_in);
-    p.x = a->x, p.x_stride = a->x_stride, p.w = a->w, p.out = a->out, p.out_stride = a->out_stride;
+    p.x = a->x, p.x_stride = a->rows > 1 ? a->x_stride : 0, p.w = without_unused(a->w, a->n_out), p.out = a->out, p.out_stride = a->out_stride;
     const hipStream_t s = (hipStream_t)stream;
     if (a->dtype == HP_BF16) choose<__bf16>(p, s);
     else choose<float>(p, s);

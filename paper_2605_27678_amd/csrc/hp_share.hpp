@@ -7,8 +7,6 @@
 
 namespace hp {
 
-constexpr int kMostUnits = 1 << 16;
-
 // The first tile of unit u (of u = units: the end).
 constexpr int first_of(int total, int u, int units) { return (int)((double)total * u / units); }
 // The unit that tile t, below total, belongs to.

@@ -2,7 +2,7 @@
 whose rules for tensors, streams and errors hold here too.
 
     cache_k, cache_v = (hp.Packed.room(rows, heads_k, dim, device) for _ in range(2))
-    hp.hp_pack([k, v], [cache_k[a:b], cache_v[a:b]])                   # as a request's states are made
+    hp.hp_pack([k, v], [cache_k.rows(a, b), cache_v.rows(a, b)])       # as a request's states are made
     hp.hp_packed_attend_step(q, cache_k, cache_v, ranges, out, workspace=scratch)
     hp.hp_packed_linear(x, w, y)                                       # y = x w^T
 """
