@@ -13,6 +13,13 @@
 // binary32).  What the codes' lift puts into a product, and 8 more so that codes lie around zero and cancel little, is taken
 // off by a product with -24 throughout, from the very same rounded weights (in binary32 they lie there as they are);
 // 8 * sum p step + sum p low come from one more product, whose left rows are the groups' steps and lows.
+//
+// A state and head are 5 bits a channel of k and of v, each read once, so memory bounds it: 288 MB of 64 requests are 56 us at
+// the rate of a large copy.  It takes 74, and 6 more for the join; the same loads without the computing take 66, behind
+// which the computing hides where three waves share a SIMD.  Heads of 256 leave it one or two: 43 us for 110 MB (loads alone 37, a
+// copy 21).  Binary32, with three products for one, takes 50 us for 53 MB in heads of 72 (30, 10).
+// Sets of heads side by side in a product's columns (few heads share a state head) took a quarter less arithmetic and no
+// less time; rings of three tiles instead of two leave room for fewer waves (64 requests 113 us).
 #include <climits>
 #include <cmath>
 #include <type_traits>
@@ -33,7 +40,7 @@ constexpr float kMiddle = 8.0f;
 struct Params {
     int64_t rows, keys;
     int32_t heads_q, group, groups, dim, head_tiles;
-    int32_t units, least;                          // of each tile of heads (0: each row is one), and the tiles that a unit has at least
+    int32_t units;                                 // of each tile of heads; 0: each row is one
     float scale2;                                  // for exponents of two
     hp_heads_t q, out;
     hp_packed_t k, v;
@@ -137,7 +144,7 @@ struct Share {
         return Range{__builtin_amdgcn_readlane(held.lo, (int)row), __builtin_amdgcn_readlane(held.hi, (int)row)};
     }
 };
-__device__ __forceinline__ Share share_of(const Params &p, int unit, int lane) {
+__device__ __forceinline__ Share share_of(const Params &p, int unit, int lane, int waves) {
     Share s{unit, 0, 0, 0, 0, 0, Range{}, false};
     if (!p.units) {
         s.left = range_of(p, unit).tiles();
@@ -160,7 +167,7 @@ __device__ __forceinline__ Share share_of(const Params &p, int unit, int lane) {
         if (lane >= d) upto += before;
     }
     s.total = __builtin_amdgcn_readlane(upto, kWave - 1);
-    s.units = min(p.units, (s.total + p.least - 1) / p.least);
+    s.units = min(p.units, (s.total + waves - 1) / waves);         // none with less than a tile for each wave
     s.at = unit < s.units ? first_of(s.total, unit, s.units) : 0;
     s.left = unit < s.units ? first_of(s.total, unit + 1, s.units) - s.at : 0;
     // the lane whose rows have that tile, then the row
@@ -194,7 +201,7 @@ constexpr float kLag = 8.0f;                       // the maximum is raised when
 // or four of 40 do not share: 1024 of these took two turns, 64 requests 88 us instead of 77).
 template <int GP> constexpr int kWaves = GP == 8 ? 7 : 4;
 template <class T, int GP> constexpr int kResident = sizeof(T) == 2 ? (GP <= 3 ? 4 : GP == 4 ? 3 : 1) : (GP <= 2 ? 3 : GP <= 4 ? 2 : 1);
-// Few rows: a workgroup a compute unit, with more waves, so that short ranges are not cut.
+// Few tiles: one workgroup for each tile of heads, with more waves.
 template <int GP> constexpr int kFewWaves = GP == 8 ? 7 : 8;
 template <class T, int GP, int WAVES> constexpr int kWavesASimd = WAVES == kWaves<GP> ? (WAVES * kResident<T, GP> + 3) / 4 : (WAVES + 3) / 4;
 
@@ -218,7 +225,7 @@ template <class T, int GP, int WAVES> __global__ __launch_bounds__((WAVES * kWav
     const Frag centre = all_of(-kLift - kMiddle);
     const Codes<T> codes;
 
-    Share share = share_of(p, unit, lane);
+    Share share = share_of(p, unit, lane, kWaves);
     for (; share.left > 0; ++share.row, share.skip = 0) {
         const int64_t row = share.row;
         const Range see = share.now(p);
@@ -508,26 +515,26 @@ int head_tiles_of(const hp_packed_attend_args_t &a) { return (a.heads_q / a.head
 
 template <class T> int resident_of(int groups) { return groups <= 2 ? kResident<T, 2> : groups <= 3 ? kResident<T, 3> : groups <= 4 ? kResident<T, 4> : kResident<T, 8>; }
 
-// Units of each tile of heads, how many tiles each has at least, and whether its workgroup has more waves.
+// Units of each tile of heads, and whether they are workgroups of more waves.
+//
+// Up to two tiles a wave of such a workgroup are left in one, which needs no join: one request of 576 states 10 us, with units
+// of one tile a wave and the launch that joins them 13; 2000 states so, in two units, took 17 us and took 12.6 with smaller
+// ones.  Others get as many units as run at once.  Sharing out evenly costs rows of like lengths the cuts and the join (256
+// requests of 500 states 60 us, with a workgroup each 51; of 50 to 2000 states 105 and 96), but nobody knows here how long the
+// longest is, and of 20000 states one workgroup would have 80 tiles a wave.  More than kMostShared rows, whose lengths no wave
+// adds up by itself, are a workgroup each (513 requests of 50 to 2000 states 180 us, 512 shared out 176).
 struct Cut {
-    int32_t units, least;
+    int32_t units;
     bool few;
 };
 Cut cut_of(const hp_packed_attend_args_t &a) {
     const int64_t columns = (int64_t)a.heads_k * head_tiles_of(a), tiles = a.keys / kTile + 1;
-    // 0: the rows are enough by themselves, or too many to be added up
-    if (a.rows > kMostShared || a.rows * tiles > INT_MAX) return Cut{0, 1, false};
-    const int groups = groups_of(a.dim), waves = groups <= 2 ? kWaves<2> : groups <= 3 ? kWaves<3> : groups <= 4 ? kWaves<4> : kWaves<8>;
-    const int few = groups <= 4 ? kFewWaves<4> : kFewWaves<8>;
-    // two tiles a wave of larger workgroups, if these are no more than compute units: joining parts is a launch more
-    const int64_t units = (a.rows * tiles + 2 * few - 1) / (2 * few);
-    if (units * columns <= kComputeUnits) return Cut{(int32_t)units, 2 * few, true};
+    if (a.rows > kMostShared || a.rows * tiles > INT_MAX) return Cut{0, false};
+    const int groups = groups_of(a.dim), waves = groups <= 4 ? kWaves<4> : kWaves<8>;
+    if (a.rows * tiles <= 2 * (groups <= 4 ? kFewWaves<4> : kFewWaves<8>)) return Cut{1, true};
     const int64_t slots = kComputeUnits * (a.dtype == HP_BF16 ? resident_of<__bf16>(groups) : resident_of<float>(groups));
-    // as many as run at once, or, of few rows each, four times as many workgroups
-    int64_t n = slots / columns;
-    if (n < 4) n = (4 * slots + columns - 1) / columns;
-    const int64_t most = (a.rows * tiles + waves - 1) / waves;
-    return Cut{(int32_t)(n < most ? n : most), waves, false};
+    const int64_t fit = slots / columns, most = (a.rows * tiles + waves - 1) / waves, units = fit < most ? fit : most;
+    return Cut{(int32_t)(units > 1 ? units : 1), false};
 }
 
 int check_sizes(const hp_packed_attend_args_t *a) {
@@ -601,7 +608,7 @@ int hp_packed_attend_step(const hp_packed_attend_args_t *a, void *stream) {
     p.rows = a->rows, p.keys = a->keys;
     p.heads_q = a->heads_q, p.group = a->heads_q / a->heads_k, p.groups = groups_of(a->dim), p.dim = a->dim;
     const Cut cut = cut_of(*a);
-    p.units = cut.units, p.least = cut.least, p.head_tiles = head_tiles_of(*a), p.part_heads = part_heads_of(*a);
+    p.units = cut.units, p.head_tiles = head_tiles_of(*a), p.part_heads = part_heads_of(*a);
     p.scale2 = a->scale * kLog2e;
     p.q = a->q, p.out = a->out, p.k = without_unused(a->k, a->keys), p.v = without_unused(a->v, a->keys), p.ranges = a->ranges, p.lse = a->lse;
     const int64_t parts = (int64_t)2 * p.units * a->heads_k * p.head_tiles * p.part_heads;

@@ -2,12 +2,17 @@
 //     = sum_g (step_ng sum_k x_rk code_nk + low_ng sum_k x_rk)            (k in group g)
 // The rows of x are the left operand of products of 16 x 16 x 32, a group of 16 rows of w at a time the right one, so that a
 // lane has results of one row of w, whose step and low are its own.  The sums of x over a group are products with ones; for
-// four groups at a time they are, split into numbers of 8 bits over the quarters, the left operand of one more product, whose
-// right one is the pairs (step, low) as they lie in memory: it puts sum x low in and takes off what the codes are lifted by.
+// four groups at a time they are, split into numbers of 8 bits over the quarters (two of bfloat16's, which leave 2^-18 of a
+// group's sum out; three of binary32's), the left operand of one more product, whose right one is the pairs (step, low) as
+// they lie in memory: it puts sum x low in and takes off what the codes are lifted by.
 // The waves of a workgroup share out the inner axis, 128 of it at a time, and add up at the end in their order.  Each brings its
 // own pieces of x and w to LDS, ahead of their use and without barriers: the operands' rows lie in neighbouring lanes, and
 // loads straight into registers took the caches 64 cycles each, one a lane, where runs of 64 and 256 bytes take 16
-// (12288 x 12288 by 16 rows: 36 us, this way 30).
+// (12288 x 12288 by 16 rows: 36 us, this way 29).
+//
+// The weights are 5 bits a value, read once by up to 64 rows: 95 MB of these 12288 x 12288 are 18 us at the rate of a large
+// copy, and the loads alone take 27.  With more rows the caches are busier with x: of 8192 x 8192 by 64
+// rows every compute unit reads all of x, 1 MB, for its 32 rows of w, 256 MB next to 44; that takes 29 us, the loads alone 24.
 #include "hp_packed.hpp"
 
 #pragma clang fp contract(fast)
