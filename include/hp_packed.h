@@ -26,8 +26,9 @@
  * that is below 2^-126), and for each value the code of the nearest level, of the lower
  * of two: no value is farther than step / 2 from its own.  A group with a value that is
  * not finite (or below -3.3895e38, which no bfloat16 is) has NaN for its step and low, and
- * all of it reads back as NaN.  Codes of channels that a shorter group lacks are zero
- * and are not read for their value.
+ * all of it reads back as NaN.  (Where the greatest value is within step of the largest
+ * binary32 number, 3.4028e38, its level may be beyond and read back as infinite.)  Codes
+ * of channels that a shorter group lacks are zero and are not read for their value.
  */
 #ifndef HP_PACKED_H_
 #define HP_PACKED_H_
@@ -103,8 +104,11 @@ int64_t hp_packed_attend_workspace(const hp_packed_attend_args_t *args);
 
 /* hp_packed_linear - out[r][n] = sum_k x[r][k] w[n][k] for x [rows, n_in], packed w
  * [n_out, n_in] (one head: head strides are not read) and out [rows, n_out].  Sums are in
- * binary32, the weights' values are not rounded; a row of x that is not finite gives NaN.
- * Made for the rows of a decoding step: every 64 rows (32 in HP_F32) read the weights once.
+ * binary32, the weights' values are not rounded (in HP_BF16 the part of the lows may be off
+ * by 2^-18 of 16 step + |low| times a group's sum of x); a row of x that is not finite gives NaN.
+ * Made for the rows of a decoding step: up to 64 rows (32 in HP_F32) at a time share a
+ * pass over the weights.  Fastest where x is 16-byte aligned and its rows and their stride
+ * are multiples of 16 bytes (other x: passes of 32 rows).
  * n_in up to HP_PACKED_MAX_DIM, n_out up to 2^24, rows up to 2^20, row strides of w up
  * to 2^24 and not negative (HP_ELAYOUT). */
 typedef struct hp_packed_linear_args {
