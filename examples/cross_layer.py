@@ -3,7 +3,8 @@
 A language model's sequence sees the images that came before each position; the images' states are the rows of the
 encoder's buffers, packed in image order.  The layer is the library's operators with plain matrix products between
 them: rotary positions in queries (their place in the sequence) and keys (their place in the image's grid), attention
-over the ranges that the token map gives, and the norms, the gate and the residual stream in one pass.
+over the ranges that the token map gives, and the norms, the gate and the residual stream in one pass.  Decoding can hold
+the states of its requests, and the projections of a step, in 4 bits.
 
     python examples/cross_layer.py
 """
@@ -59,6 +60,29 @@ class CrossLayer(torch.nn.Module):
         hp.hp_cross_attend_step(q, k, v, ranges, out, workspace=scratch, stream=torch.cuda.current_stream())
         return self.behind(x, out)
 
+    @torch.no_grad()
+    def pack(self, k, v):
+        """(k, v) and the weights of a step's projections, in 4 bits."""
+        def packed(*tensors):
+            rooms = [hp.Packed.room(len(t), t.shape[1] if t.dim() == 3 else None, t.shape[-1], t.device) for t in tensors]
+            hp.hp_pack(tensors, rooms, stream=torch.cuda.current_stream())
+            return rooms
+        return packed(k, v), [packed(w.t().contiguous())[0] for w in (self.wq, self.wo)]
+
+    @torch.no_grad()
+    def step_packed(self, x, positions, k, v, ranges, weights):
+        """step() from what pack() made."""
+        stream = torch.cuda.current_stream()
+        _, z = hp.gated_norm(x, None, w_pre=self.w_in)
+        q = torch.empty(len(x), self.heads_q * self.dim, dtype=x.dtype, device=x.device)
+        hp.hp_packed_linear(z, weights[0], q, stream=stream)
+        q = hp.rotary([q.view(-1, self.heads_q, self.dim)], self.table, positions)[0]
+        out, y = torch.empty_like(q), torch.empty_like(x)
+        scratch = torch.empty(max(hp.hp_packed_attend_workspace(q, k), 16), dtype=torch.uint8, device=q.device)
+        hp.hp_packed_attend_step(q, k, v, ranges, out, workspace=scratch, stream=stream)
+        hp.hp_packed_linear(out.flatten(1), weights[1], y, stream=stream)
+        return hp.gated_norm(x, y, self.w_post, self.gate, self.w_pre, gate_tanh=True)
+
 
 def main(batch=2, seq=512, side=24, hidden=1024, enc_hidden=768, heads_q=16, heads_k=4, dim=64, steps=8,
          dtype=torch.bfloat16, say=print):
@@ -94,8 +118,11 @@ def main(batch=2, seq=512, side=24, hidden=1024, enc_hidden=768, heads_q=16, hea
         last = torch.arange(batch, device=dev) * seq + seq - 1
         _, whole = layer(x, positions, k, v, ranges)
         _, token = layer.step(x[last], positions[last], k, v, ranges[last].contiguous())
+        cache, weights = layer.pack(k, v)
+        _, four = layer.step_packed(x[last], positions[last], *cache, ranges[last].contiguous(), weights)
     apart = float((token.float() - whole[last].float()).abs().max())
     say(f"last tokens decoded by themselves: at most {apart:.4f} from the whole pass")
+    say(f"the same with states and projections in 4 bits: {float((four - token).float().norm() / token.float().norm()):.4f} of their size apart")
     return losses, apart
 
 
