@@ -131,23 +131,25 @@ __device__ __forceinline__ Range range_of(const Params &p, int64_t row) {
 }
 
 // All rows' tiles lie one behind the other, and the units take equal shares, whatever the rows' lengths: each wave adds up
-// the lengths for itself, a few rows a lane.  The tiles of a unit: `left` of them, the first of which is the skip-th of `row`
-// and the at-th of all.
+// the lengths for itself, a few rows a lane.  A row begins with a tile more for each wave, for what it takes to begin and end
+// one (30 requests of 1 to 2305 states in heads of 72: 35 us without, 31.7 so, 34 with two).  The tiles of a unit: `left` of
+// them, the first of which is the skip-th of `row` and the at-th of all.
 constexpr int kRowsALane = 8, kMostShared = kRowsALane * kWave;
-struct Share {
+template <int WAVES> struct Share {
     int64_t row;
     int skip, left, at, total, units;
     Range held;                                    // of row `lane`, where there are no more rows than lanes
     bool few;
+    static __device__ __forceinline__ int cost(const Range &r) { return WAVES + r.tiles(); }
     __device__ __forceinline__ Range now(const Params &p) const {
         if (!few) return range_of(p, row);
         return Range{__builtin_amdgcn_readlane(held.lo, (int)row), __builtin_amdgcn_readlane(held.hi, (int)row)};
     }
 };
-__device__ __forceinline__ Share share_of(const Params &p, int unit, int lane, int waves) {
-    Share s{unit, 0, 0, 0, 0, 0, Range{}, false};
+template <int WAVES> __device__ __forceinline__ Share<WAVES> share_of(const Params &p, int unit, int lane) {
+    Share<WAVES> s{unit, 0, 0, 0, 0, 0, Range{}, false};
     if (!p.units) {
-        s.left = range_of(p, unit).tiles();
+        s.left = s.cost(range_of(p, unit));
         return s;
     }
     const int rows = (int)p.rows, each = (rows + kWave - 1) / kWave, mine = lane * each;
@@ -155,10 +157,10 @@ __device__ __forceinline__ Share share_of(const Params &p, int unit, int lane, i
     int own = 0;
     if (s.few) {
         s.held = range_of(p, min(lane, rows - 1));
-        own = lane < rows ? s.held.tiles() : 0;
+        own = lane < rows ? s.cost(s.held) : 0;
     } else {
         for (int i = 0; i < each; ++i)
-            if (mine + i < rows) own += range_of(p, mine + i).tiles();
+            if (mine + i < rows) own += s.cost(range_of(p, mine + i));
     }
     int upto = own;
 #pragma unroll
@@ -167,7 +169,7 @@ __device__ __forceinline__ Share share_of(const Params &p, int unit, int lane, i
         if (lane >= d) upto += before;
     }
     s.total = __builtin_amdgcn_readlane(upto, kWave - 1);
-    s.units = min(p.units, (s.total + waves - 1) / waves);         // none with less than a tile for each wave
+    s.units = min(p.units, (s.total + WAVES - 1) / WAVES);         // none with less than a tile for each wave
     s.at = unit < s.units ? first_of(s.total, unit, s.units) : 0;
     s.left = unit < s.units ? first_of(s.total, unit + 1, s.units) - s.at : 0;
     // the lane whose rows have that tile, then the row
@@ -175,7 +177,7 @@ __device__ __forceinline__ Share share_of(const Params &p, int unit, int lane, i
     int before = __builtin_amdgcn_readlane(upto - own, at_lane), row = at_lane * each;
     if (!s.few)
         for (;; ++row) {
-            const int n = range_of(p, row).tiles();
+            const int n = s.cost(range_of(p, row));
             if (before + n > s.at) break;
             before += n;
         }
@@ -195,25 +197,51 @@ template <int N, class F> __device__ __forceinline__ void each(const F &f) {
     }
 }
 
+constexpr int kSideHeads = 4;                      // of a state head, at most, for the three terms of each to stand side by side
 constexpr float kLag = 8.0f;                       // the maximum is raised when a score passes it by 2^8
 
 // Waves of a workgroup, and workgroups of a compute unit: as registers and LDS let run (of 160 KiB, which two workgroups of 80
 // or four of 40 do not share: 1024 of these took two turns, 64 requests 88 us instead of 77).
 template <int GP> constexpr int kWaves = GP == 8 ? 7 : 4;
-template <class T, int GP> constexpr int kResident = sizeof(T) == 2 ? (GP <= 3 ? 4 : GP == 4 ? 3 : 1) : (GP <= 2 ? 3 : GP <= 4 ? 2 : 1);
+template <class T, int GP, bool SIDE = false> constexpr int kResident = SIDE && GP <= 3 ? 3 : sizeof(T) == 2 || SIDE ? (GP <= 3 ? 4 : GP == 4 ? 3 : 1) : (GP <= 2 ? 3 : GP <= 4 ? 2 : 1);
 // Few tiles: one workgroup for each tile of heads, with more waves.
-template <int GP> constexpr int kFewWaves = GP == 8 ? 7 : 8;
-template <class T, int GP, int WAVES> constexpr int kWavesASimd = WAVES == kWaves<GP> ? (WAVES * kResident<T, GP> + 3) / 4 : (WAVES + 3) / 4;
+constexpr int kMostWaves = 8;
+template <int GP> constexpr int kFewWaves = GP == 8 ? 7 : kMostWaves;
+template <class T, int GP, int WAVES, bool SIDE> constexpr int kWavesASimd = WAVES == kWaves<GP> ? (WAVES * kResident<T, GP, SIDE> + 3) / 4 : (WAVES + 3) / 4;
 
-template <class T, int GP, int WAVES> __global__ __launch_bounds__((WAVES * kWave), (kWavesASimd<T, GP, WAVES>)) void packed_attend_kernel(Params p) {
+// Where a state head has four heads at most, the three bfloat16 terms of their binary32 queries and weights stand side by side,
+// term t in the columns 4t and on of one product, in the place of three products one behind the other; their sums meet once
+// for the scores and once at the end.  64 requests of 576 to 6404 states, 32 heads of 128 on 8: 126 us without, 120 so; heads of
+// 256, whose registers hold no three operands of each kind, 44 and 32.
+struct Side {
+    float first, second;                           // whether this lane's term is behind the first, the second
+    __device__ __forceinline__ explicit Side(int term) : first(term >= 1 ? 1.0f : 0.0f), second(term >= 2 ? 1.0f : 0.0f) {}
+    __device__ __forceinline__ __bf16 operator()(float x) const {
+        x = __builtin_fmaf(-first, (float)(__bf16)x, x);
+        return (__bf16)__builtin_fmaf(-second, (float)(__bf16)x, x);
+    }
+};
+// Over the four lanes of a row of 16 that have the same head's terms, in all of them alike.
+template <int BY> __device__ __forceinline__ float turned(float x) {
+    return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), 0x120 + BY, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float side_sum(float x) {
+    x += turned<8>(x);
+    return x + turned<4>(x);
+}
+
+template <class T, int GP, int WAVES, bool SIDE> __global__ __launch_bounds__((WAVES * kWave), (kWavesASimd<T, GP, WAVES, SIDE>)) void packed_attend_kernel(Params p) {
     typedef Layout<GP> L;
     constexpr float kLift = Codes<T>::kLift;
     constexpr bool kCentred = kLift == -kMiddle;
-    constexpr int N = kTerms<T>, kSets = (GP + 3) / 4, kWaves = WAVES;
+    constexpr int N = SIDE ? 1 : kTerms<T>, kSets = (GP + 3) / 4, kWaves = WAVES;
     __shared__ __attribute__((aligned(16))) char lds[kWaves * L::kBytes];
     static_assert(sizeof(lds) >= 16 * kWaves * 2 * GP * kWave + 8 * kWaves * kHeads, "room for the join");
     const int tid = (int)threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), col = lane % 16, quarter = lane / 16;
     const int unit = (int)blockIdx.x, state_head = (int)blockIdx.y / p.head_tiles, first_head = ((int)blockIdx.y % p.head_tiles) * kHeads;
+    const int col_head = SIDE ? col % kSideHeads : col, term = SIDE ? col / kSideHeads : 0;
+    const Side side(term);
+    const bool spare = SIDE && term == kTerms<T>;  // columns without a term: zeros
     const int heads = min(p.group - first_head, kHeads), head0 = state_head * p.group + first_head;
     char *const k_tile = lds + wave * L::kBytes, *const v_tile = k_tile + L::kTensor;
     const uint32_t *const k_scales = (const uint32_t *)(k_tile + L::kCodes), *const v_scales = (const uint32_t *)(v_tile + L::kCodes);
@@ -222,27 +250,30 @@ template <class T, int GP, int WAVES> __global__ __launch_bounds__((WAVES * kWav
     vs.plan(p.v, p.groups, lane);
     // of a quarter's states 16 a + 4 quarter + i, a and i < 4, lane 4 a + i has the steps and brings the transposed codes
     const int own = 16 * (col / 4) + 4 * quarter + col % 4;
+    const auto split = [&](float x, Frag (&f)[N], int i) {
+        if constexpr (SIDE) f[0][i] = side(x);
+        else terms(x, f, i);
+    };
     const Frag centre = all_of(-kLift - kMiddle);
     const Codes<T> codes;
 
-    Share share = share_of(p, unit, lane, kWaves);
+    Share share = share_of<kWaves>(p, unit, lane);
     for (; share.left > 0; ++share.row, share.skip = 0) {
         const int64_t row = share.row;
         const Range see = share.now(p);
         const int lo = see.lo, hi = see.hi, n_tiles = see.tiles();
-        const int begin = share.skip, end = min(n_tiles, begin + share.left);
-        share.left -= end - begin;
+        const int first = share.at - share.skip, cost = share.cost(see), taken = min(cost - share.skip, share.left);    // first: the row's place among all
+        const int begin = max(share.skip - kWaves, 0), end = share.skip + taken - kWaves;
+        share.left -= taken, share.at += taken;
+        if (end <= begin) break;                   // the next unit has the row's first tile
         const bool whole = begin == 0 && end == n_tiles;
-        if (p.units && begin == 0 && blockIdx.y == 0 && tid == 0) {
-            const int first = share.at;                // its place among all tiles
-            p.row_units[row] = make_int2(unit, whole ? unit : unit_of(share.total, first + n_tiles - 1, share.units));
-        }
-        share.at += end - begin;
+        if (p.units && begin == 0 && blockIdx.y == 0 && tid == 0)
+            p.row_units[row] = make_int2(unit, whole ? unit : unit_of(share.total, first + cost - 1, share.units));
 
         // the queries, and the right operand that puts the lows in: for each pair (step, low) of four groups the values
         // (-lift sum q, sum q), split into three numbers over the quarters
         Frag q[GP][N], sums[kSets] = {};
-        const T *q_row = (const T *)p.q.data + row * p.q.row_stride + (int64_t)(head0 + min(col, heads - 1)) * p.q.head_stride;
+        const T *q_row = (const T *)p.q.data + row * p.q.row_stride + (int64_t)(head0 + min(col_head, heads - 1)) * p.q.head_stride;
         Vec<T, 8> x[GP];
         int dim = p.dim;
         asm volatile("" : "+s"(dim));                  // or the places of all channels would be kept over the rows
@@ -275,15 +306,18 @@ template <class T, int GP, int WAVES> __global__ __launch_bounds__((WAVES * kWav
         __builtin_amdgcn_sched_barrier(0);
     #pragma unroll
         for (int g = 0; g < GP; ++g) {
-            terms<T>(x[g], q[g]);
+            if constexpr (SIDE)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) q[g][0][i] = side(spare ? 0.0f : (float)x[g][i]);
+            else terms<T>(x[g], q[g]);
             float sum = 0.0f;
     #pragma unroll
             for (int i = 0; i < 8; ++i) sum += (float)x[g][i];
             sum = column_sum(sum);
             const __bf16 a = (__bf16)sum, b = (__bf16)(sum - (float)a), c = (__bf16)(sum - (float)a - (float)b);
-            const float part = quarter == 0 ? (float)a : quarter == 1 ? (float)b : quarter == 2 ? (float)c : 0.0f;
-            sums[g / 4][2 * (g % 4)] = (__bf16)(-kLift * part);
-            sums[g / 4][2 * (g % 4) + 1] = (__bf16)part;
+            const float part = quarter == 0 ? (float)a : quarter == 1 ? (float)b : quarter == 2 ? (float)c : 0.0f, of_this = term == 0 ? part : 0.0f;
+            sums[g / 4][2 * (g % 4)] = (__bf16)(-kLift * of_this);
+            sums[g / 4][2 * (g % 4) + 1] = (__bf16)of_this;
         }
 
         float top = -INFINITY, sum = 0.0f;
@@ -316,6 +350,11 @@ template <class T, int GP, int WAVES> __global__ __launch_bounds__((WAVES * kWav
                     each<4>([&](auto i) { s[a][i.value] += of_lane<4 * a + i>(step_of(k_pairs[g.value])) * d[i.value]; });
                 });
             });
+            if constexpr (SIDE)
+#pragma unroll
+                for (int a = 0; a < 4; ++a)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) s[a][i] = side_sum(s[a][i]);
             // here, not behind the branch, where all these products' results would have to be kept until then
     #pragma unroll
             for (int a = 0; a < 4; ++a) asm("" : "+v"(s[a]));
@@ -349,6 +388,7 @@ template <class T, int GP, int WAVES> __global__ __launch_bounds__((WAVES * kWav
                 for (int i = 0; i < 4; ++i) {
                     s[a][i] = __builtin_amdgcn_exp2f(s[a][i] * p.scale2 - base);
                     sum += s[a][i];
+                    if constexpr (SIDE) s[a][i] = spare ? 0.0f : s[a][i];
                 }
 
             if (more) __builtin_amdgcn_s_waitcnt(but(Loader<GP>::kLoads));
@@ -367,8 +407,8 @@ template <class T, int GP, int WAVES> __global__ __launch_bounds__((WAVES * kWav
                     Frag weights[N];
     #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        terms(s[2 * b][i], weights, i);
-                        terms(s[2 * b + 1][i], weights, 4 + i);
+                        split(s[2 * b][i], weights, i);
+                        split(s[2 * b + 1][i], weights, 4 + i);
                     }
     #pragma unroll
                     for (int n = 0; n < N; ++n) rest = mma(pairs, weights[n], rest);
@@ -380,8 +420,8 @@ template <class T, int GP, int WAVES> __global__ __launch_bounds__((WAVES * kWav
                 each<8>([&](auto e) {
                     constexpr int b = e / 4, i = e % 4;
                     const float step = step_of(v_pairs[g.value]);
-                    terms(of_lane<8 * b + i>(step) * s[2 * b][i], weights[b], 2 * i);
-                    terms(of_lane<8 * b + 4 + i>(step) * s[2 * b + 1][i], weights[b], 2 * i + 1);
+                    split(of_lane<8 * b + i>(step) * s[2 * b][i], weights[b], 2 * i);
+                    split(of_lane<8 * b + 4 + i>(step) * s[2 * b + 1][i], weights[b], 2 * i + 1);
                 });
                 typedef int Pair __attribute__((ext_vector_type(2)));
                 typedef __attribute__((address_space(3))) Pair *Lds;
@@ -442,6 +482,9 @@ template <class T, int GP, int WAVES> __global__ __launch_bounds__((WAVES * kWav
             Quad v = {};
     #pragma unroll
             for (int w = 0; w < kWaves; ++w) v += join[(w * 2 * GP + t) * kWave + lane];
+            if constexpr (SIDE)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = side_sum(v[i]);
             if (col >= heads || d >= p.dim) continue;
             if (!whole) {
                 store<4>(p.products + (part * p.part_heads + col) * p.dim + d, v, p.dim - d);
@@ -513,7 +556,10 @@ int64_t align16(int64_t n) { return (n + 15) / 16 * 16; }
 
 int head_tiles_of(const hp_packed_attend_args_t &a) { return (a.heads_q / a.heads_k + kHeads - 1) / kHeads; }
 
-template <class T> int resident_of(int groups) { return groups <= 2 ? kResident<T, 2> : groups <= 3 ? kResident<T, 3> : groups <= 4 ? kResident<T, 4> : kResident<T, 8>; }
+template <class T, bool SIDE = false> int resident_of(int groups) {
+    return groups <= 2 ? kResident<T, 2, SIDE> : groups <= 3 ? kResident<T, 3, SIDE> : groups <= 4 ? kResident<T, 4, SIDE> : kResident<T, 8, SIDE>;
+}
+bool side_by_side(const hp_packed_attend_args_t &a) { return a.dtype == HP_F32 && a.heads_q / a.heads_k <= kSideHeads; }
 
 // Units of each tile of heads, and whether they are workgroups of more waves.
 //
@@ -529,10 +575,10 @@ struct Cut {
 };
 Cut cut_of(const hp_packed_attend_args_t &a) {
     const int64_t columns = (int64_t)a.heads_k * head_tiles_of(a), tiles = a.keys / kTile + 1;
-    if (a.rows > kMostShared || a.rows * tiles > INT_MAX) return Cut{0, false};
+    if (a.rows > kMostShared || a.rows * (tiles + kMostWaves) > INT_MAX) return Cut{0, false};
     const int groups = groups_of(a.dim), waves = groups <= 4 ? kWaves<4> : kWaves<8>;
     if (a.rows * tiles <= 2 * (groups <= 4 ? kFewWaves<4> : kFewWaves<8>)) return Cut{1, true};
-    const int64_t slots = kComputeUnits * (a.dtype == HP_BF16 ? resident_of<__bf16>(groups) : resident_of<float>(groups));
+    const int64_t slots = kComputeUnits * (a.dtype == HP_BF16 ? resident_of<__bf16>(groups) : side_by_side(a) ? resident_of<float, true>(groups) : resident_of<float>(groups));
     const int64_t fit = slots / columns, most = (a.rows * tiles + waves - 1) / waves, units = fit < most ? fit : most;
     return Cut{(int32_t)(units > 1 ? units : 1), false};
 }
@@ -573,15 +619,15 @@ int check(const hp_packed_attend_args_t *a) {
     return HP_OK;
 }
 
-template <class T, int GP> void launch(bool few, const Params &p, const dim3 &grid, hipStream_t s) {
-    if (few) packed_attend_kernel<T, GP, kFewWaves<GP>><<<grid, kFewWaves<GP> * kWave, 0, s>>>(p);
-    else packed_attend_kernel<T, GP, kWaves<GP>><<<grid, kWaves<GP> * kWave, 0, s>>>(p);
+template <class T, int GP, bool SIDE> void launch(bool few, const Params &p, const dim3 &grid, hipStream_t s) {
+    if (few) packed_attend_kernel<T, GP, kFewWaves<GP>, SIDE><<<grid, kFewWaves<GP> * kWave, 0, s>>>(p);
+    else packed_attend_kernel<T, GP, kWaves<GP>, SIDE><<<grid, kWaves<GP> * kWave, 0, s>>>(p);
 }
-template <class T> void launch(bool few, const Params &p, const dim3 &grid, hipStream_t s) {
-    if (p.groups <= 2) launch<T, 2>(few, p, grid, s);
-    else if (p.groups == 3) launch<T, 3>(few, p, grid, s);
-    else if (p.groups == 4) launch<T, 4>(few, p, grid, s);
-    else launch<T, 8>(few, p, grid, s);
+template <class T, bool SIDE> void launch(bool few, const Params &p, const dim3 &grid, hipStream_t s) {
+    if (p.groups <= 2) launch<T, 2, SIDE>(few, p, grid, s);
+    else if (p.groups == 3) launch<T, 3, SIDE>(few, p, grid, s);
+    else if (p.groups == 4) launch<T, 4, SIDE>(few, p, grid, s);
+    else launch<T, 8, SIDE>(few, p, grid, s);
 }
 
 template <class T> void join(const Params &p, hipStream_t s) {
@@ -617,8 +663,9 @@ int hp_packed_attend_step(const hp_packed_attend_args_t *a, void *stream) {
     p.lse2 = (float *)(ws + align16(4 * parts * p.dim));
     p.row_units = (int2 *)(ws + align16(4 * parts * p.dim) + align16(4 * parts));
     const dim3 grid((uint32_t)(p.units ? p.units : p.rows), (uint32_t)(a->heads_k * p.head_tiles));
-    if (a->dtype == HP_BF16) launch<__bf16>(cut.few, p, grid, s);
-    else launch<float>(cut.few, p, grid, s);
+    if (a->dtype == HP_BF16) launch<__bf16, false>(cut.few, p, grid, s);
+    else if (side_by_side(*a)) launch<float, true>(cut.few, p, grid, s);
+    else launch<float, false>(cut.few, p, grid, s);
     if (hip_failed(hipGetLastError())) return HP_EHIP;
     if (p.units <= 1) return HP_OK;                // no row has parts
     if (a->dtype == HP_BF16) join<__bf16>(p, s);
