@@ -111,6 +111,8 @@ template <class C> __global__ __launch_bounds__(kBlock) void packed_linear_kerne
     Quad acc[MT][NT] = {};
     const Frag ones = all_of(1.0f);
     const Codes<T> codes_of;
+    // whether this quarter's number of a sum is behind the first, the second
+    const float first = quarter >= 1 ? -1.0f : 0.0f, second = quarter >= 2 ? -1.0f : 0.0f;
     const auto add = [&](const char *from) {
         Words low[MT] = {};
         Frag sums[NT] = {};
@@ -132,8 +134,9 @@ template <class C> __global__ __launch_bounds__(kBlock) void packed_linear_kerne
                 Quad sum = {};                     // of this lane's row of x, in all four numbers
 #pragma unroll
                 for (int n = 0; n < N; ++n) sum = mma(ones, a[t][n], sum);
-                const float second = sum[0] - (float)(__bf16)sum[0];
-                const float part = quarter == 0 ? sum[0] : quarter == 1 ? second : N > 1 && quarter == 2 ? second - (float)(__bf16)second : 0.0f;
+                // the quarter's number of it; what stands in quarters without one meets zeros
+                float part = __builtin_fmaf(first, (float)(__bf16)sum[0], sum[0]);
+                if constexpr (N > 1) part = __builtin_fmaf(second, (float)(__bf16)part, part);
                 sums[t][2 * j] = (__bf16)(-kLift * part);
                 sums[t][2 * j + 1] = (__bf16)part;
             }
@@ -141,8 +144,9 @@ template <class C> __global__ __launch_bounds__(kBlock) void packed_linear_kerne
             for (int m = 0; m < MT; ++m) {
                 const int row = kOuts * m + col;
                 const Frag l = codes_of(*(const uint32_t *)(from + C::kCodes + (row * CH + C::code_slot(row, j)) * kGroupBytes + 4 * quarter));
-                low[m][j] = *(const uint32_t *)(from + C::kPairs + (row * CH + j) * 4);
-                const float step = step_of(low[m][j]);
+                const uint32_t pair = *(const uint32_t *)(from + C::kPairs + (row * CH + j) * 4);
+                const float step = step_of(pair);
+                low[m][j] = quarter <= (N > 1 ? 2 : 1) ? pair : 0;
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
                     Quad d = {};
