@@ -25,17 +25,17 @@ __device__ __forceinline__ Quad mma(const Frag &a, const Frag &b, const Quad &c)
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
-// A word's eight codes as an operand of products, kLift more than they are, in the order of their channels.
+// A word's eight codes as an operand of products, (code + kLift) * kUnit, in the order of their channels.
 //
 // For bfloat16 results a code's four bits go below the leading one of 16: 0x4180 | code << 3 is 16 + code, two at a time with
 // a shift and an and-or, one instruction a code.  (128 + code would save one shift in eight and cost the sums three more bits
 // to cancel.)  What the 16 adds is taken off again with sum x, which the matrix units make too.
 //
 // Binary32 results would feel that the lift cancels (1.8e-6 of their size off instead of 8e-7): there a code less 8 goes
-// through binary32, by the conversion of 4-bit whole numbers, 2.4 instructions a code.
+// through binary32, by the conversion of 4-bit whole numbers, which gives sixteenths.
 template <class T> struct Codes;
 template <> struct Codes<__bf16> {
-    static constexpr float kLift = 16.0f;
+    static constexpr float kLift = 16.0f, kUnit = 1.0f;
     uint32_t sixteen = 0x41804180u;
     // in a vector register: an and-or takes one constant from a scalar one
     __device__ __forceinline__ Codes() { asm("" : "+v"(sixteen)); }
@@ -45,12 +45,15 @@ template <> struct Codes<__bf16> {
     }
 };
 template <> struct Codes<float> {
-    static constexpr float kLift = -8.0f;
+    static constexpr float kLift = -8.0f, kUnit = 0.0625f;
     __device__ __forceinline__ Frag operator()(uint32_t w) const {
-        const uint32_t twos = w ^ 0x88888888u;
+        // bytes' lower halves, and one shift for the upper ones; the conversion picks bytes by itself
+        const uint32_t even = w ^ 0x88888888u;
+        uint32_t odd = even >> 4;
+        asm("" : "+v"(odd));
         Frag f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = (__bf16)(16.0f * __builtin_amdgcn_cvt_off_f32_i4((int)(twos >> (4 * (i / 2) + 16 * (i % 2)))));
+        for (int i = 0; i < 8; ++i) f[i] = (__bf16)__builtin_amdgcn_cvt_off_f32_i4((int)((i / 2 % 2 ? odd : even) >> (8 * (i / 4) + 16 * (i % 2)) & 0xffu));
         return f;
     }
 };
@@ -66,14 +69,20 @@ __device__ __forceinline__ Frag all_of(float x) {
 __device__ __forceinline__ float step_of(uint32_t pair) { return __uint_as_float(pair << 16); }
 __device__ __forceinline__ float low_of(uint32_t pair) { return __uint_as_float(pair & 0xffff0000u); }
 
-// The bfloat16 numbers that stand for a value of type T as an operand: itself, or three that add up to its 24 bits.
+// The bfloat16 numbers that stand for a value of type T as an operand: itself (rounded, if it is a result), or three that add
+// up to its 24 bits, 8 bits each.
 template <class T> constexpr int kTerms = sizeof(T) == 2 ? 1 : 3;
+__device__ __forceinline__ float upper_half(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
+__device__ __forceinline__ __bf16 half_of(float x) { return __builtin_bit_cast(__bf16, (uint16_t)(__float_as_uint(x) >> 16)); }
 template <int N> __device__ __forceinline__ void terms(float x, Frag (&f)[N], int i) {
+    if constexpr (N == 1) {
+        f[0][i] = (__bf16)x;
+    } else {
 #pragma unroll
-    for (int t = 0; t < N; ++t) {
-        const __bf16 b = (__bf16)x;
-        f[t][i] = b;
-        x -= (float)b;
+        for (int t = 0; t < N; ++t) {
+            f[t][i] = half_of(x);
+            x -= upper_half(x);
+        }
     }
 }
 template <class T> __device__ __forceinline__ void terms(const Vec<T, 8> &x, Frag (&f)[kTerms<T>]) {

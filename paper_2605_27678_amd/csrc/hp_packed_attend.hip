@@ -41,7 +41,7 @@ struct Params {
     int64_t rows, keys;
     int32_t heads_q, group, groups, dim, head_tiles;
     int32_t units;                                 // of each tile of heads; 0: each row is one
-    float scale2;                                  // for exponents of two
+    float scale2;                                  // for exponents of two, of scores in kUnit
     hp_heads_t q, out;
     hp_packed_t k, v;
     const int32_t *ranges;
@@ -217,8 +217,8 @@ struct Side {
     float first, second;                           // whether this lane's term is behind the first, the second
     __device__ __forceinline__ explicit Side(int term) : first(term >= 1 ? 1.0f : 0.0f), second(term >= 2 ? 1.0f : 0.0f) {}
     __device__ __forceinline__ __bf16 operator()(float x) const {
-        x = __builtin_fmaf(-first, (float)(__bf16)x, x);
-        return (__bf16)__builtin_fmaf(-second, (float)(__bf16)x, x);
+        x = __builtin_fmaf(-first, upper_half(x), x);
+        return half_of(__builtin_fmaf(-second, upper_half(x), x));
     }
 };
 // Over the four lanes of a row of 16 that have the same head's terms, in all of them alike.
@@ -232,7 +232,7 @@ __device__ __forceinline__ float side_sum(float x) {
 
 template <class T, int GP, int WAVES, bool SIDE> __global__ __launch_bounds__((WAVES * kWave), (kWavesASimd<T, GP, WAVES, SIDE>)) void packed_attend_kernel(Params p) {
     typedef Layout<GP> L;
-    constexpr float kLift = Codes<T>::kLift;
+    constexpr float kLift = Codes<T>::kLift, kUnit = Codes<T>::kUnit;
     constexpr bool kCentred = kLift == -kMiddle;
     constexpr int N = SIDE ? 1 : kTerms<T>, kSets = (GP + 3) / 4, kWaves = WAVES;
     __shared__ __attribute__((aligned(16))) char lds[kWaves * L::kBytes];
@@ -316,8 +316,8 @@ template <class T, int GP, int WAVES, bool SIDE> __global__ __launch_bounds__((W
             sum = column_sum(sum);
             const __bf16 a = (__bf16)sum, b = (__bf16)(sum - (float)a), c = (__bf16)(sum - (float)a - (float)b);
             const float part = quarter == 0 ? (float)a : quarter == 1 ? (float)b : quarter == 2 ? (float)c : 0.0f, of_this = term == 0 ? part : 0.0f;
-            sums[g / 4][2 * (g % 4)] = (__bf16)(-kLift * of_this);
-            sums[g / 4][2 * (g % 4) + 1] = (__bf16)of_this;
+            sums[g / 4][2 * (g % 4)] = (__bf16)(-kLift * kUnit * of_this);
+            sums[g / 4][2 * (g % 4) + 1] = (__bf16)(kUnit * of_this);
         }
 
         float top = -INFINITY, sum = 0.0f;
@@ -470,7 +470,7 @@ template <class T, int GP, int WAVES, bool SIDE> __global__ __launch_bounds__((W
     #pragma unroll
             for (int c = 0; c < 2; ++c) {
                 // rows of the transposed load are a word's bits in order: even channels in one quarter, odd ones in the next
-                const Quad v = (out[2 * g + c] + more) * part_of_all;
+                const Quad v = (out[2 * g + c] * (1.0f / kUnit) + more) * part_of_all;
                 const float2 a = across_rows(v[0], v[2]), b = across_rows(v[1], v[3]);
                 join[(wave * 2 * GP + 2 * g + c) * kWave + lane] = Quad{a.x, a.y, b.x, b.y};
             }
@@ -594,6 +594,8 @@ int check_sizes(const hp_packed_attend_args_t *a) {
     return HP_OK;
 }
 
+float scale2_of(const hp_packed_attend_args_t &a) { return a.scale * kLog2e / (a.dtype == HP_BF16 ? Codes<__bf16>::kUnit : Codes<float>::kUnit); }
+
 int part_heads_of(const hp_packed_attend_args_t &a) { return a.heads_q / a.heads_k < kHeads ? a.heads_q / a.heads_k : kHeads; }
 
 int64_t workspace_of(const hp_packed_attend_args_t &a) {
@@ -603,7 +605,7 @@ int64_t workspace_of(const hp_packed_attend_args_t &a) {
 
 int check(const hp_packed_attend_args_t *a) {
     if (const int rc = check_sizes(a)) return rc;
-    if (!(a->scale > 0) || !std::isfinite(a->scale) || !std::isfinite(a->scale * kLog2e)) return HP_EINVAL;
+    if (!(a->scale > 0) || !std::isfinite(a->scale) || !std::isfinite(scale2_of(*a))) return HP_EINVAL;
     const int size = a->dtype == HP_BF16 ? 2 : 4;
     for (const hp_heads_t *t : {&a->q, &a->out}) {
         if (a->rows > 0 && !t->data) return HP_EINVAL;
@@ -655,7 +657,7 @@ int hp_packed_attend_step(const hp_packed_attend_args_t *a, void *stream) {
     p.heads_q = a->heads_q, p.group = a->heads_q / a->heads_k, p.groups = groups_of(a->dim), p.dim = a->dim;
     const Cut cut = cut_of(*a);
     p.units = cut.units, p.head_tiles = head_tiles_of(*a), p.part_heads = part_heads_of(*a);
-    p.scale2 = a->scale * kLog2e;
+    p.scale2 = scale2_of(*a);
     p.q = a->q, p.out = a->out, p.k = without_unused(a->k, a->keys), p.v = without_unused(a->v, a->keys), p.ranges = a->ranges, p.lse = a->lse;
     const int64_t parts = (int64_t)2 * p.units * a->heads_k * p.head_tiles * p.part_heads;
     char *ws = (char *)a->workspace;

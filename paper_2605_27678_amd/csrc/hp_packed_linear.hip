@@ -58,7 +58,7 @@ template <class T, int R_, int CH_, int MT_, int DEPTH_, bool EXACT_> struct Cut
 template <class C> __global__ __launch_bounds__(kBlock) void packed_linear_kernel(Params p) {
     typedef typename C::type T;
     constexpr int R = C::R, CH = C::CH, MT = C::MT, DEPTH = C::DEPTH, N = C::N, NT = C::NT;
-    constexpr float kLift = Codes<T>::kLift;
+    constexpr float kLift = Codes<T>::kLift, kUnit = Codes<T>::kUnit;
     extern __shared__ __attribute__((aligned(16))) char shared[];
     const int tid = (int)threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), col = lane % 16, quarter = lane / 16;
     const int turn = wave & (p.waves_k - 1), tiles = kWaves / p.waves_k;
@@ -137,8 +137,8 @@ template <class C> __global__ __launch_bounds__(kBlock) void packed_linear_kerne
                 // the quarter's number of it; what stands in quarters without one meets zeros
                 float part = __builtin_fmaf(first, (float)(__bf16)sum[0], sum[0]);
                 if constexpr (N > 1) part = __builtin_fmaf(second, (float)(__bf16)part, part);
-                sums[t][2 * j] = (__bf16)(-kLift * part);
-                sums[t][2 * j + 1] = (__bf16)part;
+                sums[t][2 * j] = (__bf16)(-kLift * kUnit * part);
+                sums[t][2 * j + 1] = (__bf16)(kUnit * part);
             }
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
@@ -234,7 +234,7 @@ template <class C> __global__ __launch_bounds__(kBlock) void packed_linear_kerne
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int r = 16 * t + 4 * quarter + i;
-                if (r < rows) ((T *)p.out)[(r0 + r) * p.out_stride + n] = (T)acc[m][t][i];
+                if (r < rows) ((T *)p.out)[(r0 + r) * p.out_stride + n] = (T)(acc[m][t][i] * (1.0f / kUnit));
             }
     }
 }
