@@ -579,7 +579,7 @@ Cut cut_of(const hp_packed_attend_args_t &a) {
     const int groups = groups_of(a.dim), waves = groups <= 4 ? kWaves<4> : kWaves<8>;
     if (a.rows * tiles <= 2 * (groups <= 4 ? kFewWaves<4> : kFewWaves<8>)) return Cut{1, true};
     const int64_t slots = kComputeUnits * (a.dtype == HP_BF16 ? resident_of<__bf16>(groups) : side_by_side(a) ? resident_of<float, true>(groups) : resident_of<float>(groups));
-    const int64_t fit = slots / columns, most = (a.rows * tiles + waves - 1) / waves, units = fit < most ? fit : most;
+    const int64_t fit = slots / columns, most = (a.rows * (tiles + waves) + waves - 1) / waves, units = fit < most ? fit : most;
     return Cut{(int32_t)(units > 1 ? units : 1), false};
 }
 
