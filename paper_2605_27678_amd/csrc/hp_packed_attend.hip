@@ -278,17 +278,17 @@ template <class T, int GP, int WAVES, bool SIDE> __global__ __launch_bounds__((W
         int dim = p.dim;
         asm volatile("" : "+s"(dim));                  // or the places of all channels would be kept over the rows
         if (dim % 8 == 0) {                            // pieces are there or not
-    #pragma unroll
+#pragma unroll
             for (int g = 0; g < GP; ++g) {
                 const int d = kGroup * g + 8 * quarter;
                 x[g] = *(const typename VecOf<T, 8>::mem *)(q_row + (d < dim ? d : 0));
                 if (d >= dim) x[g] = Vec<T, 8>{};
             }
         } else {
-    #pragma unroll
+#pragma unroll
             for (int g = 0; g < GP; ++g) {
                 const int d = kGroup * g + 8 * quarter;
-    #pragma unroll
+#pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const T one = q_row[min(d + i, dim - 1)];
                     x[g][i] = d + i < dim ? one : (T)0.0f;
@@ -304,14 +304,14 @@ template <class T, int GP, int WAVES, bool SIDE> __global__ __launch_bounds__((W
             vs.fetch(v_tile, p.v, key0, state_head, hi - key0, lane);
         }
         __builtin_amdgcn_sched_barrier(0);
-    #pragma unroll
+#pragma unroll
         for (int g = 0; g < GP; ++g) {
             if constexpr (SIDE)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) q[g][0][i] = side(spare ? 0.0f : (float)x[g][i]);
             else terms<T>(x[g], q[g]);
             float sum = 0.0f;
-    #pragma unroll
+#pragma unroll
             for (int i = 0; i < 8; ++i) sum += (float)x[g][i];
             sum = column_sum(sum);
             const __bf16 a = (__bf16)sum, b = (__bf16)(sum - (float)a), c = (__bf16)(sum - (float)a - (float)b);
@@ -329,14 +329,14 @@ template <class T, int GP, int WAVES, bool SIDE> __global__ __launch_bounds__((W
             settle();
             Quad s[4];
             const Vec<uint32_t, L::kPairs> k_pairs = *(const Vec<uint32_t, L::kPairs> *)(k_scales + L::kPairs * own);
-    #pragma unroll
+#pragma unroll
             for (int a = 0; a < 4; ++a) {
                 s[a] = Quad{};
                 const Vec<uint32_t, L::kPairs> pairs = *(const Vec<uint32_t, L::kPairs> *)(k_scales + L::kPairs * (16 * a + col));
-    #pragma unroll
+#pragma unroll
                 for (int h = 0; h < kSets; ++h) {
                     Words w = {};
-    #pragma unroll
+#pragma unroll
                     for (int j = 0; j < 4 && 4 * h + j < L::kPairs; ++j) w[j] = pairs[4 * h + j];
                     s[a] = mma(__builtin_bit_cast(Frag, w), sums[h], s[a]);
                 }
@@ -345,7 +345,7 @@ template <class T, int GP, int WAVES, bool SIDE> __global__ __launch_bounds__((W
                 each<4>([&](auto a) {
                     const Frag c = codes(*(const uint32_t *)(k_tile + L::at(16 * a + col, g) + 4 * quarter));
                     Quad d = {};
-    #pragma unroll
+#pragma unroll
                     for (int n = 0; n < N; ++n) d = mma(c, q[g][n], d);
                     each<4>([&](auto i) { s[a][i.value] += of_lane<4 * a + i>(step_of(k_pairs[g.value])) * d[i.value]; });
                 });
@@ -356,20 +356,20 @@ template <class T, int GP, int WAVES, bool SIDE> __global__ __launch_bounds__((W
 #pragma unroll
                     for (int i = 0; i < 4; ++i) s[a][i] = side_sum(s[a][i]);
             // here, not behind the branch, where all these products' results would have to be kept until then
-    #pragma unroll
+#pragma unroll
             for (int a = 0; a < 4; ++a) asm("" : "+v"(s[a]));
             reads_done();
             if (more) ks.fetch(k_tile, p.k, next, state_head, hi - next, lane);
 
             if (key0 + kTile > hi)
-    #pragma unroll
+#pragma unroll
                 for (int a = 0; a < 4; ++a)
-    #pragma unroll
+#pragma unroll
                     for (int i = 0; i < 4; ++i) s[a][i] = key0 + 16 * a + 4 * quarter + i < hi ? s[a][i] : -INFINITY;
             float most = s[0][0];
-    #pragma unroll
+#pragma unroll
             for (int a = 0; a < 4; ++a)
-    #pragma unroll
+#pragma unroll
                 for (int i = 0; i < 4; ++i) most = fmaxf(most, s[a][i]);
             most = column_max(most) * p.scale2;
             const bool grows = most > top + kLag;
@@ -378,13 +378,13 @@ template <class T, int GP, int WAVES, bool SIDE> __global__ __launch_bounds__((W
                 top = grows ? most : top;
                 sum *= keep;
                 rest *= keep;
-    #pragma unroll
+#pragma unroll
                 for (int c = 0; c < 2 * GP; ++c) out[c] *= keep;
             }
             const float base = top == -INFINITY ? 0.0f : top;
-    #pragma unroll
+#pragma unroll
             for (int a = 0; a < 4; ++a)
-    #pragma unroll
+#pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     s[a][i] = __builtin_amdgcn_exp2f(s[a][i] * p.scale2 - base);
                     sum += s[a][i];
@@ -394,23 +394,40 @@ template <class T, int GP, int WAVES, bool SIDE> __global__ __launch_bounds__((W
             if (more) __builtin_amdgcn_s_waitcnt(but(Loader<GP>::kLoads));
             else __builtin_amdgcn_s_waitcnt(but(0));
             settle();
-            // 8 sum p step + sum p low: row 2g of the left operand has group g's steps, row 2g + 1 its lows
-            {
+            if constexpr (kCentred) {
+                // sum p (8 step + low): row g of the left operand has group g's pairs as they lie there, the right one 8p and p by
+                // turns, so that what is large of either meets in the product and does not add up by itself (binary32 would lose
+                // three bits of outputs that are small beside the values)
+#pragma unroll
+                for (int a = 0; a < 4; ++a) {
+                    Words pairs;
+                    Frag weights[N];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        pairs[i] = v_scales[L::kPairs * (16 * a + 4 * quarter + i) + col % L::kPairs];
+                        split(kMiddle * s[a][i], weights, 2 * i);
+                        split(s[a][i], weights, 2 * i + 1);
+                    }
+#pragma unroll
+                    for (int n = 0; n < N; ++n) rest = mma(__builtin_bit_cast(Frag, pairs), weights[n], rest);
+                }
+            } else {
+                // 8 sum p step + sum p low: row 2g of the left operand has group g's steps, row 2g + 1 its lows
                 typedef short Four __attribute__((ext_vector_type(4)));
                 typedef __attribute__((address_space(3))) Four *Lds;
                 // 16 lanes bring four states' pairs, 8 bytes a lane; beyond a state's pairs rows of the product are not read
                 const uint32_t *line = v_scales + L::kPairs * (4 * quarter + col / 4) + 2 * (col % 4 % (L::kPairs / 2));
-    #pragma unroll
+#pragma unroll
                 for (int b = 0; b < 2; ++b) {
                     const Four even = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(line + L::kPairs * 32 * b)), odd = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(line + L::kPairs * (32 * b + 16)));
                     const Frag pairs = __builtin_bit_cast(Frag, __builtin_shufflevector(even, odd, 0, 1, 2, 3, 4, 5, 6, 7));
                     Frag weights[N];
-    #pragma unroll
+#pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         split(s[2 * b][i], weights, i);
                         split(s[2 * b + 1][i], weights, 4 + i);
                     }
-    #pragma unroll
+#pragma unroll
                     for (int n = 0; n < N; ++n) rest = mma(pairs, weights[n], rest);
                 }
             }
@@ -426,13 +443,13 @@ template <class T, int GP, int WAVES, bool SIDE> __global__ __launch_bounds__((W
                 typedef int Pair __attribute__((ext_vector_type(2)));
                 typedef __attribute__((address_space(3))) Pair *Lds;
                 const char *line = v_tile + L::at(own, g);
-    #pragma unroll
+#pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     const Pair w = __builtin_amdgcn_ds_read_tr4_b64_v2i32((Lds)(line + 8 * c));
-    #pragma unroll
+#pragma unroll
                     for (int b = 0; b < 2; ++b) {
                         const Frag l = codes((uint32_t)w[b]);
-    #pragma unroll
+#pragma unroll
                         for (int n = 0; n < N; ++n) {
                             if constexpr (!kCentred) out[2 * g + c] = mma(centre, weights[b][n], out[2 * g + c]);
                             out[2 * g + c] = mma(l, weights[b][n], out[2 * g + c]);
@@ -455,19 +472,21 @@ template <class T, int GP, int WAVES, bool SIDE> __global__ __launch_bounds__((W
         }
         __syncthreads();
         float most = -INFINITY, total = 0.0f;
-    #pragma unroll
+#pragma unroll
         for (int w = 0; w < kWaves; ++w) most = fmaxf(most, tops[w * kHeads + col]);
         // a wave without a maximum has seen nothing, or NaN alone
         const auto weight = [&](float t) { return t == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(t - most); };
-    #pragma unroll
+#pragma unroll
         for (int w = 0; w < kWaves; ++w) total += totals[w * kHeads + col] * weight(tops[w * kHeads + col]);
         const float part_of_all = total == 0.0f ? 0.0f : weight(top) / total;
         const float lse2 = total == 0.0f ? -INFINITY : most + __builtin_amdgcn_logf(total);
-    #pragma unroll
+#pragma unroll
         for (int g = 0; g < GP; ++g) {
-            const int from = 16 * (g / 2) + col;
-            const float more = kMiddle * __shfl(rest[2 * (g % 2)], from) + __shfl(rest[2 * (g % 2) + 1], from);
-    #pragma unroll
+            const int from = kCentred ? 16 * (g / 4) + col : 16 * (g / 2) + col;
+            float more;
+            if constexpr (kCentred) more = __shfl(rest[g % 4], from);
+            else more = kMiddle * __shfl(rest[2 * (g % 2)], from) + __shfl(rest[2 * (g % 2) + 1], from);
+#pragma unroll
             for (int c = 0; c < 2; ++c) {
                 // rows of the transposed load are a word's bits in order: even channels in one quarter, odd ones in the next
                 const Quad v = (out[2 * g + c] * (1.0f / kUnit) + more) * part_of_all;
@@ -480,7 +499,7 @@ template <class T, int GP, int WAVES, bool SIDE> __global__ __launch_bounds__((W
         for (int t = wave; t < 2 * GP; t += kWaves) {
             const int d = 16 * t + 4 * quarter;
             Quad v = {};
-    #pragma unroll
+#pragma unroll
             for (int w = 0; w < kWaves; ++w) v += join[(w * 2 * GP + t) * kWave + lane];
             if constexpr (SIDE)
 #pragma unroll
@@ -490,7 +509,7 @@ template <class T, int GP, int WAVES, bool SIDE> __global__ __launch_bounds__((W
                 store<4>(p.products + (part * p.part_heads + col) * p.dim + d, v, p.dim - d);
             } else {
                 Vec<T, 4> o;
-    #pragma unroll
+#pragma unroll
                 for (int i = 0; i < 4; ++i) o[i] = (T)v[i];
                 store<4>((T *)p.out.data + row * p.out.row_stride + (int64_t)(head0 + col) * p.out.head_stride + d, o, p.dim - d);
             }

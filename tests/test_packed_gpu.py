@@ -203,6 +203,23 @@ def test_large_scores_and_far_maxima():
         attend_check(q, packed_of(k.flip(0).contiguous().to(dtype)), v, None, 1.0)
 
 
+def test_outputs_that_are_small_beside_the_values():
+    """Means of 8000 values around zero.  A wave of a row's four adds up 2000 of them in 32 tiles, in six products each at most; every
+    addition rounds by half a step of what it has then, and 200 such roundings come to six times the root of their number at most.
+    (What cancels, steps against lows, has 20 times their size and may not add up by itself.)"""
+    rows, keys, dim = 600, 8000, 64
+    k, v = packed_of(rand(2, keys, 1, dim, dtype=F32)), packed_of(rand(3, keys, 1, dim, dtype=F32))
+    q = rand(4, 1, 1, dim, dtype=F32).expand(rows, 1, dim)
+    out, _ = attend_run(q, k, v, None)
+    p = torch.softmax(plain.values(k, dim)[:, 0] @ q[0, 0].double() * dim ** -0.5, 0)
+    terms = p[:, None] * plain.values(v, dim)[:, 0]
+    most = sum(terms[64 * w:].unfold(0, 64, 256).sum(-1).cumsum(0).abs().amax(0) for w in range(4))
+    # and the weights themselves: their exponents' roundings, of unlike signs too
+    weights = 6 * (terms * terms).sum(0).sqrt() * 2.0 ** -20
+    apart = (out.double()[:, 0] - terms.sum(0)).abs()
+    assert float((apart - (6 * 200 ** 0.5 * 2.0 ** -24 * most + weights)).max()) <= 0
+
+
 # ---- linear ---------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
