@@ -77,7 +77,8 @@ int hp_unpack(const hp_pack_args_t *args, void *stream);
  * own pass over its range, and what it does not see has no influence on it.  The states'
  * values enter as they are, not rounded to the type.  In HP_BF16 two numbers on the way
  * are rounded to 16 bits, the weights P and P * step, operands of matrix products
- * (HP_F32: none).  A state that is seen and is NaN in a group of v leaves NaN in that
+ * (HP_F32: none).  Sums on the way may be 2^11 times the number of states times the largest
+ * value of v: values from 2^90 on are not safe from overflow.  A state that is seen and is NaN in a group of v leaves NaN in that
  * group's channels; queries that are not finite, NaN in their head's.
  *   q, out: [rows, heads_q, dim]; k, v: [keys, heads_k, dim]; dim 1..HP_ATTEND_MAX_DIM.
  *   Limits are hp_cross_attend_step's; row strides of packed states up to 2^24 (HP_ELAYOUT),
@@ -105,7 +106,7 @@ int64_t hp_packed_attend_workspace(const hp_packed_attend_args_t *args);
 /* hp_packed_linear - out[r][n] = sum_k x[r][k] w[n][k] for x [rows, n_in], packed w
  * [n_out, n_in] (one head: head strides are not read) and out [rows, n_out].  Sums are in
  * binary32, the weights' values are not rounded (in HP_BF16 the part of the lows may be off
- * by 2^-18 of 16 step + |low| times a group's sum of x); a row of x that is not finite gives NaN.
+ * by 2^-18 of 16 step + |low| times a group's sum of x); out may not overlap x; a row of x that is not finite gives NaN.
  * Made for the rows of a decoding step: up to 64 rows (32 in HP_F32) at a time share a
  * pass over the weights.  Fastest where x is 16-byte aligned and its rows and their stride
  * are multiples of 16 bytes (other x: passes of 32 rows).

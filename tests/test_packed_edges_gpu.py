@@ -134,6 +134,32 @@ def test_the_most_rows():
     assert torch.equal(out.view(-1, 64, 1, dim), want[None].expand(rows // 64, -1, -1, -1))
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("heads_q,heads_k,dim", [(6, 2, 64), (12, 2, 96), (4, 4, 256)])
+def test_queries_that_are_not_finite_stay_by_themselves(dtype, heads_q, heads_k, dim):
+    q, k, v = rand(1, 5, heads_q, dim, dtype=dtype), packed_of(rand(2, 900, heads_k, dim)), packed_of(rand(3, 900, heads_k, dim))
+    ranges = ranges_of((0, 900), (5, 300), (7, 7), (100, 200), (0, 64))
+    want, _ = attend_run(q, k, v, ranges)
+    q[0, 1, 3], q[1, heads_q - 1, dim - 1], q[2, 0, 0], q[3, 2, 1] = float("inf"), float("nan"), float("nan"), -float("inf")
+    got, _ = attend_run(q, k, v, ranges)
+    nan = torch.zeros_like(got, dtype=torch.bool)
+    nan[0, 1] = nan[1, heads_q - 1] = nan[3, 2] = True
+    assert torch.equal(torch.isnan(got), nan) and torch.equal(got[~nan], want[~nan])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_large_and_small_values(dtype):
+    q, k, v = rand(1, 4, 6, 96, dtype=dtype), rand(2, 500, 2, 96, dtype=dtype), rand(3, 500, 2, 96, dtype=dtype, around=0.5)
+    x, w = rand(4, 5, 320, dtype=dtype), rand(5, 70, 320, dtype=dtype)
+    for size in (2.0 ** 60, 2.0 ** -60):
+        attend_check(q * size, packed_of(k / size), packed_of(v * size), None)
+        out = torch.empty(5, 70, dtype=dtype, device=DEV)
+        for a, b in ((x * size, w), (x, w * size), (x * size, w / size)):
+            p = packed_of(b)
+            hp.hp_packed_linear(a, p, out)
+            check("out", out, *plain.linear(a, p))
+
+
 # ---- far apart ----------------------------------------------------------------------------------------------------------
 
 def test_caches_whose_places_pass_32_bits():
@@ -281,6 +307,26 @@ def test_a_step_on_another_stream():
         step(scratch, side)
         torch.cuda.current_stream().wait_stream(side)
         assert torch.equal(t["y"], want)
+
+
+def test_two_steps_at_once():
+    """On streams of their own, with scratch memory of their own."""
+    calls = [layer_of(), layer_of(heads_k=4, dim=128, keys=2500)]
+    want = []
+    for t, step, scratch, _ in calls:
+        step(scratch, None)
+        torch.cuda.synchronize()
+        want.append(t["y"].clone())
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        for t, *_ in calls:
+            t["y"].zero_()
+        torch.cuda.synchronize()
+        for _ in range(3):
+            for (t, step, scratch, _), stream in zip(calls, streams):
+                step(scratch, stream)
+        torch.cuda.synchronize()
+        assert all(torch.equal(t["y"], y) for (t, *_), y in zip(calls, want))
 
 
 def test_two_captured_steps_that_share_scratch_memory():
