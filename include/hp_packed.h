@@ -107,9 +107,9 @@ int64_t hp_packed_attend_workspace(const hp_packed_attend_args_t *args);
  * [n_out, n_in] (one head: head strides are not read) and out [rows, n_out].  Sums are in
  * binary32, the weights' values are not rounded (in HP_BF16 the part of the lows may be off
  * by 2^-18 of 16 step + |low| times a group's sum of x); out may not overlap x; a row of x that is not finite gives NaN.
- * Made for the rows of a decoding step: up to 64 rows (32 in HP_F32) at a time share a
- * pass over the weights.  Fastest where x is 16-byte aligned and its rows and their stride
- * are multiples of 16 bytes (other x: passes of 32 rows).
+ * Made for the rows of a decoding step: up to 32 rows at a time share a pass over the
+ * weights.  Fastest where x is 16-byte aligned and its rows and their stride
+ * are multiples of 16 bytes.
  * n_in up to HP_PACKED_MAX_DIM, n_out up to 2^24, rows up to 2^20, row strides of w up
  * to 2^24 and not negative (HP_ELAYOUT). */
 typedef struct hp_packed_linear_args {

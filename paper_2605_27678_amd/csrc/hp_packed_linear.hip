@@ -5,14 +5,14 @@
 // four groups at a time they are, split into numbers of 8 bits over the quarters (two of bfloat16's, which leave 2^-18 of a
 // group's sum out; three of binary32's), the left operand of one more product, whose right one is the pairs (step, low) as
 // they lie in memory: it puts sum x low in and takes off what the codes are lifted by.
-// The waves of a workgroup share out the inner axis, 128 of it at a time, and add up at the end in their order.  Each brings its
+// The waves of a workgroup share out the inner axis, 64 to 256 of it at a time, and add up at the end in their order.  Each brings its
 // own pieces of x and w to LDS, ahead of their use and without barriers: the operands' rows lie in neighbouring lanes, and
 // loads straight into registers took the caches 64 cycles each, one a lane, where runs of 64 and 256 bytes take 16
 // (12288 x 12288 by 16 rows: 36 us, this way 29).
 //
-// The weights are 5 bits a value, read once by up to 64 rows: 95 MB of these 12288 x 12288 are 18 us at the rate of a large
-// copy, and the loads alone take 27.  With more rows the caches are busier with x: of 8192 x 8192 by 64
-// rows every compute unit reads all of x, 1 MB, for its 32 rows of w, 256 MB next to 44; that takes 29 us, the loads alone 24.
+// The weights are 5 bits a value, read once by up to 32 rows: 95 MB of these 12288 x 12288 are 18 us at the rate of a large
+// copy, and the loads alone take 27.  With more rows the caches are busier with x: of 8192 x 8192 by 64 rows every compute
+// unit reads half of x, 0.5 MB, for its 64 rows of w, 128 MB next to 2 x 44; that takes 25 us, where a copy of the 44 MB takes 9.
 #include "hp_packed.hpp"
 
 #pragma clang fp contract(fast)
@@ -47,7 +47,8 @@ template <class T, int R_, int CH_, int MT_, int DEPTH_, bool EXACT_> struct Cut
     static constexpr int kLoads = (EXACT ? kXLoads : 0) + 2 * kWLoads, kLds = kWaves * DEPTH * kBytes;
     // binary32 operands are two pieces, which stay neighbours
     static __device__ __forceinline__ int x_slot(int row, int piece) { return sizeof(T) == 2 ? piece ^ (row & (kPieces - 1)) : piece ^ (2 * row & (kPieces - 2)); }
-    static __device__ __forceinline__ int code_slot(int row, int piece) { return CH == 4 ? piece ^ (row >> 1 & 3) : piece ^ (row >> 2 & 1); }
+    static __device__ __forceinline__ int code_slot(int row, int piece) { return piece ^ ((CH == 8 ? row : row / (16 / CH)) & (CH - 1)); }
+    static_assert(CH <= 8, "a load has as many rows of w as are turned in a period");
     // loads of x whose pieces are turned alike are so many rows and loads apart
     static constexpr int kRowsALoad = kWave / kPieces, kPeriod = sizeof(T) == 2 ? kPieces : kPieces / 2;
     static constexpr int kKinds = kPeriod / kRowsALoad < kXLoads ? kPeriod / kRowsALoad : kXLoads;
@@ -57,7 +58,7 @@ template <class T, int R_, int CH_, int MT_, int DEPTH_, bool EXACT_> struct Cut
 
 template <class C> __global__ __launch_bounds__(kBlock) void packed_linear_kernel(Params p) {
     typedef typename C::type T;
-    constexpr int R = C::R, CH = C::CH, MT = C::MT, DEPTH = C::DEPTH, N = C::N, NT = C::NT;
+    constexpr int R = C::R, CH = C::CH, MT = C::MT, DEPTH = C::DEPTH, N = C::N, NT = C::NT, kSets = (CH + 3) / 4;
     constexpr float kLift = Codes<T>::kLift, kUnit = Codes<T>::kUnit;
     extern __shared__ __attribute__((aligned(16))) char shared[];
     const int tid = (int)threadIdx.x, lane = tid % kWave, wave = __builtin_amdgcn_readfirstlane(tid / kWave), col = lane % 16, quarter = lane / 16;
@@ -114,8 +115,8 @@ template <class C> __global__ __launch_bounds__(kBlock) void packed_linear_kerne
     // whether this quarter's number of a sum is behind the first, the second
     const float first = quarter >= 1 ? -1.0f : 0.0f, second = quarter >= 2 ? -1.0f : 0.0f;
     const auto add = [&](const char *from) {
-        Words low[MT] = {};
-        Frag sums[NT] = {};
+        Words low[MT][kSets] = {};                 // for four groups at a time
+        Frag sums[NT][kSets] = {};
 #pragma unroll
         for (int j = 0; j < CH; ++j) {
             Frag a[NT][N];
@@ -137,8 +138,8 @@ template <class C> __global__ __launch_bounds__(kBlock) void packed_linear_kerne
                 // the quarter's number of it; what stands in quarters without one meets zeros
                 float part = __builtin_fmaf(first, (float)(__bf16)sum[0], sum[0]);
                 if constexpr (N > 1) part = __builtin_fmaf(second, (float)(__bf16)part, part);
-                sums[t][2 * j] = (__bf16)(-kLift * kUnit * part);
-                sums[t][2 * j + 1] = (__bf16)(kUnit * part);
+                sums[t][j / 4][2 * (j % 4)] = (__bf16)(-kLift * kUnit * part);
+                sums[t][j / 4][2 * (j % 4) + 1] = (__bf16)(kUnit * part);
             }
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
@@ -146,7 +147,7 @@ template <class C> __global__ __launch_bounds__(kBlock) void packed_linear_kerne
                 const Frag l = codes_of(*(const uint32_t *)(from + C::kCodes + (row * CH + C::code_slot(row, j)) * kGroupBytes + 4 * quarter));
                 const uint32_t pair = *(const uint32_t *)(from + C::kPairs + (row * CH + j) * 4);
                 const float step = step_of(pair);
-                low[m][j] = quarter <= (N > 1 ? 2 : 1) ? pair : 0;
+                low[m][j / 4][j % 4] = quarter <= (N > 1 ? 2 : 1) ? pair : 0;
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
                     Quad d = {};
@@ -160,7 +161,9 @@ template <class C> __global__ __launch_bounds__(kBlock) void packed_linear_kerne
 #pragma unroll
         for (int m = 0; m < MT; ++m)
 #pragma unroll
-            for (int t = 0; t < NT; ++t) acc[m][t] = mma(sums[t], __builtin_bit_cast(Frag, low[m]), acc[m][t]);
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int h = 0; h < kSets; ++h) acc[m][t] = mma(sums[t][h], __builtin_bit_cast(Frag, low[m][h]), acc[m][t]);
     };
 
     const auto group_of = [&](int i) { return (turn + i * p.waves_k) * CH; };
@@ -262,12 +265,12 @@ template <class C> dim3 blocks_of(Params &p) {
 }
 
 // The first of these cuts, the smallest, of which the compute units take all workgroups at once; otherwise the last.  A
-// larger tile reads x and waits for the join less often, a second turn costs as much as the first (us, each cut by itself):
-//   4096 x 4096 by 16 rows in tiles of 16 / 32 rows of w   6.0 / 7.8      12288 x 12288: 16 / 32 / 48 / 64   42 / 40 / 29 / 35
-//   8192 x 2048 by 64 rows in tiles of 16 x 32 / 32 x 32 / 64 x 32 (rows of x times rows of w)   11.8 / 16.1 / 23.4
-//   8192 x 8192 by 64 rows, the same                                                             44.9 / 35.2 / 28.6
+// larger tile reads x and waits for the join less often, a second turn costs as much as the first (us, bfloat16, each cut by itself):
+//   4096 x 4096 by 16 rows in tiles of 16 / 32 rows of w   6.0 / 7.1      12288 x 12288: 16 / 32 / 48 / 64   36 / 37 / 29 / 30
+//   8192 x 2048 by 64 rows in tiles of 16 x 32 / 32 x 32 / 32 x 64 (rows of x times rows of w)   11.5 / 14.8 / 22
+//   8192 x 8192 by 64 rows, the same                                                             47 / 31 / 25
 // Up to four rows in bfloat16 are the exception: their workgroups are small enough that several share a compute unit, and
-// tiles of 16 were the fastest throughout (12288 x 12288 by one row 24.4, of 48 26.2; 28672 x 4096 22.6 and 28.8).
+// tiles of 16 were the fastest throughout (12288 x 4096 by one row 8.6, of 48 11.6; 28672 x 4096 17.7 and 23.3).
 template <class C, class... More> void launch(Params &p, hipStream_t s) {
     const dim3 blocks = blocks_of<C>(p);
     if constexpr (sizeof...(More) > 0)
@@ -275,9 +278,13 @@ template <class C, class... More> void launch(Params &p, hipStream_t s) {
     packed_linear_kernel<C><<<blocks, kBlock, C::kLds, s>>>(p);
 }
 
-// Rows of x that are no whole aligned pieces of 16 bytes pass through registers and wait for themselves (12288 x 12288 by 16
-// rows: 49 us).  Up to 4 rows take 1/4 of the LDS that 16 do (4096 x 4096 by one row 5.7 us, as 16 rows 5.9; 12288 x 12288 24 and
-// 33).  Binary32 has three products for one and twice x's bytes: 64 rows do not fit.
+// Chunks are as long as LDS allows, for few and long requests to the caches, or fewer and more in turn, for loads to be ahead: two
+// waves a SIMD hide the loads of a single chunk if there is enough to do with it (8192 x 8192 by 64 rows in tiles of 32 x 64: one
+// chunk of 128 channels 25 us, two of 64 in turn 28; 4096 x 4096 by 16 rows: three of 64 6.0, one of 128 6.5).  Where workgroups
+// are small, two chunks in turn leave room for four of them (28672 x 4096 by one row 17.7 us, four chunks 21.2).
+//
+// Rows of x that are no whole aligned pieces of 16 bytes pass through registers and wait for themselves (12288 x 8195 by 16
+// rows: 40 us, of 8192 about 20).  Binary32 has three products for one and twice x's bytes.
 template <class T> void choose(Params &p, hipStream_t s) {
     constexpr int kPiece = 16 / sizeof(T);
     const bool exact = (uintptr_t)p.x % 16 == 0 && p.n_in % kPiece == 0 && p.x_stride % kPiece == 0 && p.x_stride >= 0 && p.x_stride <= kMostStride / 4;
@@ -286,14 +293,13 @@ template <class T> void choose(Params &p, hipStream_t s) {
         else if (p.rows <= 16) launch<Cut<T, 16, 2, 1, 3, false>, Cut<T, 16, 2, 2, 3, false>>(p, s);
         else launch<Cut<T, 32, 2, 2, 2, false>>(p, s);
     } else if constexpr (sizeof(T) == 2) {
-        if (p.rows <= 4) launch<Cut<T, 4, 4, 1, 4, true>>(p, s);
-        else if (p.rows <= 16) launch<Cut<T, 16, 2, 1, 3, true>, Cut<T, 16, 4, 2, 3, true>, Cut<T, 16, 4, 3, 2, true>, Cut<T, 16, 4, 4, 2, true>>(p, s);
-        else if (p.rows <= 32) launch<Cut<T, 16, 4, 2, 3, true>, Cut<T, 32, 2, 2, 3, true>, Cut<T, 32, 2, 4, 2, true>>(p, s);
-        else launch<Cut<T, 16, 4, 2, 3, true>, Cut<T, 32, 2, 2, 3, true>, Cut<T, 64, 2, 2, 2, true>>(p, s);
+        if (p.rows <= 4) launch<Cut<T, 4, 4, 1, 2, true>>(p, s);
+        else if (p.rows <= 16) launch<Cut<T, 16, 2, 1, 3, true>, Cut<T, 16, 4, 2, 1, true>, Cut<T, 16, 4, 3, 2, true>, Cut<T, 16, 8, 4, 1, true>>(p, s);
+        else launch<Cut<T, 16, 4, 2, 3, true>, Cut<T, 32, 4, 2, 1, true>, Cut<T, 32, 4, 3, 1, true>, Cut<T, 32, 4, 4, 1, true>>(p, s);
     } else {
-        if (p.rows <= 4) launch<Cut<T, 4, 4, 1, 4, true>, Cut<T, 4, 4, 2, 4, true>, Cut<T, 4, 4, 3, 3, true>, Cut<T, 4, 4, 4, 2, true>>(p, s);
+        if (p.rows <= 4) launch<Cut<T, 4, 4, 1, 2, true>, Cut<T, 4, 4, 2, 2, true>, Cut<T, 4, 4, 3, 2, true>, Cut<T, 4, 4, 4, 1, true>>(p, s);
         else if (p.rows <= 16) launch<Cut<T, 16, 2, 1, 3, true>, Cut<T, 16, 2, 2, 3, true>, Cut<T, 16, 2, 3, 3, true>, Cut<T, 16, 2, 4, 2, true>>(p, s);
-        else launch<Cut<T, 16, 2, 2, 3, true>, Cut<T, 32, 2, 2, 2, true>>(p, s);
+        else launch<Cut<T, 16, 2, 2, 3, true>, Cut<T, 32, 2, 2, 2, true>, Cut<T, 32, 2, 2, 1, true>>(p, s);
     }
 }
 
