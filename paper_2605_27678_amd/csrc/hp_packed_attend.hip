@@ -5,19 +5,20 @@
 // in one pass with a running maximum m and sum.  The codes go into the matrix units as they are (hp_packed.hpp).
 //
 // A wave takes 64 states at a time by itself.  S^T = K Q^T, so that a lane has scores of one head, four states of each 16.
-// A word of codes is a lane's 8 channels of one state, an operand as it is.  The steps go over a group's 16 x 16 results before they add up: each lane reads those of one state, and a
-// multiplication takes them from whichever lane of its row has them.  (Read from LDS by every lane that needs them they were
-// 32 of 56 LDS reads of 16 bytes, and 120 us for 64 requests of 576 to 6404 states.)  out^T = V^T P^T has the states as inner
-// values: the transposing LDS load brings a lane 16 states of one channel, in the order in which it has their weights, so
-// that no weight leaves its lane; the weights, times the group's steps, are rounded to bfloat16 (three such numbers in
-// binary32).  What the codes' lift puts into a product, and 8 more so that codes lie around zero and cancel little, is taken
-// off by a product with -24 throughout, from the very same rounded weights (in binary32 they lie there as they are);
-// 8 * sum p step + sum p low come from one more product, whose left rows are the groups' steps and lows.
+// A word of codes is a lane's 8 channels of one state, an operand as it is.  The steps go over a group's 16 x 16 results
+// before they add up: each lane reads those of one state, and a multiplication takes them from whichever lane of its row has
+// them.  (Read from LDS by every lane that needs them they were 32 of 56 LDS reads of 16 bytes, and 120 us for 64 requests of
+// 576 to 6404 states.)  out^T = V^T P^T has the states as inner values: the transposing LDS load brings a lane 16 states of one
+// channel, in the order in which it has their weights, so that no weight leaves its lane; the weights, times the group's
+// steps, are rounded to bfloat16 (three such numbers in binary32).  What the codes' lift puts into a product, and 8 more so
+// that codes lie around zero and cancel little, is taken off by a product with -24 throughout, from the very same rounded
+// weights (in binary32 they lie there as they are); 8 sum p step + sum p low come from one more product.
 //
 // A state and head are 5 bits a channel of k and of v, each read once, so memory bounds it: 288 MB of 64 requests are 56 us at
-// the rate of a large copy.  It takes 74, and 6 more for the join; the same loads without the computing take 66, behind
-// which the computing hides where three waves share a SIMD.  Heads of 256 leave it one or two: 43 us for 110 MB (loads alone 37, a
-// copy 21).  Binary32, with three products for one, takes 50 us for 53 MB in heads of 72 (30, 10).
+// the rate of a large copy.  It takes 72, and 5 more for the join; the same loads without the computing take 66, behind
+// which the computing hides where three waves share a SIMD.  Heads of 256 leave it one or two: 36 us for 110 MB (a copy 21).
+// Where rows are short, what begins and ends them counts: 30 requests of 1 to 2305 states, 16 heads of 72, 53 MB (a copy
+// 10) take 31 us in bfloat16, 37 in binary32; per added MB they take no more than a copy, and 1.7 times as much.
 // Sets of heads side by side in a product's columns (few heads share a state head) took a quarter less arithmetic and no
 // less time; rings of three tiles instead of two leave room for fewer waves (64 requests 113 us).
 #include <climits>
@@ -523,7 +524,8 @@ template <class T, int GP, int WAVES, bool SIDE> __global__ __launch_bounds__((W
 }
 
 // Joins the parts of rows that lie in several units.  A row and head has `waves` waves, which take every waves-th part; a
-// workgroup is one row and head of four or sixteen waves, or four heads of one.
+// workgroup is one row and head of four or sixteen waves, or four heads of one.  4 to 7 us, a launch and three loads one behind
+// the other: which units, their sums, their products (asking for the first products ahead changed nothing).
 constexpr int kMostJoin = 16;
 template <class T> __global__ __launch_bounds__(kMostJoin * kWave) void packed_join_kernel(Params p, int waves) {
     __shared__ __attribute__((aligned(16))) float shared[kMostJoin][HP_ATTEND_MAX_DIM];
