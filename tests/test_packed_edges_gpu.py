@@ -198,6 +198,32 @@ def test_caches_whose_places_pass_32_bits():
     assert all(torch.equal(back[a:a + (1 << 20)], value.expand_as(back[a:a + (1 << 20)])) for a in range(0, rows, 1 << 20))
 
 
+def apart_by(t, stride):
+    """The same rows, `stride` elements from one to the next (and of heads what a row has)."""
+    far = torch.empty(len(t) * stride, dtype=t.dtype, device=DEV).as_strided(t.shape, (stride, *t[0].contiguous().stride()))
+    return far.copy_(t)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_the_largest_strides(dtype):
+    """Rows of a tile of 64 lie 2^30 bytes of codes and 2^31 of scales apart; x beyond what offsets of 32 bits hold takes another way."""
+    q, k = rand(1, 3, 4, 96, dtype=dtype), packed_of(rand(2, 130, 2, 96))
+    far = hp.Packed(apart_by(k.codes, 1 << 24), apart_by(k.scales, 1 << 24))
+    ranges = ranges_of((0, 130), (1, 66), (64, 129))
+    got, want = attend_run(q, far, far, ranges), attend_run(q, k, k, ranges)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    w, x = packed_of(rand(3, 130, 320)), rand(4, 40, 320, dtype=dtype)
+    far_w = hp.Packed(apart_by(w.codes, 1 << 24), apart_by(w.scales, 1 << 24))
+    for rows in (3, 16, 40):
+        outs = [torch.empty(rows, 130, dtype=dtype, device=DEV) for _ in range(4)]
+        for out, a, b in zip(outs, (x, x, apart_by(x, 1 << 22), apart_by(x, (1 << 22) + 8)), (w, far_w, w, w)):
+            hp.hp_packed_linear(a[:rows], b, out)
+        assert torch.equal(outs[1], outs[0]) and torch.equal(outs[2], outs[0])
+        check("through registers", outs[3], *plain.linear(x[:rows], w))
+    with pytest.raises(hp.HpError):
+        hp.hp_packed_linear(x, hp.Packed(apart_by(w.codes[:3], (1 << 24) + 16), w.scales[:3]), outs[0][:, :3])
+
+
 def test_levels_beyond_the_largest_number():
     x = torch.zeros(2, 1, 32, dtype=F32, device=DEV)
     x[0, 0, 3], x[0, 0, 4] = torch.finfo(F32).max, -3.0e38
