@@ -544,7 +544,7 @@ template <class T> __global__ __launch_bounds__(kMostJoin * kWave) void packed_j
     for (int u = first + kWave; u <= units.y; u += kWave) top = fmaxf(top, p.lse2[part(u)]);
 #pragma unroll
     for (int d = kWave / 2; d; d /= 2) top = fmaxf(top, __shfl_xor(top, d));
-    // nothing seen in a part: no weight; NaN stays
+    // nothing seen in a part: no weight; NaN stays, of the products too, which are added up whatever their weight
     const auto weight = [&](float t) { return t == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(t - top); };
     const float mine = weight(own);
     float sum = mine;
@@ -555,7 +555,7 @@ template <class T> __global__ __launch_bounds__(kMostJoin * kWave) void packed_j
     for (int u = units.x + wave; u <= units.y; u += waves) {
         const Quad v = load<4>(p.products + part(u) * p.dim + d, p.dim - d);
         const float w = u - units.x < kWave ? __shfl(mine, u - units.x) : weight(p.lse2[part(u)]);
-        if (w != 0.0f) acc += w * v;
+        acc += w * v;
     }
     if (waves > 1) {
         *(Quad *)&shared[wave][d] = acc;

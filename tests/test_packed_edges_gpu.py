@@ -92,6 +92,32 @@ def test_one_row_that_sees_much_among_many_that_see_little(dtype):
         check("lse", lse[only], *want["lse"])
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("heads_q,heads_k,dim", [(4, 2, 64), (12, 2, 72), (40, 2, 128), (2, 1, 160), (12, 2, 256)])
+def test_a_seen_nan_stays_however_the_row_is_cut(dtype, heads_q, heads_k, dim):
+    """Scores of neighbouring states one apart, so that all weights but those of the last hundred states are zero.  A state that is
+    seen and NaN in a group of v leaves NaN in that group, wherever it lies: in the part of another unit than the greatest score,
+    another wave's tile, or the same tile."""
+    keys, group = 6000, heads_q // heads_k
+    k, v = packed_of(torch.arange(keys, device=DEV, dtype=F32)[:, None, None].expand(keys, heads_k, dim).contiguous()), packed_of(rand(3, keys, heads_k, dim))
+    one = torch.ones(1, heads_q, dim, dtype=dtype, device=DEV)
+    groups = plain.groups(dim)
+    for rows, n in ((1, keys), (5, keys), (520, 4000), (1, 500)):       # cut among units, five rows of them, a workgroup each, one workgroup
+        q = one.expand(rows, heads_q, dim).contiguous()
+        first = keys - n
+        ranges = ranges_of((first, keys)).expand(rows, 2).contiguous()
+        want = attend_run(q, k, v, ranges, 1.0 / dim)
+        assert bool(torch.isfinite(want[0]).all())
+        for at in (first, first + 70, first + n // 3, keys - 200, keys - 1):
+            g, bad = at % groups, hp.Packed(v.codes, v.scales.clone())
+            bad.scales[at, 0, g, at % 2] = float("nan")                  # step or low of a group of the first state head
+            got = attend_run(q, k, bad, ranges, 1.0 / dim)
+            nan = torch.zeros_like(got[0], dtype=torch.bool)
+            nan[:, :group, 32 * g:32 * g + 32] = True
+            assert torch.equal(torch.isnan(got[0]), nan), (rows, at - first)
+            assert torch.equal(got[0][~nan], want[0][~nan]) and torch.equal(got[1], want[1])
+
+
 def test_rows_that_all_see_nothing():
     for rows, keys in ((1, 50), (3, 5000), (200, 900), (600, 10), (4, 0)):
         q, k = rand(1, rows, 4, 64), packed_of(rand(2, keys, 2, 64))
