@@ -205,7 +205,7 @@ constexpr float kLag = 8.0f;                       // the maximum is raised when
 // or four of 40 do not share: 1024 of these took two turns, 64 requests 88 us instead of 77).
 template <int GP> constexpr int kWaves = GP == 8 ? 7 : 4;
 template <class T, int GP, bool SIDE = false> constexpr int kResident = SIDE && GP <= 3 ? 3 : sizeof(T) == 2 || SIDE ? (GP <= 3 ? 4 : GP == 4 ? 3 : 1) : (GP <= 2 ? 3 : GP <= 4 ? 2 : 1);
-// Few tiles: one workgroup for each tile of heads, with more waves.
+// One row of few tiles: one workgroup for each tile of heads, with more waves.
 constexpr int kMostWaves = 8;
 template <int GP> constexpr int kFewWaves = GP == 8 ? 7 : kMostWaves;
 template <class T, int GP, int WAVES, bool SIDE> constexpr int kWavesASimd = WAVES == kWaves<GP> ? (WAVES * kResident<T, GP, SIDE> + 3) / 4 : (WAVES + 3) / 4;
@@ -584,12 +584,14 @@ bool side_by_side(const hp_packed_attend_args_t &a) { return a.dtype == HP_F32 &
 
 // Units of each tile of heads, and whether they are workgroups of more waves.
 //
-// Up to two tiles a wave of such a workgroup are left in one, which needs no join: one request of 576 states 10 us, with units
-// of one tile a wave and the launch that joins them 13; 2000 states so, in two units, took 17 us and took 12.6 with smaller
-// ones.  Others get as many units as run at once.  Sharing out evenly costs rows of like lengths the cuts and the join (256
-// requests of 500 states 60 us, with a workgroup each 51; of 50 to 2000 states 105 and 96), but nobody knows here how long the
-// longest is, and of 20000 states one workgroup would have 80 tiles a wave.  More than kMostShared rows, whose lengths no wave
-// adds up by itself, are a workgroup each (513 requests of 50 to 2000 states 180 us, 512 shared out 176).
+// One row of up to two tiles a wave of such a workgroup is left in one, which needs no join: one request of 63, 576 and 1000
+// states 7.8, 10.1 and 12.3 us, shared out with the launch that joins its parts 10.3, 12.5 and 12.6 (32 heads of 128 on 8); 2000
+// states in two such workgroups took 17 us and took 12.6 with smaller ones.  Several rows are not, however little each sees: the
+// workgroup would take them one behind the other, 5 us each (2 requests of 60 states 13 us, shared out 10; 8 of 7 states 44 and
+// 10; 16 of 3 states 84 and 10).  All others get as many units as run at once.  Sharing out evenly costs rows of like lengths the
+// cuts and the join (256 requests of 500 states 60 us, with a workgroup each 51; of 50 to 2000 states 105 and 96), but nobody
+// knows here how long the longest is, and of 20000 states one workgroup would have 80 tiles a wave.  More than kMostShared rows,
+// whose lengths no wave adds up by itself, are a workgroup each (513 requests of 50 to 2000 states 180 us, 512 shared out 176).
 struct Cut {
     int32_t units;
     bool few;
@@ -598,7 +600,7 @@ Cut cut_of(const hp_packed_attend_args_t &a) {
     const int64_t columns = (int64_t)a.heads_k * head_tiles_of(a), tiles = a.keys / kTile + 1;
     if (a.rows > kMostShared || a.rows * (tiles + kMostWaves) > INT_MAX) return Cut{0, false};
     const int groups = groups_of(a.dim), waves = groups <= 4 ? kWaves<4> : kWaves<8>;
-    if (a.rows * tiles <= 2 * (groups <= 4 ? kFewWaves<4> : kFewWaves<8>)) return Cut{1, true};
+    if (a.rows == 1 && tiles <= 2 * (groups <= 4 ? kFewWaves<4> : kFewWaves<8>)) return Cut{1, true};
     const int64_t slots = kComputeUnits * (a.dtype == HP_BF16 ? resident_of<__bf16>(groups) : side_by_side(a) ? resident_of<float, true>(groups) : resident_of<float>(groups));
     const int64_t fit = slots / columns, most = (a.rows * (tiles + waves) + waves - 1) / waves, units = fit < most ? fit : most;
     return Cut{(int32_t)(units > 1 ? units : 1), false};

@@ -118,6 +118,19 @@ def test_a_seen_nan_stays_however_the_row_is_cut(dtype, heads_q, heads_k, dim):
             assert torch.equal(got[0][~nan], want[0][~nan]) and torch.equal(got[1], want[1])
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("heads_q,heads_k,dim", [(8, 2, 64), (3, 3, 72), (17, 1, 128), (16, 2, 256)])
+def test_a_few_rows_of_a_few_states(dtype, heads_q, heads_k, dim):
+    for rows, keys in ((1, 1), (1, 63), (1, 900), (2, 1), (2, 447), (3, 319), (5, 190), (8, 127), (15, 61), (16, 63)):
+        q, k, v = rand(1, rows, heads_q, dim, dtype=dtype), packed_of(rand(2, keys, heads_k, dim, dtype=dtype)), packed_of(rand(3, keys, heads_k, dim, dtype=dtype))
+        attend_check(q, k, v, None)
+        lo = torch.arange(rows) * keys // rows
+        ranges = torch.stack([lo, (torch.arange(rows) + 1) * keys // rows], 1).to(torch.int32).to(DEV).contiguous()
+        out, lse = attend_check(q, k, v, ranges)
+        none = ranges[:, 0] == ranges[:, 1]
+        assert not bool(out[none].any()) and bool((lse[none] == float("-inf")).all())
+
+
 def test_rows_that_all_see_nothing():
     for rows, keys in ((1, 50), (3, 5000), (200, 900), (600, 10), (4, 0)):
         q, k = rand(1, rows, 4, 64), packed_of(rand(2, keys, 2, 64))

@@ -129,6 +129,20 @@ def test_attend_workspace():
     assert L.hp_pack(None, None) == L.hp_unpack(None, None) == L.hp_packed_linear(None, None) == HP_EINVAL
 
 
+def test_several_rows_of_few_states_are_not_one_workgroups():
+    """A workgroup goes through its rows one behind the other.  The scratch memory says how many units share them: two places of
+    partial results each."""
+    size = lambda **kw: pk._lib().hp_packed_attend_workspace(C.byref(attend_args(**kw)))  # noqa: E731
+    whole = lambda n: (n + 15) // 16 * 16  # noqa: E731
+    for heads_q, heads_k, dim in ((32, 8, 128), (1, 1, 64), (16, 2, 256), (16, 16, 72)):
+        for dtype in (0, 1):
+            of = lambda units, rows: whole(4 * 2 * units * heads_q * dim) + whole(4 * 2 * units * heads_q) + whole(8 * rows)  # noqa: E731
+            sizes = dict(dtype=dtype, heads_q=heads_q, heads_k=heads_k, dim=dim)
+            for rows, keys in ((2, 0), (2, 120), (2, 447), (3, 319), (5, 190), (8, 127), (15, 61), (16, 63), (16, 0)):
+                assert size(rows=rows, keys=keys, **sizes) >= of(rows, rows)
+            assert size(rows=1, keys=800, **sizes) == of(1, 1)         # a single one's are
+
+
 # ---- linear ----------------------------------------------------------------------------------------------------------
 
 def linear_args(**kw):
