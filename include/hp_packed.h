@@ -78,8 +78,16 @@ int hp_unpack(const hp_pack_args_t *args, void *stream);
  * values enter as they are, not rounded to the type.  In HP_BF16 two numbers on the way
  * are rounded to 16 bits, the weights P and P * step, operands of matrix products
  * (HP_F32: none).  Sums on the way may be 2^11 times the number of states times the largest
- * value of v: values from 2^90 on are not safe from overflow.  A state that is seen and is NaN in a group of v leaves NaN in that
- * group's channels; queries that are not finite, NaN in their head's.
+ * value of v: values from 2^90 on are not safe from overflow; nor are queries from 2^118 on
+ * (HP_F32: 2^122), or those whose sum over the channels of |q| times the largest value of k
+ * is 2^125 or more, before the scale.  A state that is seen and is NaN in a group of v leaves
+ * NaN in that group's channels, whatever its weight; queries that are not finite, NaN in
+ * their head's.
+ * How a call is cut goes by its rows and by the rows of the cache, not by what ranges leave of
+ * them: one row of up to 1023 states (dim above 128: 895) is one launch, longer caches and
+ * several rows are shared out and joined by a second.  A short request in a large cache is
+ * faster if k and v are the rows that it sees (32 heads of 128 on 8, one row of 576 states:
+ * 10.2 us, in a cache of 100000: 12.5).
  *   q, out: [rows, heads_q, dim]; k, v: [keys, heads_k, dim]; dim 1..HP_ATTEND_MAX_DIM.
  *   Limits are hp_cross_attend_step's; row strides of packed states up to 2^24 (HP_ELAYOUT),
  *   none negative.
@@ -106,7 +114,11 @@ int64_t hp_packed_attend_workspace(const hp_packed_attend_args_t *args);
 /* hp_packed_linear - out[r][n] = sum_k x[r][k] w[n][k] for x [rows, n_in], packed w
  * [n_out, n_in] (one head: head strides are not read) and out [rows, n_out].  Sums are in
  * binary32, the weights' values are not rounded (in HP_BF16 the part of the lows may be off
- * by 2^-18 of 16 step + |low| times a group's sum of x); out may not overlap x; a row of x that is not finite gives NaN.
+ * by 2^-18 of 16 step + |low| times a group's sum of x); out may not overlap x; a row of x that
+ * is not finite gives NaN.  Sums on the way may be 32 times a group's sum of |x| (HP_F32: twice
+ * it), and 8 times what these sums of |x|, each times its group's largest value in w's row, add
+ * up to: values of x from 2^118 on (HP_F32: 2^122) are not safe from overflow, and the latter
+ * has to stay below 2^128.
  * Made for the rows of a decoding step: up to 32 rows at a time share a pass over the
  * weights.  Fastest where x is 16-byte aligned and its rows and their stride
  * are multiples of 16 bytes.

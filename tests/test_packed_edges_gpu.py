@@ -199,6 +199,28 @@ def test_large_and_small_values(dtype):
             check("out", out, *plain.linear(a, p))
 
 
+@pytest.mark.parametrize("dtype,most", [(BF16, 118), (F32, 122)])
+def test_the_largest_values_whose_sums_are_safe(dtype, most):
+    """Activations and queries of one sign right below the sizes that the header names.  A group's sum of |x| is 2^(most + 5) at
+    most; weights below 2^-4 leave 8 times what adds up over ten groups below 2^128."""
+    g = torch.Generator(device=DEV).manual_seed(7)
+    largest = 2.0 ** most * (1 - unit(dtype))
+    for rows in (3, 16, 40):
+        x = (largest * (1 - torch.rand(rows, 320, generator=g, device=DEV) / 64)).to(dtype)
+        x[1], x[2, 7:] = largest, -largest
+        for n_in, w in ((320, 2.0 ** -4 * (2 * torch.rand(50, 320, generator=g, device=DEV) - 1)), (317, torch.full((50, 317), 2.0 ** -20, device=DEV))):
+            p, out = packed_of(w.to(dtype)), torch.empty(rows, 50, dtype=dtype, device=DEV)
+            a = x[:, :n_in].contiguous()
+            assert float(a.abs().max()) == largest
+            hp.hp_packed_linear(a, p, out)
+            check("out", out, *plain.linear(a, p))
+    for heads_q, heads_k, dim in ((6, 2, 96), (5, 1, 256)):
+        q, k, v = torch.full((4, heads_q, dim), largest, dtype=dtype, device=DEV), rand(2, 700, heads_k, dim, dtype=dtype), packed_of(rand(3, 700, heads_k, dim, dtype=dtype))
+        q[1] *= 1 - torch.rand(heads_q, dim, generator=g, device=DEV).to(dtype) / 2
+        q[2] = -q[2]
+        attend_check(q, packed_of(k / 2.0 ** most), v, None)
+
+
 # ---- far apart ----------------------------------------------------------------------------------------------------------
 
 def test_caches_whose_places_pass_32_bits():
