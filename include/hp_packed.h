@@ -85,7 +85,8 @@ int hp_unpack(const hp_pack_args_t *args, void *stream);
  * their head's.
  * How a call is cut goes by its rows and by the rows of the cache, not by what ranges leave of
  * them: one row of up to 1023 states (dim above 128: 895) is one launch, longer caches and
- * several rows are shared out and joined by a second.  A short request in a large cache is
+ * several rows are shared out and joined by a second, where a row's last bits may go by the
+ * other rows' ranges (up to 512 rows; of more, each is by itself).  A short request in a large cache is
  * faster if k and v are the rows that it sees (32 heads of 128 on 8, one row of 576 states:
  * 10.2 us, in a cache of 100000: 12.5).
  *   q, out: [rows, heads_q, dim]; k, v: [keys, heads_k, dim]; dim 1..HP_ATTEND_MAX_DIM.

@@ -3,7 +3,8 @@
 // A lane that packs takes 16 channels, half a group, and one row after the other; one that reads back 8.  (Eight when packing,
 // four lanes a group: four times the group's arithmetic for one use.)  Bound by memory, 2 (or 4) bytes and 0.625 a value, and a
 // copy of as much takes what this does but for the last twentieth: 40139 rows of 8 heads of 128, k and v, packed and read back,
-// 432 MB, 87 us (83 at the rate of a large copy).  Binary32 rows of heads of 72, the last group of 8: 37 us for 124 MB (24).
+// 432 MB, 87 us (83 at the rate of a large copy).  Binary32 rows of heads of 72, the last group of 8: 37 us for 124 MB
+// (24); 123 MB of whole groups, heads of 128, take 29, so it is the short group that costs (bfloat16 alike: 57 us and 36).
 #include <cfloat>
 #include <cmath>
 

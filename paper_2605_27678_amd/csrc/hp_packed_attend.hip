@@ -15,10 +15,12 @@
 // weights (in binary32 they lie there as they are); 8 sum p step + sum p low come from one more product.
 //
 // A state and head are 5 bits a channel of k and of v, each read once, so memory bounds it: 288 MB of 64 requests are 56 us at
-// the rate of a large copy.  It takes 72, and 5 more for the join; the same loads without the computing take 66, behind
-// which the computing hides where three waves share a SIMD.  Heads of 256 leave it one or two: 36 us for 110 MB (a copy 21).
+// the rate of a large copy.  It takes 72, and 5 more for the join, which with the same loads without the computing are 63: most
+// of the computing hides where three waves share a SIMD.  Heads of 256 leave it one or two: 46 us for 110 MB (a copy 21), 31
+// without the computing; heads of 129 to 224 have as many registers, LDS and loads (of 160, 69 MB: 42).
 // Where rows are short, what begins and ends them counts: 30 requests of 1 to 2305 states, 16 heads of 72, 53 MB (a copy
-// 10) take 31 us in bfloat16, 37 in binary32; per added MB they take no more than a copy, and 1.7 times as much.
+// 10) take 32 us in bfloat16, 38 in binary32 (21 without the computing); per added MB they take no more than a copy, and 1.7
+// times as much.
 // Sets of heads side by side in a product's columns (few heads share a state head) took a quarter less arithmetic and no
 // less time; rings of three tiles instead of two leave room for fewer waves (64 requests 113 us).
 #include <climits>

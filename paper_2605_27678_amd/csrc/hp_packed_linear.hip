@@ -11,8 +11,10 @@
 // (12288 x 12288 by 16 rows: 36 us, this way 29).
 //
 // The weights are 5 bits a value, read once by up to 32 rows: 95 MB of these 12288 x 12288 are 18 us at the rate of a large
-// copy, and the loads alone take 27.  With more rows the caches are busier with x: of 8192 x 8192 by 64 rows every compute
-// unit reads half of x, 0.5 MB, for its 64 rows of w, 128 MB next to 2 x 44; that takes 25 us, where a copy of the 44 MB takes 9.
+// copy.  The call takes 29 with nothing in the caches (26 where the 256 MB cache has a part of them), its loads without the
+// computing 27.  With more rows the caches are busier with x: of 8192 x 8192 by 64 rows every compute unit reads half of x,
+// 0.5 MB, for its 64 rows of w, 128 MB next to 2 x 44; that takes 25 us, the loads alone 18, where a copy of the 44 MB takes 9.
+// Binary32 has three products for each: 60 us.
 #include "hp_packed.hpp"
 
 #pragma clang fp contract(fast)
@@ -189,7 +191,8 @@ template <class C> __global__ __launch_bounds__(kBlock) void packed_linear_kerne
         } else {
 #pragma unroll
             for (int n = 0; n < C::kXLoads; ++n) *(Piece *)(stage(i) + (n * kWave + lane) * 16) = held[n];
-            // the pieces came behind w's chunk i
+            // w's chunk i came before the pieces; this waits for the chunk asked for last as well, so that what is further
+            // ahead than the next one is not of use here
             __builtin_amdgcn_s_waitcnt(but(0));
 #pragma unroll
             for (int n = 0; n < C::kXLoads; ++n) held[n] = *(const typename VecOf<T, C::kPiece>::mem *)(from_row(n) + group_of(i + 1 < chunks ? i + 1 : i) * kGroup);
@@ -266,9 +269,9 @@ template <class C> dim3 blocks_of(Params &p) {
 
 // The first of these cuts, the smallest, of which the compute units take all workgroups at once; otherwise the last.  A
 // larger tile reads x and waits for the join less often, a second turn costs as much as the first (us, bfloat16, each cut by itself):
-//   4096 x 4096 by 16 rows in tiles of 16 / 32 rows of w   6.0 / 7.1      12288 x 12288: 16 / 32 / 48 / 64   36 / 37 / 29 / 30
-//   8192 x 2048 by 64 rows in tiles of 16 x 32 / 32 x 32 / 32 x 64 (rows of x times rows of w)   11.5 / 14.8 / 22
-//   8192 x 8192 by 64 rows, the same                                                             47 / 31 / 25
+//   4096 x 4096 by 16 rows in tiles of 16 / 32 rows of w   6.0 / 7.1      12288 x 12288: 16 / 32 / 48 / 64   46 / 38 / 29 / 30
+//   8192 x 2048 by 64 rows in tiles of 16 x 32 / 32 x 32 / 32 x 64 (rows of x times rows of w)   11.3 / 14.7 / 22
+//   8192 x 8192 by 64 rows, the same                                                             45 / 30 / 25
 // Up to four rows in bfloat16 are the exception: their workgroups are small enough that several share a compute unit, and
 // tiles of 16 were the fastest throughout (12288 x 4096 by one row 8.6, of 48 11.6; 28672 x 4096 17.7 and 23.3).
 template <class C, class... More> void launch(Params &p, hipStream_t s) {
@@ -283,8 +286,8 @@ template <class C, class... More> void launch(Params &p, hipStream_t s) {
 // chunk of 128 channels 25 us, two of 64 in turn 28; 4096 x 4096 by 16 rows: three of 64 6.0, one of 128 6.5).  Where workgroups
 // are small, two chunks in turn leave room for four of them (28672 x 4096 by one row 17.7 us, four chunks 21.2).
 //
-// Rows of x that are no whole aligned pieces of 16 bytes pass through registers and wait for themselves (12288 x 8195 by 16
-// rows: 40 us, of 8192 about 20).  Binary32 has three products for one and twice x's bytes.
+// Rows of x that are no whole aligned pieces of 16 bytes pass through registers, and each chunk waits for x's and w's next
+// (12288 x 8195 by 16 rows: 40 us, of 8192 21).  Binary32 has three products for one and twice x's bytes.
 template <class T> void choose(Params &p, hipStream_t s) {
     constexpr int kPiece = 16 / sizeof(T);
     const bool exact = (uintptr_t)p.x % 16 == 0 && p.n_in % kPiece == 0 && p.x_stride % kPiece == 0 && p.x_stride >= 0 && p.x_stride <= kMostStride / 4;
