@@ -131,6 +131,19 @@ def test_a_few_rows_of_a_few_states(dtype, heads_q, heads_k, dim):
         assert not bool(out[none].any()) and bool((lse[none] == float("-inf")).all())
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("heads,dim", [(1030, 32), (600, 128), (260, 256)])
+def test_several_rows_of_so_many_heads_that_each_has_one_unit(dtype, heads, dim):
+    rows, keys = 9, 300
+    q, k, v = rand(1, rows, heads, dim, dtype=dtype), packed_of(rand(2, keys, heads, dim)), packed_of(rand(3, keys, heads, dim))
+    ranges = ranges_of((0, 300), (5, 5), (7, 8), (0, 64), (1, 66), (250, 400), (9, 2), (100, 229), (299, 300))
+    out, lse = attend_run(q, k, v, ranges)
+    for h in (slice(0, 3), slice(heads - 3, heads)):
+        want = plain.attend(q[:, h], hp.Packed(k.codes[:, h], k.scales[:, h]), hp.Packed(v.codes[:, h], v.scales[:, h]), ranges, dim ** -0.5)
+        check("out", out[:, h], *want["out"])
+        check("lse", lse[:, h], *want["lse"])
+
+
 def test_rows_that_all_see_nothing():
     for rows, keys in ((1, 50), (3, 5000), (200, 900), (600, 10), (4, 0)):
         q, k = rand(1, rows, 4, 64), packed_of(rand(2, keys, 2, 64))
